@@ -437,6 +437,116 @@ ar_status ar_genmodel_select_tiered(int32_t n, int64_t N, int32_t dtype, const d
                                     int32_t* kind, int32_t* num_levels, int32_t* fanin,
                                     double* seconds);
 
+/* ----------------------------------------------------- replica operators */
+
+/* What a data-parallel replica computes between two AllReduces, from tokens
+ * to the gradients that an ar_plan sums: an embedding lookup and its
+ * gradient, a gated feed-forward block and its gradients, and a distillation
+ * loss with its gradient.  Common to all of them:
+ *   - dtype is AR_F32 or AR_BF16 (AR_ERR_UNSUPPORTED for AR_I32) and is that
+ *     of every matrix.  Sums, softmax statistics and products accumulate in
+ *     fp32; a bf16 result is rounded once (round to nearest even) unless the
+ *     call says more.  Results do not depend on timing: the same call on the
+ *     same inputs gives the same bits.
+ *   - A matrix is a device pointer and a row stride in elements, at least its
+ *     width; the elements of a row are adjacent.  Any alignment to the
+ *     element size works (AR_ERR_INVALID_ARG below that); rows at 16-byte
+ *     boundaries are faster.  Offsets are 64-bit.  Widths and row counts are
+ *     at most 2^31 - 1, unless the call says less (AR_ERR_UNSUPPORTED).
+ *   - Buffers live on the current device.  An output must not overlap
+ *     another output or an input (AR_ERR_INVALID_ARG), except where stated.
+ *   - `stream` is a hipStream_t; a call enqueues kernel launches on it and
+ *     returns.  No call allocates device memory, copies from the host or
+ *     waits, so each may be captured into a HIP graph.  Where a call takes a
+ *     workspace, it needs as many bytes as the function named with it
+ *     returns (AR_ERR_INVALID_ARG with the size in ar_last_error for fewer,
+ *     or for one not aligned to 16 bytes); its contents need no
+ *     initialisation and mean nothing after the call, and calls that may
+ *     overlap need one each.
+ *   - Zero rows, or zero columns, are valid and leave outputs that have
+ *     elements at the value of an empty sum.  Pointers of empty matrices may
+ *     be NULL. */
+
+/* out[t, :] = scale * table[ids[t], :] for t < T; table is V x D, out T x D.
+ * An id outside [0, V) is no token: its row of out is zero. */
+ar_status ar_embed_lookup(int32_t dtype, int64_t V, int64_t D, int64_t T, const void* table,
+                          int64_t table_stride, const int64_t* ids, float scale, void* out,
+                          int64_t out_stride, void* stream);
+
+/* The gradient of ar_embed_lookup's table:
+ *   dtable[v, :] = scale * (sum of dout[t, :] over t with ids[t] = v)
+ * for every v < V (rows no token has become zero), or, with accumulate != 0,
+ * dtable[v, :] += that (rows no token has are not touched).  Ids outside
+ * [0, V) add nothing.  The sum takes t in increasing order, in runs of
+ * AR_EMBED_RUN tokens whose sums are then added in order, all in fp32; the
+ * product with scale and the sum with the old value are fp32 as well.
+ * V, T <= 2^31 - 1. */
+#define AR_EMBED_RUN 32
+ar_status ar_embed_grad_workspace(int64_t V, int64_t D, int64_t T, int64_t* bytes);
+ar_status ar_embed_grad(int32_t dtype, int64_t V, int64_t D, int64_t T, const void* dout,
+                        int64_t dout_stride, const int64_t* ids, float scale, int32_t accumulate,
+                        void* dtable, int64_t dtable_stride, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
+/* The gated feed-forward block's first half, h = a(x Wg^T) * (x Wu^T): x is
+ * M x D, Wg and Wu are F x D, h is M x F.  Both projections, the activation
+ * and the product run as one kernel on fp32 accumulators; h is rounded once.
+ *   AR_ACT_SILU   a(g) = g / (1 + exp(-g))
+ *   AR_ACT_GELU   a(g) = g (1 + erf(g / sqrt 2)) / 2
+ * For a backward pass the call also stores the two factors that the chain
+ * rule needs, each rounded once to dtype: saved_gate = a'(g) u and saved_up =
+ * a(g) (M x F, a common stride; both NULL for a forward pass alone). */
+typedef enum ar_act { AR_ACT_SILU = 0, AR_ACT_GELU = 1 } ar_act;
+#define AR_GLU_MAX_EXTENT 4194304 /* M, D and F (AR_ERR_UNSUPPORTED above) */
+ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_t D, int64_t F,
+                         const void* x, int64_t x_stride, const void* wg, const void* wu,
+                         int64_t w_stride, void* h, int64_t h_stride, void* saved_gate,
+                         void* saved_up, int64_t saved_stride, void* workspace,
+                         int64_t workspace_bytes, void* stream);
+
+/* The gradients of the block for dh = dL/dh (M x F), from what the forward
+ * pass saved: with dg = dh * saved_gate and du = dh * saved_up (rounded once
+ * to dtype, held in the workspace),
+ *   dx = dg Wg + du Wu,  dwg = dg^T x,  dwu = du^T x,
+ * or, with accumulate != 0, dwg and dwu += those (dx is always stored).  dx,
+ * or dwg and dwu together, may be NULL and are then not computed. */
+ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t F, const void* dh,
+                          int64_t dh_stride, const void* x, int64_t x_stride, const void* wg,
+                          const void* wu, int64_t w_stride, const void* saved_gate,
+                          const void* saved_up, int64_t saved_stride, int32_t accumulate,
+                          void* dx, int64_t dx_stride, void* dwg, void* dwu, int64_t dw_stride,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+
+/* The larger of the two calls' workspaces (backward == 0: the forward
+ * call's alone). */
+ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_t F, int32_t backward,
+                           int64_t* bytes);
+
+/* Distillation from a teacher's top logits.  For row t < T: z = logits[t, :]
+ * (V of them), and up to K entries (i, s) = (ids[t, k], teacher[t, k]); an
+ * entry whose id is outside [0, V) or whose s is -inf is absent.  With
+ *   p = softmax over the present entries of s / temperature,
+ *   q = softmax over all V of z / temperature,
+ *   loss[t]    = weights[t] temperature^2 sum_k p_k (log p_k - log q[i_k])
+ *   grad[t, j] = weights[t] temperature (q_j - sum of p_k with i_k = j),
+ * the gradient of the losses' sum; weights NULL means all 1.  A row whose
+ * weight is 0, that has no present entry, or whose logits are all -inf has
+ * loss 0 and gradient 0 whatever else it holds, NaN and infinities included.
+ * Elsewhere a logit of NaN or +inf makes the row's loss and gradient NaN, such
+ * a teacher entry the loss and the gradient at the entries' ids; a masked
+ * student logit of -inf at an entry with p > 0 gives loss +inf and a finite
+ * gradient.  teacher_dtype may
+ * differ from dtype; loss and weights are fp32 vectors.  grad may be NULL
+ * (the loss alone), or logits itself with the same stride (in place).
+ * K <= AR_DISTILL_MAX_K (AR_ERR_UNSUPPORTED above); temperature finite and > 0. */
+#define AR_DISTILL_MAX_K 4096
+ar_status ar_distill_workspace(int64_t T, int64_t V, int64_t K, int64_t* bytes);
+ar_status ar_distill(int32_t dtype, int64_t T, int64_t V, int64_t K, const void* logits,
+                     int64_t logits_stride, int32_t teacher_dtype, const void* teacher,
+                     int64_t teacher_stride, const int64_t* ids, int64_t ids_stride,
+                     float temperature, const float* weights, float* loss, void* grad,
+                     int64_t grad_stride, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* --------------------------------------------------------------- timing */
 
 /* A timer holds up to `capacity` launch records (capacity >= 1).  Its HIP

@@ -96,6 +96,20 @@ _sig = {
     "ar_genmodel_select": [c_int32, c_int64, c_int32, POINTER(c_double), c_int64, c_int32,
                            POINTER(c_int32), POINTER(c_int32), POINTER(c_int32),
                            POINTER(c_double)],
+    "ar_embed_lookup": [c_int32, c_int64, c_int64, c_int64, _P, c_int64, _P, c_float, _P, c_int64,
+                        _P],
+    "ar_embed_grad_workspace": [c_int64, c_int64, c_int64, POINTER(c_int64)],
+    "ar_embed_grad": [c_int32, c_int64, c_int64, c_int64, _P, c_int64, _P, c_float, c_int32, _P,
+                      c_int64, _P, c_int64, _P],
+    "ar_glu_workspace": [c_int32, c_int64, c_int64, c_int64, c_int32, POINTER(c_int64)],
+    "ar_glu_forward": [c_int32, c_int32, c_int64, c_int64, c_int64, _P, c_int64, _P, _P, c_int64,
+                       _P, c_int64, _P, _P, c_int64, _P, c_int64, _P],
+    "ar_glu_backward": [c_int32, c_int64, c_int64, c_int64, _P, c_int64, _P, c_int64, _P, _P,
+                        c_int64, _P, _P, c_int64, c_int32, _P, c_int64, _P, _P, c_int64, _P,
+                        c_int64, _P],
+    "ar_distill_workspace": [c_int64, c_int64, c_int64, POINTER(c_int64)],
+    "ar_distill": [c_int32, c_int64, c_int64, c_int64, _P, c_int64, c_int32, _P, c_int64, _P,
+                   c_int64, c_float, _P, _P, _P, c_int64, _P, c_int64, _P],
     "ar_timer_create": [c_int64, POINTER(_P)],
     "ar_timer_reset": [_P],
     "ar_timer_read": [_P, c_int64, POINTER(c_int64), POINTER(c_int32),
@@ -358,6 +372,78 @@ def ar_genmodel_select(n, N, dtype, params, cache_bytes, max_levels=3):
                                    fan, ctypes.byref(sec)))
     name = {v: k for k, v in KINDS.items()}[kind.value]
     return name, (tuple(fan[i] for i in range(lv.value)) if lv.value else None), sec.value
+
+
+# ----------------------------------------------------- replica operators
+#
+# Pointers, strides and sizes as in the header; ``paper_2409_04202_amd.ops``
+# calls these with torch tensors.
+
+AR_ACT_SILU, AR_ACT_GELU = 0, 1
+ACTS = {"silu": AR_ACT_SILU, "gelu": AR_ACT_GELU}
+AR_EMBED_RUN = 32
+AR_DISTILL_MAX_K = 4096
+AR_GLU_MAX_EXTENT = 4194304
+
+
+def ar_embed_lookup(dtype, V, D, T, table, table_stride, ids, scale, out, out_stride, stream=None):
+    _check(_lib.ar_embed_lookup(_dtype(dtype), V, D, T, _ptr(table), table_stride, _ptr(ids), scale,
+                                _ptr(out), out_stride, _stream(stream)))
+
+
+def ar_embed_grad_workspace(V, D, T):
+    """The workspace's bytes."""
+    b = c_int64()
+    _check(_lib.ar_embed_grad_workspace(V, D, T, ctypes.byref(b)))
+    return b.value
+
+
+def ar_embed_grad(dtype, V, D, T, dout, dout_stride, ids, scale, accumulate, dtable, dtable_stride,
+                  workspace, workspace_bytes, stream=None):
+    _check(_lib.ar_embed_grad(_dtype(dtype), V, D, T, _ptr(dout), dout_stride, _ptr(ids), scale,
+                              int(accumulate), _ptr(dtable), dtable_stride, _ptr(workspace),
+                              workspace_bytes, _stream(stream)))
+
+
+def ar_glu_workspace(dtype, M, D, F, backward):
+    """The workspace's bytes."""
+    b = c_int64()
+    _check(_lib.ar_glu_workspace(_dtype(dtype), M, D, F, int(backward), ctypes.byref(b)))
+    return b.value
+
+
+def ar_glu_forward(dtype, act, M, D, F, x, x_stride, wg, wu, w_stride, h, h_stride, saved_gate,
+                   saved_up, saved_stride, workspace, workspace_bytes, stream=None):
+    _check(_lib.ar_glu_forward(_dtype(dtype), ACTS[act] if isinstance(act, str) else int(act), M, D,
+                               F, _ptr(x), x_stride, _ptr(wg), _ptr(wu), w_stride, _ptr(h),
+                               h_stride, _ptr(saved_gate), _ptr(saved_up), saved_stride,
+                               _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ar_glu_backward(dtype, M, D, F, dh, dh_stride, x, x_stride, wg, wu, w_stride, saved_gate,
+                    saved_up, saved_stride, accumulate, dx, dx_stride, dwg, dwu, dw_stride,
+                    workspace, workspace_bytes, stream=None):
+    _check(_lib.ar_glu_backward(_dtype(dtype), M, D, F, _ptr(dh), dh_stride, _ptr(x), x_stride,
+                                _ptr(wg), _ptr(wu), w_stride, _ptr(saved_gate), _ptr(saved_up),
+                                saved_stride, int(accumulate), _ptr(dx), dx_stride, _ptr(dwg),
+                                _ptr(dwu), dw_stride, _ptr(workspace), workspace_bytes,
+                                _stream(stream)))
+
+
+def ar_distill_workspace(T, V, K):
+    """The workspace's bytes."""
+    b = c_int64()
+    _check(_lib.ar_distill_workspace(T, V, K, ctypes.byref(b)))
+    return b.value
+
+
+def ar_distill(dtype, T, V, K, logits, logits_stride, teacher_dtype, teacher, teacher_stride, ids,
+               ids_stride, temperature, weights, loss, grad, grad_stride, workspace,
+               workspace_bytes, stream=None):
+    _check(_lib.ar_distill(_dtype(dtype), T, V, K, _ptr(logits), logits_stride,
+                           _dtype(teacher_dtype), _ptr(teacher), teacher_stride, _ptr(ids),
+                           ids_stride, temperature, _ptr(weights), _ptr(loss), _ptr(grad),
+                           grad_stride, _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 # ---------------------------------------------------------------- timing

@@ -1,0 +1,217 @@
+"""The replica operators on torch tensors.
+
+What a data-parallel replica computes between two AllReduces: an embedding
+lookup and its gradient, a gated feed-forward block and its gradients, a
+distillation loss and its gradient.  The functions here check their tensors,
+allocate what the caller did not give and call the C functions of the same
+names in ``paper_2409_04202_amd.arplan``, whose header says what each
+computes.  There is no fallback: all work is the library's kernels.
+
+Tensors are float32 or bfloat16 matrices on one GPU whose rows may have any
+stride (adjacent elements within a row), so gradients can be written straight
+into a slice of the vector that an AllReduce plan sums.  A call runs on
+``stream`` (a ``torch.cuda.Stream``), by default the device's current stream,
+and returns without waiting.  With another stream than the current one the
+caller orders it after the work that made the inputs, as for any torch call;
+what the call itself allocates belongs to the stream it runs on.  A
+``workspace`` (a uint8 tensor of at least the bytes the ``*_workspace``
+function of ``arplan`` names) is allocated where it is not given.
+
+Wrong shapes, types or devices raise ValueError; what the library refuses
+raises ``arplan.ArError``.
+"""
+
+import contextlib
+
+import torch
+
+from . import arplan
+
+_DT = {torch.float32: arplan.AR_F32, torch.bfloat16: arplan.AR_BF16}
+
+
+def _matrix(name, x, shape=None, like=None):
+    """The tensor's row stride, after checking that it is a matrix the library
+    takes: of ``like``'s type and device, of ``shape`` where that is given."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("%s: a two-dimensional tensor expected" % name)
+    if not x.is_cuda:
+        raise ValueError("%s: a GPU tensor expected" % name)
+    if like is None:
+        if x.dtype not in _DT:
+            raise ValueError("%s: float32 or bfloat16 expected, got %s" % (name, x.dtype))
+    elif x.dtype != like.dtype or x.device != like.device:
+        raise ValueError("%s: type and device differ from the first operand's" % name)
+    if shape is not None and tuple(x.shape) != tuple(shape):
+        raise ValueError("%s: shape %s expected, got %s" % (name, tuple(shape), tuple(x.shape)))
+    rows, cols = x.shape
+    if cols > 1 and x.stride(1) != 1:
+        raise ValueError("%s: the elements of a row have to be adjacent" % name)
+    return x.stride(0) if rows > 1 else max(cols, 1)
+
+
+def _ids(name, ids, like):
+    if not isinstance(ids, torch.Tensor) or ids.dtype != torch.int64 or ids.device != like.device:
+        raise ValueError("%s: an int64 tensor on the operands' device expected" % name)
+
+
+@contextlib.contextmanager
+def _on(like, stream, tensors):
+    """The stream a call runs on; its allocations are made there, and the
+    tensors it is given are marked as used there."""
+    with torch.cuda.device(like.device):
+        if stream is None or stream == torch.cuda.current_stream():
+            yield torch.cuda.current_stream().cuda_stream
+            return
+        with torch.cuda.stream(stream):
+            yield stream.cuda_stream
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _space(workspace, need, like):
+    """(pointer, bytes) of the workspace, and what keeps it alive."""
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+    elif (workspace.dtype != torch.uint8 or workspace.device != like.device
+          or not workspace.is_contiguous()):
+        raise ValueError("workspace: a contiguous uint8 tensor on the operands' device expected")
+    return workspace.data_ptr(), workspace.numel(), workspace
+
+
+# ------------------------------------------------------------- embedding
+
+def embed_lookup(table, ids, scale=1.0, out=None, stream=None):
+    """``scale * table[ids]``, a row of zeros where an id is outside the table:
+    (..., D) for ids of shape (...), or ``out`` (T, D)."""
+    st = _matrix("table", table)
+    _ids("ids", ids, table)
+    V, D = table.shape
+    T = ids.numel()
+    with _on(table, stream, (table, ids, out)) as s:
+        flat = ids if ids.is_contiguous() else ids.contiguous()
+        if out is None:
+            res = torch.empty(ids.shape + (D,), dtype=table.dtype, device=table.device)
+            so = max(D, 1)
+        else:
+            res, so = out, _matrix("out", out, (T, D), table)
+        arplan.ar_embed_lookup(_DT[table.dtype], V, D, T, table, st, flat, scale, res, so, s)
+    return res
+
+
+def embed_grad(dout, ids, dtable, scale=1.0, accumulate=False, workspace=None, stream=None):
+    """The gradient of ``embed_lookup``'s table for ``dout`` (T, D), stored
+    into ``dtable`` (V, D), all of it, or added to it; returns ``dtable``."""
+    sd = _matrix("dout", dout)
+    st = _matrix("dtable", dtable, None, dout)
+    _ids("ids", ids, dout)
+    T, D = dout.shape
+    V = dtable.shape[0]
+    if dtable.shape[1] != D or ids.numel() != T:
+        raise ValueError("dtable has to be as wide as dout, and ids one a row of dout")
+    with _on(dout, stream, (dout, ids, dtable, workspace)) as s:
+        flat = ids if ids.is_contiguous() else ids.contiguous()
+        w, n, keep = _space(workspace, arplan.ar_embed_grad_workspace(V, D, T), dout)
+        arplan.ar_embed_grad(_DT[dout.dtype], V, D, T, dout, sd, flat, scale, accumulate, dtable,
+                             st, w, n, s)
+    return dtable
+
+
+# ---------------------------------------------------- gated feed-forward
+
+def glu_forward(x, wg, wu, act="silu", save=False, out=None, workspace=None, stream=None):
+    """``act(x wg^T) * (x wu^T)`` for x (M, D) and wg, wu (F, D): (M, F).  With
+    ``save`` returns it and what ``glu_backward`` needs, a (2, M, F) tensor."""
+    sx = _matrix("x", x)
+    M, D = x.shape
+    sw = _matrix("wg", wg, None, x)
+    F = wg.shape[0]
+    su = _matrix("wu", wu, (F, D), x)
+    if wg.shape[1] != D:
+        raise ValueError("wg: as wide as x expected")
+    if su != sw:
+        raise ValueError("wg and wu: one row stride expected")
+    if act not in arplan.ACTS:
+        raise ValueError("act: one of %s expected" % ", ".join(sorted(arplan.ACTS)))
+    with _on(x, stream, (x, wg, wu, out, workspace)) as s:
+        h = torch.empty(M, F, dtype=x.dtype, device=x.device) if out is None else out
+        sh = _matrix("out", h, (M, F), x)
+        saved = torch.empty(2, M, F, dtype=x.dtype, device=x.device) if save else None
+        a, b = (saved[0], saved[1]) if save else (None, None)
+        w, n, keep = _space(workspace, arplan.ar_glu_workspace(_DT[x.dtype], M, D, F, False), x)
+        arplan.ar_glu_forward(_DT[x.dtype], act, M, D, F, x, sx, wg, wu, sw, h, sh, a, b,
+                              max(F, 1), w, n, s)
+    return (h, saved) if save else h
+
+
+def glu_backward(dh, x, wg, wu, saved, dx=None, dwg=None, dwu=None, accumulate=False,
+                 workspace=None, stream=None):
+    """(dx, dwg, dwu) for ``dh`` (M, F), the gradient at ``glu_forward``'s
+    result, and what that saved.  Outputs that are given are written in place;
+    with ``accumulate`` dwg and dwu are added to (and have to be given)."""
+    sh = _matrix("dh", dh)
+    M, F = dh.shape
+    sx = _matrix("x", x, None, dh)
+    D = x.shape[1]
+    if x.shape[0] != M:
+        raise ValueError("x: a row for each of dh's expected")
+    sw = _matrix("wg", wg, (F, D), dh)
+    if _matrix("wu", wu, (F, D), dh) != sw:
+        raise ValueError("wg and wu: one row stride expected")
+    if (not isinstance(saved, torch.Tensor) or saved.dim() != 3 or saved.shape[0] != 2):
+        raise ValueError("saved: what glu_forward saved expected")
+    sg, su = saved[0], saved[1]
+    ss = _matrix("saved", sg, (M, F), dh)
+    if _matrix("saved", su, (M, F), dh) != ss:
+        raise ValueError("saved: one row stride expected")
+    if (dwg is None) != (dwu is None):
+        raise ValueError("dwg and dwu are given together")
+    if accumulate and dwg is None:
+        raise ValueError("accumulate: dwg and dwu have to be given")
+    with _on(dh, stream, (dh, x, wg, wu, saved, dx, dwg, dwu, workspace)) as s:
+        if dx is None:
+            dx = torch.empty(M, D, dtype=dh.dtype, device=dh.device)
+        if dwg is None:
+            dwg, dwu = torch.empty(2, F, D, dtype=dh.dtype, device=dh.device).unbind(0)
+        sdx = _matrix("dx", dx, (M, D), dh)
+        sdw = _matrix("dwg", dwg, (F, D), dh)
+        if _matrix("dwu", dwu, (F, D), dh) != sdw:
+            raise ValueError("dwg and dwu: one row stride expected")
+        w, n, keep = _space(workspace, arplan.ar_glu_workspace(_DT[dh.dtype], M, D, F, True), dh)
+        arplan.ar_glu_backward(_DT[dh.dtype], M, D, F, dh, sh, x, sx, wg, wu, sw, sg, su, ss,
+                               accumulate, dx, sdx, dwg, dwu, sdw, w, n, s)
+    return dx, dwg, dwu
+
+
+# ----------------------------------------------------------- distillation
+
+def distill(logits, teacher, ids, temperature=1.0, weights=None, grad=None, workspace=None,
+            stream=None):
+    """The distillation loss of each row of ``logits`` (T, V) from the
+    teacher's top logits ``teacher`` (T, K) at ``ids`` (T, K), times
+    ``weights`` (T,): a float32 (T,) tensor.  With ``grad`` (T, V; ``logits``
+    itself for a gradient in place) returns the losses and ``grad``, holding
+    the gradient of their sum."""
+    sl = _matrix("logits", logits)
+    T, V = logits.shape
+    st = _matrix("teacher", teacher)
+    K = teacher.shape[1]
+    _ids("ids", ids, logits)
+    if teacher.device != logits.device or teacher.shape[0] != T or ids.shape != teacher.shape:
+        raise ValueError("teacher and ids: a (rows of logits, K) tensor each expected")
+    if K > 1 and ids.stride(1) != 1:
+        raise ValueError("ids: the elements of a row have to be adjacent")
+    si = ids.stride(0) if T > 1 else max(K, 1)
+    if weights is not None and (weights.shape != (T,) or weights.dtype != torch.float32
+                                or weights.device != logits.device or not weights.is_contiguous()):
+        raise ValueError("weights: a contiguous float32 vector, one a row, expected")
+    sg = _matrix("grad", grad, (T, V), logits) if grad is not None else 0
+    with _on(logits, stream, (logits, teacher, ids, weights, grad, workspace)) as s:
+        loss = torch.empty(T, dtype=torch.float32, device=logits.device)
+        w, n, keep = _space(workspace, arplan.ar_distill_workspace(T, V, K), logits)
+        arplan.ar_distill(_DT[logits.dtype], T, V, K, logits, sl, _DT[teacher.dtype], teacher, st,
+                          ids, si, temperature, weights, loss, grad, sg, w, n, s)
+    return (loss, grad) if grad is not None else loss

@@ -1,0 +1,431 @@
+"""The replica operators on the GPU against plain definitions in 64 bits."""
+
+import math
+
+import pytest
+import torch
+
+import ops_reference as ref
+from gpu_helpers import say
+
+arplan = pytest.importorskip(
+    "paper_2409_04202_amd.arplan",
+    reason="HIP library not built (run python -m paper_2409_04202_amd.build)")
+from paper_2409_04202_amd import ops  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DTYPES = ("f32", "bf16")
+
+
+def rnd(seed, *shape, dtype="f32", scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(ref.TORCH[dtype])
+
+
+def laid(x, layout):
+    """x on the GPU: its rows adjacent ("rows"), or inside a wider matrix of
+    other values, at an odd element ("wide")."""
+    if layout == "rows" or x.numel() == 0:
+        return x.cuda()
+    r, c = x.shape
+    m = torch.full((r, c + 5), float("nan"), dtype=x.dtype, device="cuda")
+    m[:, 3:3 + c] = x.cuda()
+    return m[:, 3:3 + c]
+
+
+def room(rows, cols, dtype, layout):
+    """An output like that, and a check that nothing around it was written."""
+    if layout == "rows":
+        return torch.full((rows, cols), 7.0, dtype=ref.TORCH[dtype], device="cuda"), lambda: None
+    m = torch.full((rows + 1, cols + 5), 7.0, dtype=ref.TORCH[dtype], device="cuda")
+
+    def check():
+        m[:rows, 3:3 + cols] = 7.0
+        assert bool((m == 7.0).all()), "elements around the output were written"
+    return m[:rows, 3:3 + cols], check
+
+
+def ids_of(seed, T, V, kind):
+    g = torch.Generator().manual_seed(seed)
+    if kind == "one":
+        return torch.full((T,), V // 2, dtype=torch.int64)
+    if kind == "none":
+        return torch.randint(0, 2, (T,), generator=g) * (V + 5) - 3
+    u = torch.rand(T, generator=g).double()
+    ids = (torch.exp(u * math.log(V)).long() - 1).clamp(0, V - 1)
+    if kind == "edges":
+        far = torch.tensor([-1, V, -2 ** 63, 2 ** 63 - 1, 2 ** 32, V - 1, 0, 2 ** 32 + 1])
+        pick = torch.randint(0, 16, (T,), generator=g)
+        ids = torch.where(pick < 8, far[pick.clamp(max=7)], ids)
+    return ids
+
+
+# ------------------------------------------------------------- embedding
+
+@pytest.mark.parametrize("layout", ("rows", "wide"))
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,V,D,kind", [
+    (1, 7, 64, "zipf"), (5, 1, 1, "edges"), (300, 130, 513, "edges"), (64, 1000, 8, "none"),
+    (33, 257, 2051, "zipf")])
+def test_embed_lookup(T, V, D, kind, dtype, layout):
+    table, ids = rnd(1, V, D, dtype=dtype), ids_of(2, T, V, kind)
+    out, check = room(T, D, dtype, layout)
+    ops.embed_lookup(laid(table, layout), ids.cuda(), scale=1.7, out=out)
+    assert torch.equal(out.cpu(), ref.embed_lookup(table, ids, 1.7))
+    check()
+
+
+@pytest.mark.parametrize("accumulate", (False, True))
+@pytest.mark.parametrize("layout", ("rows", "wide"))
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,V,D,kind", [
+    (1, 7, 64, "zipf"), (0, 5, 9, "zipf"), (31, 1, 3, "one"), (32, 3, 16, "one"),
+    (33, 3, 16, "one"), (700, 300, 257, "edges"), (1000, 9, 40, "zipf"), (64, 1000, 8, "none"),
+    (4097, 70001, 24, "zipf"), (9000, 2, 12, "zipf"), (20011, 400, 16, "zipf"),
+    (40000, 100000, 8, "edges")])
+def test_embed_grad(T, V, D, kind, dtype, layout, accumulate):
+    dout, ids = rnd(3, T, D, dtype=dtype), ids_of(4, T, V, kind)
+    out, check = room(V, D, dtype, layout)
+    old = out.cpu() if accumulate else None
+    ops.embed_grad(laid(dout, layout), ids.cuda(), out, scale=0.37, accumulate=accumulate)
+    got = out.cpu()
+    assert torch.equal(got, ref.embed_grad(dout, ids, V, 0.37, arplan.AR_EMBED_RUN, old))
+    if not accumulate:
+        want, e = ref.embed_grad64(dout, ids, V, 0.37)
+        ref.compare("gradient", got, want, e + ref.stored(want, dtype))
+    check()
+
+
+def test_embed_far_rows():
+    """Offsets beyond 32 bits, in elements and in bytes."""
+    V, D = 1100000, 4096
+    table = torch.empty(V, D, dtype=torch.bfloat16, device="cuda")
+    ids = torch.tensor([0, V - 1, 600000, V - 2, V - 1])
+    for i in set(ids.tolist()):
+        table[i] = rnd(i, 1, D, dtype="bf16")[0].cuda()
+    out = ops.embed_lookup(table, ids.cuda(), scale=2.0)
+    for t, i in enumerate(ids.tolist()):
+        assert torch.equal(out[t].cpu(), (rnd(i, 1, D, dtype="bf16")[0].float() * 2).bfloat16())
+    dout = rnd(9, 5, D, dtype="bf16")
+    ops.embed_grad(dout.cuda(), ids.cuda(), table, scale=1.0, accumulate=True)
+    want = (dout[1].float() + dout[4].float()) + rnd(V - 1, 1, D, dtype="bf16")[0].float()
+    assert torch.equal(table[V - 1].cpu(), want.bfloat16())
+    want = dout[2].float() + rnd(600000, 1, D, dtype="bf16")[0].float()
+    assert torch.equal(table[600000].cpu(), want.bfloat16())
+
+
+def test_embed_grad_is_the_lookups_derivative():
+    """Against central differences of <lookup, dout> in the table."""
+    T, V, D = 19, 6, 5
+    table, dout, ids = rnd(1, V, D).double(), rnd(2, T, D), ids_of(3, T, V, "edges")
+    out = torch.empty(V, D, device="cuda")
+    got = ops.embed_grad(dout.cuda(), ids.cuda(), out, scale=1.5).cpu().double()
+    ok = (ids >= 0) & (ids < V)
+
+    def value(tab):
+        return float((1.5 * tab[ids[ok]] * dout[ok].double()).sum())
+    for v in range(V):
+        for d in range(D):
+            e = torch.zeros(V, D).double()
+            e[v, d] = 1e-3
+            diff = (value(table + e) - value(table - e)) / 2e-3
+            assert abs(diff - float(got[v, d])) < 1e-5
+
+
+# ------------------------------------------------------ gated feed-forward
+
+GLU_SIZES = [
+    (1, 64, 128), (1, 1, 1), (2, 8, 16), (3, 100, 37), (16, 256, 512), (17, 264, 200),
+    (33, 129, 65), (64, 64, 64), (65, 1000, 130), (130, 72, 300), (256, 512, 256),
+    (300, 333, 515), (257, 520, 776)]
+
+
+@pytest.mark.parametrize("layout", ("rows", "wide"))
+@pytest.mark.parametrize("act", ("silu", "gelu"))
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,D,F", GLU_SIZES)
+def test_glu(M, D, F, dtype, act, layout):
+    x, wg = rnd(1, M, D, dtype=dtype), rnd(2, F, D, dtype=dtype, scale=D ** -0.5)
+    wu, dh = rnd(3, F, D, dtype=dtype, scale=D ** -0.5), rnd(4, M, F, dtype=dtype)
+    h, dx, dwg, dwu = ref.glu(x, wg, wu, act, dh, dtype)
+    gx, gg, gu, gd = (laid(t, layout) for t in (x, wg, wu, dh))
+    out, check = room(M, F, dtype, layout)
+    ops.glu_forward(gx, gg, gu, act=act, out=out)
+    ref.compare("h", out, *h)
+    alone = out.clone()
+    check()
+    got, saved = ops.glu_forward(gx, gg, gu, act=act, save=True)
+    ref.compare("h", got, *h)
+    if M > 16:
+        assert torch.equal(alone, got)
+    (ox, c0), (og, c1), (ou, c2) = (room(r, D, dtype, layout) for r in (M, F, F))
+    ops.glu_backward(gd, gx, gg, gu, saved, dx=ox, dwg=og, dwu=ou)
+    for name, o, w in (("dx", ox, dx), ("dwg", og, dwg), ("dwu", ou, dwu)):
+        ref.compare(name, o, *w)
+    first = [t.clone() for t in (ox, og, ou)]
+    # once more, adding: the sum's own rounding on top
+    ops.glu_backward(gd, gx, gg, gu, saved, dx=ox, dwg=og, dwu=ou, accumulate=True)
+    assert torch.equal(ox, first[0])
+    for name, o, w, f in (("dwg", og, dwg, first[1]), ("dwu", ou, dwu, first[2])):
+        v = w[0] + f.double().cpu()
+        ref.compare(name + " added", o, v, w[1] + ref.stored(v, dtype))
+    for c in (c0, c1, c2):
+        c()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_glu_empty(dtype):
+    dt = ref.TORCH[dtype]
+    e = lambda *s: torch.zeros(*s, dtype=dt, device="cuda")  # noqa: E731
+    assert ops.glu_forward(e(0, 8), e(4, 8), e(4, 8)).shape == (0, 4)
+    # an empty sum: g = u = 0
+    h, saved = ops.glu_forward(e(3, 0), e(4, 0), e(4, 0), save=True)
+    assert bool((h == 0).all())
+    dwg, dwu = e(4, 8) + 5, e(4, 8) + 5
+    ops.glu_backward(e(0, 4), e(0, 8), e(4, 8), e(4, 8), e(2, 0, 4), dwg=dwg, dwu=dwu,
+                     accumulate=True)
+    assert bool((dwg == 5).all()) and bool((dwu == 5).all())
+    ops.glu_backward(e(0, 4), e(0, 8), e(4, 8), e(4, 8), e(2, 0, 4), dwg=dwg, dwu=dwu)
+    assert bool((dwg == 0).all()) and bool((dwu == 0).all())
+    dx, _, _ = ops.glu_backward(e(3, 0), e(3, 8), e(0, 8), e(0, 8), e(2, 3, 0))
+    assert bool((dx == 0).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("act", ("silu", "gelu"))
+@pytest.mark.parametrize("M", (1, 40))
+def test_glu_extremes(M, act, dtype):
+    """Gates at the ends of the range: the activation's limits, no NaN; and a
+    NaN or an infinity stays in its own row."""
+    D, F = 8, 48
+    x = torch.zeros(M, D)
+    x[:, 0] = 1
+    wg, wu = torch.zeros(F, D), torch.zeros(F, D)
+    wg[:, 0] = torch.tensor([0.0, 1e30, -1e30, 200.0, -200.0, 50.0, -50.0, -88.0] * 6)
+    wu[:, 0] = 1
+    x, wg, wu = (t.to(ref.TORCH[dtype]) for t in (x, wg, wu))
+    h, saved = ops.glu_forward(x.cuda(), wg.cuda(), wu.cuda(), act=act, save=True)
+    g = wg[:, 0].double()
+    a, da = ref.activate(act, g)
+    a, da = torch.where(a.isnan(), 0.0, a), torch.where(da.isnan(), (g > 0).double(), da)
+    for name, got, want in (("h", h, a), ("a", saved[1], a), ("a'", saved[0], da)):
+        want = want[None, :].expand(M, F)
+        ref.compare(name, got, want, want.abs() * 2.0 ** -8 + 1e-30)
+    if M > 1:
+        y = x.clone()
+        y[3, 5], y[7, 2] = float("nan"), float("inf")
+        h2 = ops.glu_forward(y.cuda(), wg.cuda(), wu.cuda(), act=act)
+        keep = [r for r in range(M) if r not in (3, 7)]
+        assert torch.equal(h2[keep], h[keep]) and bool(h2[3].isnan().all())
+
+
+def test_glu_gradients_are_derivatives():
+    """Against central differences of <h, dh> in 64 bits."""
+    M, D, F = 5, 4, 3
+    for act in ("silu", "gelu"):
+        args = [rnd(i, *s) for i, s in enumerate(((M, D), (F, D), (F, D)))]
+        dh = rnd(9, M, F)
+        _, saved = ops.glu_forward(*(a.cuda() for a in args), act=act, save=True)
+        got = ops.glu_backward(dh.cuda(), *(a.cuda() for a in args), saved)
+
+        def value(x, wg, wu):
+            return float((ref.activate(act, x @ wg.t())[0] * (x @ wu.t()) * dh.double()).sum())
+        for i, a in enumerate(args):
+            for j in range(a.numel()):
+                e = torch.zeros(a.numel()).double()
+                e[j] = 1e-4
+                lo, hi = [b.double() for b in args], [b.double() for b in args]
+                lo[i], hi[i] = lo[i] - e.view(a.shape), hi[i] + e.view(a.shape)
+                diff = (value(*hi) - value(*lo)) / 2e-4
+                assert abs(diff - float(got[i].flatten()[j])) < 2e-5
+
+
+def test_glu_side_by_side():
+    """Both weight gradients as columns of one wider matrix."""
+    M, D, F = 40, 24, 56
+    x, wg, wu, dh = (rnd(i, *s).cuda() for i, s in enumerate(((M, D), (F, D), (F, D), (M, F))))
+    _, saved = ops.glu_forward(x, wg, wu, save=True)
+    _, a, b = ops.glu_backward(dh, x, wg, wu, saved)
+    both = torch.empty(F, 2 * D, device="cuda")
+    ops.glu_backward(dh, x, wg, wu, saved, dwg=both[:, :D], dwu=both[:, D:])
+    assert torch.equal(both, torch.cat((a, b), 1))
+
+
+# ----------------------------------------------------------- distillation
+
+def teacher_of(seed, T, V, K, repeat=False):
+    g = torch.Generator().manual_seed(seed)
+    if repeat:
+        ids = torch.randint(0, max(1, V // 2), (T, K), generator=g)
+    else:
+        ids = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(T)]) if T else \
+            torch.zeros(0, K, dtype=torch.int64)
+    return ids, torch.randn(T, K, generator=g) * 3
+
+
+@pytest.mark.parametrize("layout", ("rows", "wide"))
+@pytest.mark.parametrize("dtype,tdtype", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"),
+                                          ("f32", "bf16")])
+@pytest.mark.parametrize("T,V,K,tau", [
+    (1, 1, 1, 1.0), (3, 7, 7, 2.0), (5, 1000, 20, 1.0), (4, 4099, 64, 4.0), (2, 65536, 10, 0.5),
+    (9, 33001, 1, 1.0), (3, 140001, 33, 2.0), (300, 513, 8, 1.0)])
+def test_distill(T, V, K, tau, dtype, tdtype, layout):
+    z = rnd(1, T, V, dtype=dtype, scale=4.0)
+    ids, tea = teacher_of(2, T, V, K)
+    tea = tea.to(ref.TORCH[tdtype])
+    wt = torch.rand(T, generator=torch.Generator().manual_seed(3))
+    (loss, el), (grad, eg) = ref.distill(z, tea, ids, tau, wt, dtype)
+    gz, gt, gi, gw = laid(z, layout), laid(tea, layout), ids.cuda(), wt.cuda()
+    ref.compare("loss", ops.distill(gz, gt, gi, temperature=tau, weights=gw), loss, el)
+    out, check = room(T, V, dtype, layout)
+    got, g = ops.distill(gz, gt, gi, temperature=tau, weights=gw, grad=out)
+    ref.compare("loss", got, loss, el)
+    ref.compare("gradient", g, grad, eg)
+    there = g.clone()
+    check()
+    # in place
+    ops.distill(gz, gt, gi, temperature=tau, weights=gw, grad=gz)
+    assert torch.equal(gz, there)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_distill_masks(dtype):
+    inf, nan, low = float("inf"), float("nan"), torch.finfo(ref.TORCH[dtype]).min
+    T, V, K = 16, 2051, 6
+    z = rnd(1, T, V, dtype=dtype, scale=3.0)
+    ids, tea = teacher_of(2, T, V, K)
+    w = torch.ones(T)
+    w[0] = 0
+    z[0], tea[0, 1] = nan, nan                      # weight 0: whatever it holds
+    ids[1] = torch.tensor([-1, V, 2 ** 40, -2 ** 63, V + 1, -7])   # no entry
+    z[1, 5] = nan
+    tea[2] = -inf                                   # no entry either
+    z[3] = -inf                                     # no logit
+    z[4] = low                                      # the mask's value throughout: uniform
+    z[5], z[5, :3] = low, z[6, :3]                  # three logits left
+    ids[5] = torch.tensor([0, 1, 2, -1, -1, -1])
+    z[6, ids[6, 0]] = -inf                          # the student excludes an entry
+    z[7, ids[7, 0]], tea[7, 0] = -inf, -inf         # that the teacher excludes too
+    tea[8] = low                                    # entries at the lowest value: uniform
+    tea[9, 1:] = low
+    z[10, 7] = nan
+    z[11, 7] = inf
+    tea[12, 2] = nan
+    ids[13, 1:] = ids[13, 0]                        # one id in every entry
+    ids[14, 3] = ids[14, 1]
+    z[15, 1000:] = -inf
+    ids[15] = torch.tensor([5, 2, 999, -1, 0, 1])
+    (loss, el), (grad, eg) = ref.distill(z, tea.to(ref.TORCH[dtype]), ids, 1.3, w, dtype)
+    assert bool(loss[6] == inf) and bool(grad[6].isfinite().all())
+    assert bool(loss[10].isnan()) and bool(loss[11].isnan()) and bool(loss[12].isnan())
+    args = z.cuda(), tea.to(ref.TORCH[dtype]).cuda(), ids.cuda()
+    got, g = ops.distill(*args, temperature=1.3, weights=w.cuda(),
+                         grad=torch.empty(T, V, dtype=z.dtype, device="cuda"))
+    only = ops.distill(*args, temperature=1.3, weights=w.cuda())
+    assert torch.equal(only.nan_to_num(nan=-5.0), got.nan_to_num(nan=-5.0))
+    ref.compare("loss", got, loss, el)
+    for t in range(T):
+        if t != 12:     # (a NaN in the teacher: below)
+            ref.compare("gradient of row %d" % t, g[t], grad[t], eg[t])
+    at = ids[12][(ids[12] >= 0) & (ids[12] < V)]
+    assert bool(g[12, at.cuda()].isnan().all())
+    rest = torch.ones(V, dtype=torch.bool)
+    rest[at] = False
+    ref.compare("gradient beside a NaN entry", g[12].cpu()[rest], grad[12][rest],
+                ref.stored(grad[12][rest], dtype) + 1e-5 * grad[12][rest])
+
+
+@pytest.mark.parametrize("K", (0, 1000, 4096))
+def test_distill_numbers_of_entries(K):
+    T, V = 3, 5003
+    z = rnd(1, T, V)
+    ids, tea = teacher_of(2, T, V, K, repeat=True)
+    (loss, el), (grad, eg) = ref.distill(z, tea, ids, 1.0, None, "f32")
+    got, g = ops.distill(z.cuda(), tea.cuda(), ids.cuda(), grad=torch.empty(T, V, device="cuda"))
+    ref.compare("loss", got, loss, el)
+    ref.compare("gradient", g, grad, eg)
+
+
+def test_distill_gradient_is_the_losses_derivative():
+    T, V, K = 3, 6, 4
+    z, (ids, tea) = rnd(1, T, V), teacher_of(2, T, V, K, repeat=True)
+    w = torch.tensor([1.0, 0.25, 2.0])
+    _, g = ops.distill(z.cuda(), tea.cuda(), ids.cuda(), temperature=1.7, weights=w.cuda(),
+                       grad=torch.empty(T, V, device="cuda"))
+    for t in range(T):
+        for j in range(V):
+            e = torch.zeros(T, V).double()
+            e[t, j] = 1e-4
+            up = ref.distill(z.double() + e, tea, ids, 1.7, w, "f32")[0][0]
+            down = ref.distill(z.double() - e, tea, ids, 1.7, w, "f32")[0][0]
+            assert abs(float((up - down).sum()) / 2e-4 - float(g[t, j])) < 1e-5
+
+
+def test_distill_far_rows():
+    """Row offsets beyond 32 bits."""
+    T, V, stride = 3, 1003, (1 << 31) + 11
+    m = torch.empty(2 * stride + V, dtype=torch.bfloat16, device="cuda")
+    far = m.as_strided((T, V), (stride, 1))
+    z = rnd(1, T, V, dtype="bf16")
+    far.copy_(z.cuda())
+    ids, tea = teacher_of(2, T, V, 5)
+    (loss, el), (grad, eg) = ref.distill(z, tea, ids, 1.0, None, "bf16")
+    got, g = ops.distill(far, tea.cuda(), ids.cuda(), grad=far)
+    ref.compare("loss", got, loss, el)
+    ref.compare("gradient", g, grad, eg)
+
+
+# ------------------------------------------------------ streams and graphs
+
+def _pass(dtype="bf16"):
+    """One pass through every operator on fixed buffers, as a function."""
+    dt = ref.TORCH[dtype]
+    T, V, D, F, K = 300, 1000, 128, 192, 8
+    table, ids = rnd(1, V, D, dtype=dtype).cuda(), ids_of(2, T, V, "edges").cuda()
+    wg, wu = (rnd(i, F, D, dtype=dtype, scale=D ** -0.5).cuda() for i in (3, 4))
+    dh = rnd(5, T, F, dtype=dtype).cuda()
+    tid, tea = teacher_of(6, T, F, K)
+    tid, tea = tid.cuda(), tea.cuda()
+    dtable = torch.empty(V, D, dtype=dt, device="cuda")
+
+    def go(stream=None):
+        x = ops.embed_lookup(table, ids, scale=3.0, stream=stream)
+        h, saved = ops.glu_forward(x, wg, wu, save=True, stream=stream)
+        loss, g = ops.distill(h, tea, tid, temperature=2.0, grad=torch.empty_like(h), stream=stream)
+        dx, dwg, dwu = ops.glu_backward(dh, x, wg, wu, saved, stream=stream)
+        ops.embed_grad(dx, ids, dtable, scale=3.0, stream=stream)
+        return x, h, loss, g, dx, dwg, dwu, dtable
+    return go, table
+
+
+def test_ops_repeat_bit_for_bit_and_on_another_stream():
+    go, _ = _pass()
+    first = [t.clone() for t in go()]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        out = go(side)
+        side.synchronize()
+        for a, b in zip(first, out):
+            assert torch.equal(a, b)
+
+
+def test_ops_in_a_graph():
+    go, table = _pass()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        go()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = go()
+    for i in range(3):
+        table.copy_(rnd(20 + i, *table.shape, dtype="bf16"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = go()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        say("replay", i)
