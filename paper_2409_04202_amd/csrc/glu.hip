@@ -1,7 +1,8 @@
 // The gated feed-forward block's products.
 #include <algorithm>
+#include <type_traits>
 
-#include "replica.hpp"
+#include "product.hpp"
 
 namespace arp {
 namespace {
@@ -21,66 +22,41 @@ __device__ __forceinline__ void activate(int act, float g, float* value, float* 
     }
 }
 
-// One product, C (rows x cols) = sum over k of A(row, k) B(col, k) over one
-// or two segments of k; any element strides.
-template <class T>
-struct Operand {
-    const T* p;
-    int64_t row, k;  // strides
-    __device__ __forceinline__ float at(int64_t r, int64_t i) const {
-        return Num<T>::up(p[r * row + i * k]);
-    }
-};
-
-constexpr int kTile = 64, kDepth = 16;
-
-// A 64 x 64 tile of A B^T by 256 threads, 4 x 4 each.
-template <class T>
-__device__ __forceinline__ void tile_product(const Operand<T> A, const Operand<T> B, int64_t r0,
-                                             int64_t rows, int64_t c0, int64_t cols, int64_t K,
-                                             float (*sa)[kTile + 4], float (*sb)[kTile + 4],
-                                             float acc[4][4]) {
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int64_t k0 = 0; k0 < K; k0 += kDepth) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < kTile * kDepth; e += 256) {
-            const int r = e / kDepth, k = e % kDepth;
-            sa[k][r] = r0 + r < rows && k0 + k < K ? A.at(r0 + r, k0 + k) : 0.0f;
-            sb[k][r] = c0 + r < cols && k0 + k < K ? B.at(c0 + r, k0 + k) : 0.0f;
-        }
-        __syncthreads();
-        for (int k = 0; k < kDepth; ++k)
-            for (int i = 0; i < 4; ++i)
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] = fmaf(sa[k][ty * 4 + i], sb[k][tx * 4 + j], acc[i][j]);
-    }
-}
-
 struct ForwardArgs {
-    int64_t M, D, F, x_stride, w_stride, h_stride, saved_stride;
+    int64_t h_stride, saved_stride;
     int act;
 };
 
-template <class T>
-__global__ __launch_bounds__(256) void forward_kernel(ForwardArgs a, const T* x, const T* wg,
-                                                      const T* wu, T* h, T* sg, T* su) {
-    __shared__ float sa[kDepth][kTile + 4], sb[kDepth][kTile + 4];
-    const int64_t r0 = int64_t(blockIdx.y) * kTile, c0 = int64_t(blockIdx.x) * kTile;
-    float g[4][4] = {}, u[4][4] = {};
-    const Operand<T> X{x, a.x_stride, 1};
-    tile_product<T>(X, {wg, a.w_stride, 1}, r0, a.M, c0, a.F, a.D, sa, sb, g);
-    tile_product<T>(X, {wu, a.w_stride, 1}, r0, a.M, c0, a.F, a.D, sa, sb, u);
-    for (int i = 0; i < 4; ++i) {
-        for (int j = 0; j < 4; ++j) {
-            const int64_t r = r0 + (threadIdx.x >> 4) * 4 + i, c = c0 + (threadIdx.x & 15) * 4 + j;
-            if (r >= a.M || c >= a.F) continue;
-            float value, slope;
-            activate(a.act, g[i][j], &value, &slope);
-            h[r * a.h_stride + c] = Num<T>::down(value * u[i][j]);
-            if (sg) {
-                sg[r * a.saved_stride + c] = Num<T>::down(slope * u[i][j]);
-                su[r * a.saved_stride + c] = Num<T>::down(value);
-            }
+template <class T, int BR, int BC, int WR, int WC, bool DIRECT>
+__global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, ForwardArgs a,
+                                                               Side<T> x, Side<T> w, T* h, T* sg,
+                                                               T* su) {
+    using P = Tile<T, BR, BC, WR, WC, true, true, true, DIRECT>;
+    using S = Store<1>;
+    static_assert(P::LDS >= WR * WC * S::BYTES, "");
+    __shared__ __attribute__((aligned(16))) char lds[P::LDS];
+    int64_t rt, ct;
+    if (!tile_of(p, blockIdx.x, &rt, &ct)) return;
+    f32x16 acc[P::SR][2] = {};
+    P::run(p, x, w, rt * BR, ct * (BC / 2), (AR_LDS char*)lds, acc);
+    const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
+    AR_LDS float* const part = (AR_LDS float*)((AR_LDS char*)lds + wave * S::BYTES);
+#pragma unroll
+    for (int i = 0; i < P::SR; ++i) {
+        const int64_t r0 = rt * BR + (wr * P::SR + i) * 32, c0 = ct * (BC / 2) + wc * 32;
+        float value[16], slope[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) activate(a.act, acc[i][0][e], &value[e], &slope[e]);
+        auto pass = [&](T* out, int64_t stride, auto f) {
+            S::fill(part, f);
+            wave_sync();
+            S::store(part, out, stride, r0, p.rows, c0, p.cols, false);
+            wave_sync();
+        };
+        pass(h, a.h_stride, [&](int, int e) { return value[e] * acc[i][1][e]; });
+        if (sg) {
+            pass(sg, a.saved_stride, [&](int, int e) { return slope[e] * acc[i][1][e]; });
+            pass(su, a.saved_stride, [&](int, int e) { return value[e]; });
         }
     }
 }
@@ -100,31 +76,78 @@ __global__ __launch_bounds__(256) void factors_kernel(int64_t M, int64_t F, cons
     }
 }
 
-// C = A1 B1^T + A2 B2^T (K2 = 0: the first alone), or C += with accumulate.
-template <class T>
-__global__ __launch_bounds__(256) void product_kernel(Operand<T> A1, Operand<T> B1, int64_t K1,
-                                                      Operand<T> A2, Operand<T> B2, int64_t K2,
-                                                      int64_t rows, int64_t cols, int accumulate,
-                                                      T* out, int64_t stride) {
-    __shared__ float sa[kDepth][kTile + 4], sb[kDepth][kTile + 4];
-    const int64_t r0 = int64_t(blockIdx.y) * kTile, c0 = int64_t(blockIdx.x) * kTile;
-    float acc[4][4] = {};
-    tile_product<T>(A1, B1, r0, rows, c0, cols, K1, sa, sb, acc);
-    tile_product<T>(A2, B2, r0, rows, c0, cols, K2, sa, sb, acc);
-    for (int i = 0; i < 4; ++i) {
-        for (int j = 0; j < 4; ++j) {
-            const int64_t r = r0 + (threadIdx.x >> 4) * 4 + i, c = c0 + (threadIdx.x & 15) * 4 + j;
-            if (r >= rows || c >= cols) continue;
-            T* const at = out + r * stride + c;
-            *at = Num<T>::down(accumulate ? Num<T>::up(*at) + acc[i][j] : acc[i][j]);
-        }
+// C = R L^T, or C += with accumulate.
+template <class T, int BR, int BC, int WR, int WC, bool RKC, bool DIRECT>
+__global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductShape p, Side<T> r, Side<T> l,
+                                                               int accumulate, T* out,
+                                                               int64_t stride) {
+    using P = Tile<T, BR, BC, WR, WC, RKC, false, false, DIRECT>;
+    using S = Store<P::SC>;
+    static_assert(P::LDS >= WR * WC * S::BYTES, "");
+    __shared__ __attribute__((aligned(16))) char lds[P::LDS];
+    int64_t rt, ct;
+    if (!tile_of(p, blockIdx.x, &rt, &ct)) return;
+    f32x16 acc[P::SR][P::SC] = {};
+    P::run(p, r, l, rt * BR, ct * BC, (AR_LDS char*)lds, acc);
+    const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
+    AR_LDS float* const part = (AR_LDS float*)((AR_LDS char*)lds + wave * S::BYTES);
+#pragma unroll
+    for (int i = 0; i < P::SR; ++i) {
+        S::fill(part, [&](int j, int e) { return acc[i][j][e]; });
+        wave_sync();
+        S::store(part, out, stride, rt * BR + (wr * P::SR + i) * 32, p.rows,
+                 ct * BC + wc * P::SC * 32, p.cols, accumulate);
+        wave_sync();
     }
+}
+
+// Whether a tile's copies may go straight to LDS: 16-byte chunks at 16-byte
+// places, within 32-bit offsets of the tile's first row.
+template <class T>
+bool direct(const void* a, const void* b, int64_t stride, int64_t extent, bool kc) {
+    constexpr int VEC = Num<T>::VEC;
+    if ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % kChunk) return false;
+    if (stride % VEC || stride * int64_t(sizeof(T)) > (int64_t(1) << 22)) return false;
+    return kc || extent % VEC == 0;
 }
 
 int64_t factor_stride(int64_t F) { return round_up(F, 8); }
 
-dim3 tiles(int64_t rows, int64_t cols) {
-    return dim3(unsigned(ceil_div(cols, kTile)), unsigned(ceil_div(rows, kTile)));
+ProductShape shape(int64_t rows, int64_t cols, int64_t K, int segments, int br, int bc) {
+    return ProductShape{rows, cols, K, segments, ceil_div(rows, br), ceil_div(cols, bc)};
+}
+
+dim3 grid_of(const ProductShape& p) {
+    return dim3(unsigned(tile_blocks(p.row_tiles * p.col_tiles)));
+}
+
+template <class T, bool RKC, int BR, int BC, int WR, int WC>
+void launch_product(const ProductShape& p, const Side<T>& r, const Side<T>& l, int accumulate,
+                    T* out, int64_t stride, hipStream_t st) {
+    const bool fast = direct<T>(r.p[0], r.p[1], r.stride, p.rows, RKC) &&
+                      direct<T>(l.p[0], l.p[1], l.stride, p.cols, false);
+    const dim3 block(64 * WR * WC);
+    if (fast)
+        hipLaunchKernelGGL((product_kernel<T, BR, BC, WR, WC, RKC, true>), grid_of(p), block, 0, st,
+                           p, r, l, accumulate, out, stride);
+    else
+        hipLaunchKernelGGL((product_kernel<T, BR, BC, WR, WC, RKC, false>), grid_of(p), block, 0,
+                           st, p, r, l, accumulate, out, stride);
+}
+
+template <class T, int BR, int BC, int WR, int WC>
+void launch_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Side<T>& x,
+                    const Side<T>& w, T* h, T* sg, T* su, hipStream_t st) {
+    const ProductShape p = shape(M, F, D, 1, BR, BC / 2);
+    const bool fast = direct<T>(x.p[0], x.p[1], x.stride, M, true) &&
+                      direct<T>(w.p[0], w.p[1], w.stride, F, true);
+    const dim3 block(64 * WR * WC);
+    if (fast)
+        hipLaunchKernelGGL((forward_kernel<T, BR, BC, WR, WC, true>), grid_of(p), block, 0, st, p, a,
+                           x, w, h, sg, su);
+    else
+        hipLaunchKernelGGL((forward_kernel<T, BR, BC, WR, WC, false>), grid_of(p), block, 0, st, p,
+                           a, x, w, h, sg, su);
 }
 
 }  // namespace
@@ -132,7 +155,10 @@ dim3 tiles(int64_t rows, int64_t cols) {
 
 using namespace arp;
 
-// Rows and columns of a product: a launch's grid holds this many tiles.
+// Whether a product of so many 256 x 256 tiles takes those, and not four times
+// as many of 128 x 128: where they fill the card's 256 CUs.
+static bool large_tiles(int64_t tiles) { return tiles >= 192; }
+
 static ar_status check_glu_sizes(int64_t M, int64_t D, int64_t F) {
     AR_TRY(check_extent("M", M));
     AR_TRY(check_extent("D", D));
@@ -182,14 +208,18 @@ AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_
     for (const MatArg& o : {su, mw}) AR_TRY(check_apart(o, sg));
     AR_TRY(check_apart(mw, su));
     if (M == 0 || F == 0) return AR_OK;
-    const ForwardArgs a{M, D, F, x_stride, w_stride, h_stride, saved_stride, act};
+    const ForwardArgs a{h_stride, saved_stride, act};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     auto go = [&](auto zero) {
         using T = decltype(zero);
-        hipLaunchKernelGGL((forward_kernel<T>), tiles(M, F), dim3(256), 0, st, a,
-                           static_cast<const T*>(x), static_cast<const T*>(wg),
-                           static_cast<const T*>(wu), static_cast<T*>(h),
-                           static_cast<T*>(saved_gate), static_cast<T*>(saved_up));
+        const Side<T> sx{{static_cast<const T*>(x), static_cast<const T*>(x)}, x_stride},
+            sw{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride};
+        T *const oh = static_cast<T*>(h), *const og = static_cast<T*>(saved_gate),
+                 *const ou = static_cast<T*>(saved_up);
+        if (large_tiles(ceil_div(M, 256) * ceil_div(F, 128)))
+            launch_forward<T, 256, 256, 2, 4>(a, M, D, F, sx, sw, oh, og, ou, st);
+        else
+            launch_forward<T, 128, 128, 2, 2>(a, M, D, F, sx, sw, oh, og, ou, st);
         return launch_status("gated feed-forward");
     };
     return dtype == AR_F32 ? go(float(0)) : go(uint16_t(0));
@@ -236,20 +266,27 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
                                dim3(256), 0, st, M, F, static_cast<const T*>(dh), dh_stride,
                                static_cast<const T*>(saved_gate), static_cast<const T*>(saved_up),
                                saved_stride, dg, du, fs);
-        const T* const X = static_cast<const T*>(x);
+        auto product = [&](auto rkc, const Side<T>& r, const Side<T>& l, int64_t rows, int64_t K,
+                           int segments, int acc, void* out, int64_t stride) {
+            constexpr bool RKC = decltype(rkc)::value;
+            T* const o = static_cast<T*>(out);
+            if (large_tiles(ceil_div(rows, 256) * ceil_div(D, 256)))
+                launch_product<T, RKC, 256, 256, 2, 4>(shape(rows, D, K, segments, 256, 256), r, l,
+                                                       acc, o, stride, st);
+            else
+                launch_product<T, RKC, 128, 128, 2, 2>(shape(rows, D, K, segments, 128, 128), r, l,
+                                                       acc, o, stride, st);
+        };
         if (dx && M > 0)
-            hipLaunchKernelGGL((product_kernel<T>), tiles(M, D), dim3(256), 0, st,
-                               (Operand<T>{dg, fs, 1}),
-                               (Operand<T>{static_cast<const T*>(wg), 1, w_stride}), F,
-                               (Operand<T>{du, fs, 1}),
-                               (Operand<T>{static_cast<const T*>(wu), 1, w_stride}), F, M, D, 0,
-                               static_cast<T*>(dx), dx_stride);
+            product(std::true_type{}, Side<T>{{dg, du}, fs},
+                    Side<T>{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride}, M, F,
+                    2, 0, dx, dx_stride);
         if (dwg && F > 0) {
-            for (int i = 0; i < 2; ++i)
-                hipLaunchKernelGGL((product_kernel<T>), tiles(F, D), dim3(256), 0, st,
-                                   (Operand<T>{i ? du : dg, 1, fs}), (Operand<T>{X, 1, x_stride}), M,
-                                   (Operand<T>{}), (Operand<T>{}), int64_t(0), F, D, accumulate,
-                                   static_cast<T*>(i ? dwu : dwg), dw_stride);
+            const Side<T> sx{{static_cast<const T*>(x), static_cast<const T*>(x)}, x_stride};
+            product(std::false_type{}, Side<T>{{dg, dg}, fs}, sx, F, M, 1, accumulate, dwg,
+                    dw_stride);
+            product(std::false_type{}, Side<T>{{du, du}, fs}, sx, F, M, 1, accumulate, dwu,
+                    dw_stride);
         }
         return launch_status("gated feed-forward gradients");
     };

@@ -1,0 +1,402 @@
+// Tiled matrix products on the matrix cores, for the gated feed-forward block:
+// C (rows x cols) = sum over k of R(row, k) L(col, k), R the row operand and L
+// the column operand, each stored with k along its rows ("K-contiguous") or
+// across them ("K-major"), both in fp32 or bf16 with fp32 accumulation.
+//
+// A block computes a tile of C; its wavefronts split it into 32 x 32 squares
+// of accumulators.  Per step of 128 bytes of k (64 bf16 or 32 fp32) the
+// operands' panels are copied into LDS, two buffers in turn: the copies of
+// the next step run while this one's products do.  The column operand is the
+// matrix instruction's first, so a lane holds, of one row of C, runs of four
+// adjacent columns.
+//
+// LDS layouts.  K-contiguous: a row of the panel is 8 chunks of 16 bytes,
+// chunk c of row r at place c ^ swz(r), so that any 8 and any 16 successive
+// rows' chunks of one k lie in different banks.  K-major bf16: a row is one k,
+// read with the transposing LDS load (16 lanes read 4 k of 16 columns and each
+// receives 4 k of its column); chunk c of row k at c ^ 2 swzk(k), which puts the
+// 32-byte pieces of 4 successive k, and of two neighbouring squares, into
+// different banks.  K-major fp32: a row is one k, unswizzled; a lane reads
+// single elements, 32 lanes 128 adjacent bytes.
+//
+// Edges.  Rows beyond an operand's end repeat its last row (their results are
+// not stored); a step's k beyond the end reads as zero in both operands, so
+// what lies there, NaN included, has no effect.
+#pragma once
+
+#include "replica.hpp"
+
+namespace arp {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kChunk = 16;       // bytes a copy moves a lane
+constexpr int kStepBytes = 128;  // bytes of k a step
+
+template <class T> struct StepOf { static constexpr int K = kStepBytes / int(sizeof(T)); };
+
+// An operand: up to two matrices one after the other in k (the second may be
+// absent), or, in a panel of the gated product, side by side (half the panel's
+// rows from each).
+template <class T>
+struct Side {
+    const T* p[2];
+    int64_t stride;
+};
+
+struct ProductShape {
+    int64_t rows, cols;  // of C (cols: of each half in the gated product)
+    int64_t K;           // of one segment
+    int segments;        // 1 or 2
+    int64_t row_tiles, col_tiles;
+};
+
+__device__ __forceinline__ int swz(int r) { return ((r >> 1) ^ ((r & 1) << 2)) & 7; }
+__device__ __forceinline__ int swzk(int k) { return ((k & 3) ^ ((k & 3) << 1)) & 7; }
+
+__device__ __forceinline__ uint32_t scalar(uint32_t v) {
+    return uint32_t(__builtin_amdgcn_readfirstlane(int(v)));
+}
+
+// One operand's panel: N rows (K-contiguous) or columns (K-major) of the step.
+template <class T, int N, int THREADS, bool KC, bool GATED>
+struct Panel {
+    static constexpr int E = int(sizeof(T));
+    static constexpr int VEC = kChunk / E;
+    static constexpr int BYTES = N * kStepBytes;
+    static constexpr int LOADS = BYTES / (kChunk * THREADS);  // chunks a thread
+    static constexpr int ROWCHUNKS = KC ? kStepBytes / kChunk : N * E / kChunk;
+    static constexpr int ROWSTEP = THREADS / ROWCHUNKS;  // panel rows from load to load
+    static_assert(THREADS % ROWCHUNKS == 0 && BYTES % (kChunk * THREADS) == 0, "");
+    static_assert(!GATED || (KC && (N / 2) % ROWSTEP == 0), "");
+
+    const Side<T> s;
+    int64_t first;      // the panel's first row (column) in the operand
+    int64_t end;        // the operand's rows (columns)
+    uint32_t off[LOADS];
+    int chunk;          // K-contiguous: the thread's chunk, in elements of k
+
+    // The thread's place in load i: panel row and chunk (logical).
+    static __device__ __forceinline__ int row_of(int i) {
+        return i * ROWSTEP + int(threadIdx.x) / ROWCHUNKS;
+    }
+    static __device__ __forceinline__ int chunk_of(int i) {
+        const int phys = int(threadIdx.x) % ROWCHUNKS, r = row_of(i);
+        return KC ? phys ^ swz(r) : (E == 2 ? phys ^ (2 * swzk(r)) : phys);
+    }
+    // The matrix and its row behind panel row r.
+    __device__ __forceinline__ int64_t source(int r, int seg, const T** p) const {
+        if constexpr (GATED) {
+            *p = r >= N / 2 ? s.p[1] : s.p[0];
+            return first + (r & (N / 2 - 1));
+        } else {
+            *p = seg ? s.p[1] : s.p[0];
+            return first + r;
+        }
+    }
+
+    __device__ __forceinline__ Panel(const Side<T>& side, int64_t f, int64_t e)
+        : s(side), first(f), end(e) {
+        if constexpr (KC) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int r = GATED ? row_of(i) & (N / 2 - 1) : row_of(i);
+                const int64_t last = end - 1 - first;
+                off[i] = uint32_t((r < last ? r : last) * s.stride * E) + chunk_of(i) * kChunk;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                // columns beyond the end: the row's last whole chunk
+                const int64_t c = int64_t(chunk_of(i)) * VEC, last = end - VEC - first;
+                off[i] = uint32_t(row_of(i) * s.stride * E) + uint32_t((c < last ? c : last) * E);
+            }
+        }
+    }
+
+    // Start the copies of the step at k0 (whole) straight into LDS, `lds` the
+    // address there: lane l's 16 bytes go to the wavefront's 1 KiB at 16 l.
+    // They are written as assembly because of the waits: the compiler would
+    // hold every LDS read back until all copies have landed, those of the
+    // other buffer among them.  Whoever reads what they bring waits for the
+    // vector memory counter and passes a barrier first (see landed()).  (m0 is
+    // never allocated: nothing else here uses it.)
+    __device__ __forceinline__ void copy(int seg, int64_t k0, uint32_t lds) const {
+        const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const T* p;
+            if constexpr (GATED) p = s.p[i * ROWSTEP >= N / 2];
+            else p = seg ? s.p[1] : s.p[0];
+            p += KC ? first * s.stride + k0 : k0 * s.stride + first;
+            const uint64_t at = reinterpret_cast<uint64_t>(p);
+            // a raw buffer from there on, without a bound below 4 GiB
+            const u32x4 rsrc = {scalar(uint32_t(at)), scalar(uint32_t(at >> 32) & 0xFFFFu),
+                                0xFFFFFFFFu, 0x00020000u};
+            const uint32_t to = scalar(lds + uint32_t(i * THREADS + wave * 64) * kChunk);
+            asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                         :: "s"(to), "v"(off[i]), "s"(rsrc) : "memory");
+        }
+    }
+
+    // The same through registers, for any alignment and with elements beyond
+    // the ends of k and of a K-major row as zeros.
+    __device__ __forceinline__ void fetch(int seg, int64_t k0, int64_t K, u32x4* v) const {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = row_of(i), c = chunk_of(i) * VEC;
+            const T* p;
+            int64_t at = source(KC ? r : 0, seg, &p), n;
+            if constexpr (KC) {
+                at = at < end ? at : end - 1;
+                p += at * s.stride + k0 + c;
+                n = K - k0 - c;
+            } else {
+                p += (k0 + r) * s.stride + first + c;
+                n = k0 + r < K ? end - first - c : 0;
+            }
+            if (n >= VEC) v[i] = load_vec(p);
+            else if (n > 0) v[i] = load_part(p, int(n));
+            else v[i] = u32x4{0, 0, 0, 0};
+        }
+    }
+    static __device__ __forceinline__ void put(AR_LDS char* lds, const u32x4* v) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            *(AR_LDS u32x4*)(lds + (i * THREADS + int(threadIdx.x)) * kChunk) = v[i];
+    }
+};
+
+// A lane's reader of one operand's fragments: 16 bytes, k 8 (4) to a half of
+// the wavefront, of row (column) lane % 32 of a square.
+template <class T, int N, bool KC>
+struct Frags {
+    static constexpr int E = int(sizeof(T));
+    int lane_off[4];
+
+    // `base`: the wavefront's first row in the panel, a multiple of 32.
+    __device__ __forceinline__ Frags(int base) {
+        const int lane = int(threadIdx.x) & 63;
+        if constexpr (KC) {
+            const int r = base + (lane & 31);
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                lane_off[s] = r * kStepBytes + (((2 * s + (lane >> 5)) ^ swz(r)) * kChunk);
+        } else if constexpr (E == 2) {
+            const int l = lane & 15, g = lane >> 4;
+            const int k = 8 * (g >> 1) + (l >> 2);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int c = base / 8 + 4 * j + 2 * (g & 1) + ((l & 3) >> 1);
+                lane_off[j] = k * (N * 2) + ((c ^ (2 * swzk(k))) * kChunk) + (l & 1) * 8;
+            }
+        } else {
+            lane_off[0] = (4 * (lane >> 5)) * (N * 4) + (base + (lane & 31)) * 4;
+        }
+    }
+    // Square j (32 rows on) of the panel at `lds`, substep s of the step's 4.
+    __device__ __forceinline__ u32x4 read(const AR_LDS char* lds, int j, int s) const {
+        if constexpr (KC) {
+            return *(const AR_LDS u32x4*)(lds + lane_off[s] + j * 32 * kStepBytes);
+        } else if constexpr (E == 2) {
+            typedef AR_LDS s16x4* P;
+            const AR_LDS char* at = lds + lane_off[j & 3] + (j >> 2) * 256 + s * 16 * (N * 2);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(at));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(at + 4 * (N * 2)));
+            struct { s16x4 a, b; } both{lo, hi};
+            return __builtin_bit_cast(u32x4, both);
+        } else {
+            u32x4 v;
+            const AR_LDS char* at = lds + lane_off[0] + j * 128 + s * 8 * (N * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = *(const AR_LDS uint32_t*)(at + e * (N * 4));
+            return v;
+        }
+    }
+};
+
+template <class T>
+__device__ __forceinline__ void multiply(const u32x4 l, const u32x4 r, f32x16& acc) {
+    if constexpr (sizeof(T) == 2) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, l),
+                                                      __builtin_bit_cast(bf16x8, r), acc, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(l[e]), __uint_as_float(r[e]),
+                                                       acc, 0, 0, 0);
+    }
+}
+
+// The tile of the block: blocks go to the 8 XCDs in turn, so XCD x takes a
+// contiguous eighth of the tiles, in strips of `kStrip` tile rows that are
+// walked along the columns: what its 32 CUs work on at a time shares panels
+// in its L2.
+constexpr int kStrip = 4;
+__device__ __forceinline__ bool tile_of(const ProductShape& p, int64_t block, int64_t* r,
+                                        int64_t* c) {
+    const int64_t tiles = p.row_tiles * p.col_tiles, share = (tiles + 7) / 8;
+    const int64_t t = (block & 7) * share + (block >> 3);
+    if ((block >> 3) >= share || t >= tiles) return false;
+    const int64_t per = kStrip * p.col_tiles, strip = t / per, in = t % per;
+    const int64_t h = p.row_tiles - strip * kStrip < kStrip ? p.row_tiles - strip * kStrip : kStrip;
+    *r = strip * kStrip + in % h;
+    *c = in / h;
+    return true;
+}
+inline int64_t tile_blocks(int64_t tiles) { return ceil_div(tiles, 8) * 8; }
+
+// This wavefront's copies have landed in LDS and its own LDS stores are done;
+// after the barrier that follows, so have all the block's.
+__device__ __forceinline__ void landed() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+}
+
+// The products of one tile: acc[i][j] is the square of row square i and column
+// square j of the wavefront (gated: j = 0 the gate's, 1 the up projection's).
+template <class T, int BR, int BC, int WR, int WC, bool RKC, bool LKC, bool GATED, bool DIRECT>
+struct Tile {
+    static constexpr int THREADS = 64 * WR * WC;
+    static constexpr int SR = BR / (32 * WR), SC = BC / (32 * WC);  // squares of a wavefront
+    static_assert(!GATED || SC == 2, "");
+    using RP = Panel<T, BR, THREADS, RKC, false>;
+    using LP = Panel<T, BC, THREADS, LKC, GATED>;
+    static constexpr int HALF = RP::BYTES + LP::BYTES;  // one of the two buffers
+    static constexpr int LDS = 2 * HALF;
+
+    static __device__ __forceinline__ void run(const ProductShape& p, const Side<T>& R,
+                                               const Side<T>& L, int64_t r0, int64_t c0,
+                                               AR_LDS char* lds, f32x16 (&acc)[SR][SC]) {
+        const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
+        const RP rp(R, r0, p.rows);
+        const LP lp(L, c0, p.cols);
+        const Frags<T, BR, RKC> rf(wr * SR * 32);
+        const Frags<T, BC, LKC> lf(wc * (GATED ? 32 : SC * 32));
+        constexpr int KS = StepOf<T>::K;
+        const int steps = int((p.K + KS - 1) / KS) * p.segments;
+        u32x4 rv[DIRECT ? 1 : RP::LOADS], lv[DIRECT ? 1 : LP::LOADS];
+
+        auto start = [&](int seg, int64_t k0, int at) {
+            AR_LDS char* const buf = lds + at;
+            if constexpr (DIRECT) {
+                if (k0 + KS <= p.K) {
+                    const uint32_t to = uint32_t(reinterpret_cast<uintptr_t>(buf));
+                    rp.copy(seg, k0, to);
+                    lp.copy(seg, k0, to + RP::BYTES);
+                } else {  // the last, partial step
+                    u32x4 a[RP::LOADS], b[LP::LOADS];
+                    rp.fetch(seg, k0, p.K, a);
+                    lp.fetch(seg, k0, p.K, b);
+                    RP::put(buf, a);
+                    LP::put(buf + RP::BYTES, b);
+                }
+            } else {
+                rp.fetch(seg, k0, p.K, rv);
+                lp.fetch(seg, k0, p.K, lv);
+            }
+        };
+        auto finish = [&](int at) {
+            if constexpr (!DIRECT) {
+                RP::put(lds + at, rv);
+                LP::put(lds + at + RP::BYTES, lv);
+            }
+        };
+        auto compute = [&](int at) {
+            const AR_LDS char* const buf = lds + at;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                u32x4 r[SR], l[SC];
+#pragma unroll
+                for (int j = 0; j < SC; ++j)
+                    l[j] = lf.read(buf + RP::BYTES, GATED ? j * (BC / 64) : j, s);
+#pragma unroll
+                for (int i = 0; i < SR; ++i) r[i] = rf.read(buf, i, s);
+#pragma unroll
+                for (int i = 0; i < SR; ++i)
+#pragma unroll
+                    for (int j = 0; j < SC; ++j) multiply<T>(l[j], r[i], acc[i][j]);
+            }
+        };
+        if (steps == 0) return;
+        int seg = 0, at = 0;
+        int64_t k0 = 0;
+        start(0, 0, 0);
+        finish(0);
+        landed();
+        __builtin_amdgcn_s_barrier();
+        for (int t = 0; t < steps; ++t) {
+            const bool more = t + 1 < steps;
+            if (more) {
+                k0 += KS;
+                if (k0 >= p.K) {
+                    k0 = 0;
+                    ++seg;
+                }
+                start(seg, k0, HALF - at);
+            }
+            compute(at);
+            at = HALF - at;
+            if (more) finish(at);
+            landed();
+            __builtin_amdgcn_s_barrier();
+        }
+    }
+};
+
+// Squares to memory: each wavefront passes a row of squares at a time through
+// its own part of LDS, as fp32, and stores whole runs of the output's rows.
+// `f(i, j, e)` is element e of the accumulators' layout.
+template <int SC>
+struct Store {
+    static constexpr int PITCH = SC * 32 + 4;              // floats a row
+    static constexpr int BYTES = 32 * PITCH * 4;           // a wavefront's part
+    template <class F>
+    static __device__ __forceinline__ void fill(AR_LDS float* part, F&& f) {
+        const int lane = int(threadIdx.x) & 63;
+#pragma unroll
+        for (int j = 0; j < SC; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                typedef float f4 __attribute__((ext_vector_type(4)));
+                const f4 v = {f(j, 4 * q), f(j, 4 * q + 1), f(j, 4 * q + 2), f(j, 4 * q + 3)};
+                *(AR_LDS f4*)(part + (lane & 31) * PITCH + j * 32 + 8 * q + 4 * (lane >> 5)) = v;
+            }
+    }
+    // rows r0 .. of `out`, columns c0 .. of the SC * 32
+    template <class T>
+    static __device__ __forceinline__ void store(const AR_LDS float* part, T* out, int64_t stride,
+                                                 int64_t r0, int64_t rows, int64_t c0, int64_t cols,
+                                                 bool accumulate) {
+        constexpr int VEC = Num<T>::VEC, PER = SC * 32 / VEC, ROWS = 64 / PER;
+        const int lane = int(threadIdx.x) & 63;
+#pragma unroll
+        for (int b = 0; b < 32; b += ROWS) {
+            const int r = b + lane / PER, c = lane % PER * VEC;
+            const int64_t left = cols - c0 - c;
+            if (r0 + r >= rows || left <= 0) continue;
+            T* const at = out + (r0 + r) * stride + c0 + c;
+            float v[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[e] = part[r * PITCH + c + e];
+            const int n = int(left < VEC ? left : VEC);
+            if (accumulate) {
+                float old[VEC];
+                Num<T>::unpack(n == VEC ? load_vec(at) : load_part(at, n), old);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[e] += old[e];
+            }
+            if (n == VEC) store_vec(at, Num<T>::pack(v));
+            else store_part(at, Num<T>::pack(v), n);
+        }
+    }
+};
+
+// The wavefront's LDS traffic of one lane is another's: order it.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+}  // namespace arp

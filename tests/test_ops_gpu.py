@@ -173,6 +173,15 @@ def test_glu(M, D, F, dtype, act, layout):
         c()
 
 
+@pytest.mark.parametrize("layout", ("rows", "wide"))
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,D,F", [(2050, 72, 3000), (2309, 5800, 40), (50, 3849, 3081)])
+def test_glu_many_tiles(M, D, F, dtype, layout):
+    """Products of so many tiles that the largest ones are taken: h's, dx's and
+    the weight gradients', in turn."""
+    test_glu(M, D, F, dtype, "silu", layout)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_glu_empty(dtype):
     dt = ref.TORCH[dtype]
