@@ -535,8 +535,7 @@ ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_t F, int32
  * Elsewhere a logit of NaN or +inf makes the row's loss and gradient NaN, such
  * a teacher entry the loss and the gradient at the entries' ids; a masked
  * student logit of -inf at an entry with p > 0 gives loss +inf and a finite
- * gradient.  teacher_dtype may
- * differ from dtype; loss and weights are fp32 vectors.  grad may be NULL
+ * gradient.  teacher_dtype may differ from dtype; loss and weights are fp32 vectors.  grad may be NULL
  * (the loss alone), or logits itself with the same stride (in place).
  * K <= AR_DISTILL_MAX_K (AR_ERR_UNSUPPORTED above); temperature finite and > 0. */
 #define AR_DISTILL_MAX_K 4096

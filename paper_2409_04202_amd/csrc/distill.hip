@@ -1,12 +1,24 @@
 // Distillation from a teacher's top logits, forward and backward.
 //
-// A block takes a row.  In units of log2, with c = log2(e) / temperature:
-//   m = max z,  S = sum 2^((z - m) c),  log2 q_j = (z_j - m) c - log2 S
+// In units of log2, with c = log2(e) / temperature and any base m near the
+// row's maximum:
+//   S = sum 2^((z - m) c),  log2 q_j = (z_j - m) c - log2 S
 // and the same for the teacher's entries; the loss and the gradient follow
-// from these.  The difference comes before the product, which could overflow
-// at a mask of the type's lowest value.  The first pass over the row takes the running maximum and sum
-// (a sum is rescaled where the maximum rises); the second computes the
-// gradient.  Bound by memory: the row read and the gradient written.
+// from these.  Over a row (z - m) c is computed as z c - r with r = m c
+// rounded, one fused multiply-add; what that is off by, m c - r, is the same
+// for every z, known exactly by one more, and taken out of the sum.  m need
+// not be the maximum, only near enough for the sum to stay in range: a
+// wavefront takes the largest of the first vectors it holds, and looks for its
+// true maximum, and takes differences, only where its sum shows that this
+// would not do (a mask of the type's lowest value throughout, say).
+//
+// Bound by memory: the row read once and the gradient written once.  Two forms:
+//  * kept: a block a row, which it holds in registers between the sum and the
+//    gradient, so the row is read once;
+//  * split: rows longer than a block holds, and rows too few to fill the card.
+//    Each row is cut into parts of a block; one launch leaves the parts' sums,
+//    a second one reads the parts again (as many rows at a time as the
+//    last-level cache holds) and writes the gradient.
 #include <algorithm>
 #include <cmath>
 
@@ -15,8 +27,26 @@
 namespace arp {
 namespace {
 
-constexpr int kBlock = 1024;
-constexpr int kWaves = kBlock / 64;
+// Vectors of a row that a thread keeps: 64 registers, which leaves a CU its 16
+// wavefronts.
+constexpr int kKeep = 16;
+
+__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The sum S of 2^((z - m) c) over some elements; an empty one is (-inf, 0).
+struct PartSum {
+    float m, S;
+    __device__ __forceinline__ void add(const PartSum& o, float c) {
+        const float high = fmaxf(m, o.m);
+        // (an empty one adds nothing, not 0 * inf)
+        S = (S == 0.0f ? 0.0f : S * pow2((m - high) * c)) +
+            (o.S == 0.0f ? 0.0f : o.S * pow2((o.m - high) * c));
+        m = high;
+    }
+};
+
+// Whether z c - r with r = m c is near enough to (z - m) c.
+__device__ __forceinline__ bool near_base(float r) { return fabsf(r) < 0x1p24f; }
 
 struct DistillArgs {
     const int64_t* ids;
@@ -26,144 +56,400 @@ struct DistillArgs {
     int64_t logits_stride, teacher_stride, ids_stride, grad_stride;
     float c;            // log2(e) / temperature
     float temperature;
+    int64_t first;      // the launch's first row
+    // split form
+    int64_t parts, part;         // parts of a row, elements of one
+    PartSum* sums;               // of each part of each row of the launch
+    float* at;                   // the student's logits at the entries, K a row
 };
-
-// A maximum and the sum of 2^((x - maximum) c); an empty one is (-inf, 0).
-struct MaxSum {
-    float m, s;
-    __device__ __forceinline__ void add(const MaxSum o, float c) {
-        const float top = fmaxf(m, o.m);
-        // nothing but -inf so far: the sums are 0 (or NaN) and stay so
-        const float base = top == -INFINITY ? 0.0f : top;
-        s = s * exp2f((m - base) * c) + o.s * exp2f((o.m - base) * c);
-        m = top;
-    }
-};
-
-__device__ __forceinline__ MaxSum wave_sum(MaxSum a, float c) {
-    for (int d = 32; d > 0; d /= 2) a.add({__shfl_xor(a.m, d), __shfl_xor(a.s, d)}, c);
-    return a;
-}
 
 __device__ __forceinline__ float wave_sum(float v) {
     for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
     return v;
 }
+__device__ __forceinline__ float wave_max(float v) {
+    for (int d = 32; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
 
-template <class T, class S>
-__global__ __launch_bounds__(kBlock) void distill_kernel(DistillArgs a, const T* logits,
-                                                         const S* teacher, T* grad) {
-    constexpr int VEC = Num<T>::VEC;
-    extern __shared__ char lds[];
-    __shared__ MaxSum part[kWaves];
-    __shared__ float terms[kWaves];
-    int32_t* const eid = reinterpret_cast<int32_t*>(lds);      // an entry's id, -1 if absent
-    float* const ep = reinterpret_cast<float*>(lds) + a.K;     // the teacher's logit, then p
-    float* const ez = reinterpret_cast<float*>(lds) + 2 * a.K; // the student's logit there, then log2 q
+// A block's part of a row, elements [0, len) of z, in its threads' registers:
+// vectors i * B + thread, and up to VEC - 1 elements at the end one a thread.
+// What lies beyond is -inf.
+template <class T, int B>
+struct Part {
+    static constexpr int VEC = Num<T>::VEC;
+    static constexpr int64_t LEN = int64_t(B) * kKeep * VEC;
+    u32x4 v[kKeep];
+    float last;
+    int vecs, tail, rounds;  // whole vectors, elements after them, rounds of B vectors
+
+    __device__ __forceinline__ void extent(int64_t len) {
+        vecs = int(len / VEC);
+        tail = int(len % VEC);
+        rounds = (vecs + B - 1) / B;
+    }
+    __device__ __forceinline__ void load(const T* z) {
+        constexpr uint32_t none = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+            v[i] = u32x4{none, none, none, none};
+            if (i < rounds && i * B + int(threadIdx.x) < vecs)
+                v[i] = load_vec(z + (i * B + int(threadIdx.x)) * VEC);
+        }
+        last = int(threadIdx.x) < tail ? Num<T>::up(z[vecs * VEC + int(threadIdx.x)]) : -INFINITY;
+    }
+    template <class F>
+    __device__ __forceinline__ void each(F&& f) const {
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+            if (i < rounds) {
+                float x[VEC];
+                Num<T>::unpack(v[i], x);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f(x[e]);
+            }
+        }
+        f(last);
+    }
+    // This wavefront's sum (the same in every lane).
+    __device__ __forceinline__ PartSum sum(float c) const {
+        float x[VEC];
+        Num<T>::unpack(v[0], x);
+        float m = last;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) m = fmaxf(m, x[e]);
+        m = wave_max(m);
+        const float r = m * c;
+        if (near_base(r)) {
+            float S[2] = {0.0f, 0.0f};
+            int n = 0;
+            each([&](float z) { S[n++ & 1] += pow2(fmaf(z, c, -r)); });
+            const float s = wave_sum(S[0] + S[1]);
+            // (the largest of the sample adds 1)
+            if (s >= 0.5f && s < 0x1p60f) return {m, s * pow2(-fmaf(m, c, -r))};
+        }
+        // by the true maximum: the sample was far from it, or empty, or there
+        // is a NaN
+        m = -INFINITY;
+        each([&](float z) { m = fmaxf(m, z); });
+        m = wave_max(m);
+        const float base = m == -INFINITY ? 0.0f : m;
+        float s = 0.0f;
+        each([&](float z) { s += pow2((z - base) * c); });
+        s = wave_sum(s);
+        return {s == 0.0f ? -INFINITY : base, s};
+    }
+    // g = f(z).
+    template <class F>
+    __device__ __forceinline__ void store_as(T* g, F&& f) const {
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+            if (i < rounds && i * B + int(threadIdx.x) < vecs) {
+                float x[VEC];
+                Num<T>::unpack(v[i], x);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) x[e] = f(x[e]);
+                store_vec(g + (i * B + int(threadIdx.x)) * VEC, Num<T>::pack(x));
+            }
+        }
+        if (int(threadIdx.x) < tail) g[vecs * VEC + int(threadIdx.x)] = Num<T>::down(f(last));
+    }
+    __device__ __forceinline__ void store_zero(T* g) const {
+        for (int i = int(threadIdx.x); i < vecs; i += B) store_vec(g + i * VEC, u32x4{0, 0, 0, 0});
+        if (int(threadIdx.x) < tail) g[vecs * VEC + int(threadIdx.x)] = T(0);
+    }
+};
+
+// A row's statistics.
+struct Row {
+    float m, S, c;
+    __device__ __forceinline__ float log2q(float z) const {
+        return (z - m) * c - __builtin_amdgcn_logf(S);
+    }
+};
+
+// The teacher's entries of a row, in LDS, one a thread at a time.
+struct Entries {
+    int32_t* id;  // -1 if absent
+    float* p;     // the teacher's logit, then p
+    float* z;     // the student's logit
+};
+
+template <int B>
+struct Shared {
+    PartSum part[B / 64];
+    float term[B / 64];
+};
+
+// Reads the entries; false if none is present (the same for every thread).
+// `logit(k, id)` is the student's logit at entry k.
+template <class S, int B, class F>
+__device__ __forceinline__ bool read_entries(const DistillArgs& a, int64_t t, const S* teacher,
+                                             const Entries& e, F&& logit) {
+    int any = 0;
+    for (int64_t k = threadIdx.x; k < a.K; k += B) {
+        const int64_t id = a.ids[t * a.ids_stride + k];
+        const float s = Num<S>::up(teacher[t * a.teacher_stride + k]);
+        const bool is = id >= 0 && id < a.V && s != -INFINITY;
+        e.id[k] = is ? int32_t(id) : -1;
+        e.p[k] = s;
+        e.z[k] = is ? logit(k, id) : 0.0f;
+        any |= is;
+    }
+    return __syncthreads_or(any) != 0;
+}
+
+// The entries' p, by differences to their largest; the block's loss, without
+// its factors, in thread 0.
+template <int B>
+__device__ __forceinline__ float finish_entries(const DistillArgs& a, const Entries& e,
+                                                const Row& row, Shared<B>& sh) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-
-    auto all = [&](MaxSum v) {  // over the block
-        v = wave_sum(v, a.c);
+    auto all = [&](float v, bool max) {
+        v = max ? wave_max(v) : wave_sum(v);
         __syncthreads();
-        if (lane == 0) part[w] = v;
+        if (lane == 0) sh.term[w] = v;
         __syncthreads();
-        MaxSum r = part[0];
-        for (int i = 1; i < kWaves; ++i) r.add(part[i], a.c);
-        return r;
+        v = sh.term[0];
+        for (int i = 1; i < B / 64; ++i) v = max ? fmaxf(v, sh.term[i]) : v + sh.term[i];
+        return v;
     };
+    float top = -INFINITY, sum = 0.0f, loss = 0.0f;
+    for (int64_t k = threadIdx.x; k < a.K; k += B)
+        if (e.id[k] >= 0) top = fmaxf(top, e.p[k]);
+    top = all(top, true);
+    for (int64_t k = threadIdx.x; k < a.K; k += B)
+        if (e.id[k] >= 0) sum += pow2((e.p[k] - top) * a.c);
+    sum = all(sum, false);
+    const float ls = __builtin_amdgcn_logf(sum);
+    for (int64_t k = threadIdx.x; k < a.K; k += B) {
+        if (e.id[k] < 0) continue;
+        const float lp = (e.p[k] - top) * a.c - ls, p = pow2(lp);
+        e.p[k] = p;
+        if (p != 0.0f) loss += p * (lp - row.log2q(e.z[k]));
+    }
+    return all(loss, false) * 0.6931471805599453f;
+}
 
-    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        const T* const z = logits + t * a.logits_stride;
-        T* const g = grad ? grad + t * a.grad_stride : nullptr;
-        const float weight = a.weights ? a.weights[t] : 1.0f;
-        MaxSum tea{-INFINITY, 0.0f}, stu{-INFINITY, 0.0f};
-        __syncthreads();  // the entries of the row before are done with
-        if (weight != 0.0f) {
-            for (int64_t k = threadIdx.x; k < a.K; k += kBlock) {
-                const int64_t id = a.ids[t * a.ids_stride + k];
-                const float s = Num<S>::up(teacher[t * a.teacher_stride + k]);
-                const bool is = id >= 0 && id < a.V && s != -INFINITY;
-                eid[k] = is ? int32_t(id) : -1;
-                ep[k] = s;
-                ez[k] = is ? Num<T>::up(z[id]) : 0.0f;
-                if (is) tea.add({s, 1.0f}, a.c);
-            }
-            tea = all(tea);
-        }
-        bool live = weight != 0.0f && (tea.s != 0.0f);
-        if (live) {
-            for (int64_t at = int64_t(threadIdx.x) * VEC; at < a.V; at += kBlock * VEC) {
-                const int n = int(a.V - at < VEC ? a.V - at : VEC);
-                float f[VEC];
-                Num<T>::unpack(n == VEC ? load_vec(z + at) : load_part(z + at, n), f);
-                for (int i = 0; i < VEC; ++i) f[i] = i < n ? f[i] : -INFINITY;
-                float top = stu.m;
-                for (int i = 0; i < VEC; ++i) top = fmaxf(top, f[i]);
-                const float base = top == -INFINITY ? 0.0f : top;
-                float s = stu.s * exp2f((stu.m - base) * a.c);
-                for (int i = 0; i < VEC; ++i) s += exp2f((f[i] - base) * a.c);
-                stu = {top, s};
-            }
-            stu = all(stu);
-            live = stu.s != 0.0f;
-        }
-        if (!live) {
-            if (threadIdx.x == 0) a.loss[t] = 0.0f;
-            if (g) {
-                for (int64_t at = int64_t(threadIdx.x) * VEC; at < a.V; at += kBlock * VEC) {
-                    if (a.V - at >= VEC) store_vec(g + at, u32x4{0, 0, 0, 0});
-                    else store_part(g + at, u32x4{0, 0, 0, 0}, int(a.V - at));
-                }
-            }
-            continue;
-        }
-        const float ls = log2f(stu.s), lt = log2f(tea.s);
-        float sum = 0.0f;
-        for (int64_t k = threadIdx.x; k < a.K; k += kBlock) {
-            if (eid[k] < 0) continue;
-            const float lp = (ep[k] - tea.m) * a.c - lt, lq = (ez[k] - stu.m) * a.c - ls;
-            const float p = exp2f(lp);
-            ep[k] = p;
-            ez[k] = lq;
-            if (p != 0.0f) sum += p * (lp - lq);
-        }
-        sum = wave_sum(sum);
-        if (lane == 0) terms[w] = sum;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            float v = 0.0f;
-            for (int i = 0; i < kWaves; ++i) v += terms[i];
-            a.loss[t] = weight * a.temperature * a.temperature * (v * 0.6931471805599453f);
-        }
-        if (!g) continue;
-        const float scale = weight * a.temperature;
-        for (int64_t at = int64_t(threadIdx.x) * VEC; at < a.V; at += kBlock * VEC) {
-            const int n = int(a.V - at < VEC ? a.V - at : VEC);
-            float f[VEC];
-            Num<T>::unpack(n == VEC ? load_vec(z + at) : load_part(z + at, n), f);
-            for (int i = 0; i < VEC; ++i) f[i] = scale * exp2f((f[i] - stu.m) * a.c - ls);
-            if (n == VEC) store_vec(g + at, Num<T>::pack(f));
-            else store_part(g + at, Num<T>::pack(f), n);
-        }
-        __syncthreads();  // the entries' elements are written once more, after these
-        for (int64_t k = threadIdx.x; k < a.K; k += kBlock) {
-            const int32_t id = eid[k];
-            if (id < 0) continue;
-            float p = 0.0f;  // of every entry with this id: each of them stores the same
-            for (int64_t j = 0; j < a.K; ++j)
-                if (eid[j] == id) p += ep[j];
-            g[id] = Num<T>::down(scale * (exp2f(ez[k]) - p));
-        }
+// The gradient at the entries in [lo, hi): every entry with an id stores the
+// same, less the p of all of them.
+template <class T, int B>
+__device__ __forceinline__ void store_entries(const DistillArgs& a, const Entries& e,
+                                              const Row& row, float scale, int64_t lo, int64_t hi,
+                                              T* g) {
+    for (int64_t k = threadIdx.x; k < a.K; k += B) {
+        const int32_t id = e.id[k];
+        if (id < lo || id >= hi || id < 0) continue;
+        float p = 0.0f;
+        for (int64_t j = 0; j < a.K; ++j)
+            if (e.id[j] == id) p += e.p[j];
+        g[id] = Num<T>::down(scale * (pow2(row.log2q(e.z[k])) - p));
     }
 }
 
+template <class T, int B>
+__device__ __forceinline__ void store_part_gradient(const Part<T, B>& part, const Row& row,
+                                                    float scale, T* g) {
+    const float r = row.m * row.c;
+    if (near_base(r)) {
+        const float f = scale / row.S * pow2(-fmaf(row.m, row.c, -r));
+        part.store_as(g, [&](float z) { return f * pow2(fmaf(z, row.c, -r)); });
+    } else {
+        const float f = scale / row.S;
+        part.store_as(g, [&](float z) { return f * pow2((z - row.m) * row.c); });
+    }
+}
+
+template <class T, class S, int B>
+__global__ __launch_bounds__(B) void kept_kernel(DistillArgs a, const T* logits, const S* teacher,
+                                                 T* grad) {
+    extern __shared__ char lds[];
+    __shared__ Shared<B> sh;
+    const Entries e{reinterpret_cast<int32_t*>(lds), reinterpret_cast<float*>(lds) + a.K,
+                    reinterpret_cast<float*>(lds) + 2 * a.K};
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t t = a.first + blockIdx.x;
+    const T* const z = logits + t * a.logits_stride;
+    T* const g = grad ? grad + t * a.grad_stride : nullptr;
+    const float weight = a.weights ? a.weights[t] : 1.0f;
+    Part<T, B> part;
+    part.extent(a.V);
+    Row row{};
+    bool live = weight != 0.0f;
+    if (live) {
+        part.load(z);
+        live = read_entries<S, B>(a, t, teacher, e, [&](int64_t, int64_t id) { return Num<T>::up(z[id]); });
+    }
+    if (live) {
+        const PartSum own = part.sum(a.c);
+        if (lane == 0) sh.part[w] = own;
+        __syncthreads();
+        PartSum s = sh.part[0];
+        for (int i = 1; i < B / 64; ++i) s.add(sh.part[i], a.c);
+        row = Row{s.m, s.S, a.c};
+        live = s.S != 0.0f;
+    }
+    if (!live) {
+        if (threadIdx.x == 0) a.loss[t] = 0.0f;
+        if (g) part.store_zero(g);
+        return;
+    }
+    const float loss = finish_entries<B>(a, e, row, sh);
+    if (threadIdx.x == 0) a.loss[t] = weight * a.temperature * a.temperature * loss;
+    if (!g) return;
+    const float scale = weight * a.temperature;
+    store_part_gradient(part, row, scale, g);
+    __syncthreads();  // the entries' elements are written once more, after these
+    store_entries<T, B>(a, e, row, scale, 0, a.V, g);
+}
+
+// Split form, first launch: the parts' sums, and the student's logits at the
+// entries (the second launch may write over them).
+template <class T, int B>
+__global__ __launch_bounds__(B) void parts_kernel(DistillArgs a, const T* logits) {
+    __shared__ Shared<B> sh;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t i = blockIdx.x / a.parts, t = a.first + i, j = blockIdx.x % a.parts;
+    if (a.weights && a.weights[t] == 0.0f) return;
+    const T* const z = logits + t * a.logits_stride;
+    if (j == 0) {
+        for (int64_t k = threadIdx.x; k < a.K; k += B) {
+            const int64_t id = a.ids[t * a.ids_stride + k];
+            a.at[i * a.K + k] = id >= 0 && id < a.V ? Num<T>::up(z[id]) : 0.0f;
+        }
+    }
+    Part<T, B> part;
+    part.extent(a.V - j * a.part < a.part ? a.V - j * a.part : a.part);
+    part.load(z + j * a.part);
+    PartSum s = part.sum(a.c);
+    if (lane == 0) sh.part[w] = s;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    s = sh.part[0];
+    for (int n = 1; n < B / 64; ++n) s.add(sh.part[n], a.c);
+    a.sums[blockIdx.x] = s;
+}
+
+// Split form, second launch: every part's block joins its row's sums; the
+// first one stores the loss, each its part of the gradient.
+template <class T, class S, int B>
+__global__ __launch_bounds__(B) void split_kernel(DistillArgs a, const T* logits, const S* teacher,
+                                                  T* grad) {
+    extern __shared__ char lds[];
+    __shared__ Shared<B> sh;
+    const Entries e{reinterpret_cast<int32_t*>(lds), reinterpret_cast<float*>(lds) + a.K,
+                    reinterpret_cast<float*>(lds) + 2 * a.K};
+    const int lane = threadIdx.x & 63;
+    const int64_t blocks = grad ? a.parts : 1;  // a row's
+    const int64_t i = blockIdx.x / blocks, t = a.first + i, j = blockIdx.x % blocks;
+    const int64_t lo = j * a.part, hi = a.V - lo < a.part ? a.V : lo + a.part;
+    const T* const z = logits + t * a.logits_stride + lo;
+    T* const g = grad ? grad + t * a.grad_stride : nullptr;
+    const float weight = a.weights ? a.weights[t] : 1.0f;
+    Part<T, B> part;
+    part.extent(hi - lo);
+    Row row{};
+    bool live = weight != 0.0f;
+    if (live) {
+        if (g) part.load(z);
+        live = read_entries<S, B>(a, t, teacher, e, [&](int64_t k, int64_t) { return a.at[i * a.K + k]; });
+    }
+    if (live) {
+        const PartSum* const sums = a.sums + i * a.parts;
+        PartSum s{-INFINITY, 0.0f};
+        for (int64_t n = lane; n < a.parts; n += 64) s.add(sums[n], a.c);
+        for (int d = 1; d < 64; d *= 2) s.add({__shfl_xor(s.m, d), __shfl_xor(s.S, d)}, a.c);
+        row = Row{s.m, s.S, a.c};
+        live = s.S != 0.0f;
+    }
+    if (!live) {
+        if (threadIdx.x == 0 && j == 0) a.loss[t] = 0.0f;
+        if (g) part.store_zero(g + lo);
+        return;
+    }
+    const float loss = finish_entries<B>(a, e, row, sh);
+    if (threadIdx.x == 0 && j == 0) a.loss[t] = weight * a.temperature * a.temperature * loss;
+    if (!g) return;
+    const float scale = weight * a.temperature;
+    store_part_gradient(part, row, scale, g + lo);
+    __syncthreads();  // the entries' elements are written once more, after these
+    store_entries<T, B>(a, e, row, scale, lo, hi, g);
+}
+
+// ------------------------------------------------------------- launches
+
+constexpr int kSplitBlock = 256;
+// Rows from which each takes a block of its own.
+constexpr int64_t kKeptRows = 192;
+// Logits of the rows whose parts are read a second time before others are
+// read: they stay in the 256 MiB last-level cache.
+constexpr int64_t kSplitBytes = int64_t(96) << 20;
+
+struct Form {
+    bool kept;
+    int64_t part, parts, rows;  // split form: elements a part, parts a row, rows a launch
+};
+
+Form form_of(int64_t T, int64_t V, int esize) {
+    const int64_t vec = 16 / esize;
+    Form f{};
+    f.kept = T >= kKeptRows && V <= 1024 * kKeep * vec;
+    if (V <= 64 * kKeep * vec) f.kept = true;  // a wavefront holds the row
+    int64_t rounds = kKeep;  // parts so long that the card's CUs have several
+    while (rounds > 1 && T * ceil_div(V, kSplitBlock * vec * rounds) < 1024) rounds /= 2;
+    f.part = kSplitBlock * vec * rounds;
+    f.parts = std::max<int64_t>(1, ceil_div(V, f.part));
+    f.rows = std::max<int64_t>(1, std::min(T, kSplitBytes / std::max<int64_t>(1, V * esize)));
+    return f;
+}
+
+struct Space {
+    int64_t at, end;  // the entries' logits, behind the sums
+};
+Space space_of(const Form& f, int64_t K) {
+    Space s{};
+    if (f.kept) return s;
+    s.at = round_up(f.rows * f.parts * int64_t(sizeof(PartSum)), 256);
+    s.end = s.at + round_up(f.rows * K * 4, 256);
+    return s;
+}
+
+template <class T, class S, int B>
+void launch_kept(DistillArgs a, const T* z, const S* teacher, T* grad, hipStream_t st) {
+    constexpr int64_t kRows = int64_t(1) << 21;  // a launch's work-items are counted in 32 bits
+    for (a.first = 0; a.first < a.T; a.first += kRows)
+        hipLaunchKernelGGL((kept_kernel<T, S, B>), dim3(unsigned(std::min(kRows, a.T - a.first))),
+                           dim3(B), size_t(12 * a.K), st, a, z, teacher, grad);
+}
+
 template <class T, class S>
-ar_status run_distill(const DistillArgs& a, const void* logits, const void* teacher, void* grad,
-                      hipStream_t st) {
-    const unsigned grid = unsigned(std::min<int64_t>(a.T, 1 << 20));
-    hipLaunchKernelGGL((distill_kernel<T, S>), dim3(grid), dim3(kBlock), size_t(12 * a.K), st, a,
-                       static_cast<const T*>(logits), static_cast<const S*>(teacher),
-                       static_cast<T*>(grad));
+ar_status run_distill(DistillArgs a, const void* logits, const void* teacher, void* grad,
+                      char* workspace, hipStream_t st) {
+    const T* const z = static_cast<const T*>(logits);
+    const S* const s = static_cast<const S*>(teacher);
+    T* const g = static_cast<T*>(grad);
+    const Form f = form_of(a.T, a.V, int(sizeof(T)));
+    if (f.kept) {
+        const int64_t threads = ceil_div(a.V, kKeep * Num<T>::VEC);
+        if (threads <= 64) launch_kept<T, S, 64>(a, z, s, g, st);
+        else if (threads <= 128) launch_kept<T, S, 128>(a, z, s, g, st);
+        else if (threads <= 256) launch_kept<T, S, 256>(a, z, s, g, st);
+        else if (threads <= 512) launch_kept<T, S, 512>(a, z, s, g, st);
+        else launch_kept<T, S, 1024>(a, z, s, g, st);
+        return launch_status("distillation");
+    }
+    a.part = f.part;
+    a.parts = f.parts;
+    a.sums = reinterpret_cast<PartSum*>(workspace);
+    a.at = reinterpret_cast<float*>(workspace + space_of(f, a.K).at);
+    for (a.first = 0; a.first < a.T; a.first += f.rows) {
+        const int64_t rows = std::min(f.rows, a.T - a.first);
+        hipLaunchKernelGGL((parts_kernel<T, kSplitBlock>), dim3(unsigned(rows * f.parts)),
+                           dim3(kSplitBlock), 0, st, a, z);
+        hipLaunchKernelGGL((split_kernel<T, S, kSplitBlock>),
+                           dim3(unsigned(rows * (g ? f.parts : 1))), dim3(kSplitBlock),
+                           size_t(12 * a.K), st, a, z, s, g);
+    }
     return launch_status("distillation");
 }
 
@@ -179,7 +465,7 @@ AR_EXPORT ar_status ar_distill_workspace(int64_t T, int64_t V, int64_t K, int64_
     AR_TRY(check_extent("V", V));
     AR_TRY(check_extent("K", K));
     if (K > AR_DISTILL_MAX_K) return fail(AR_ERR_UNSUPPORTED, "K exceeds AR_DISTILL_MAX_K");
-    *bytes = 0;
+    *bytes = std::max(space_of(form_of(T, V, 4), K).end, space_of(form_of(T, V, 2), K).end);
     return AR_OK;
 }
 
@@ -209,12 +495,24 @@ AR_EXPORT ar_status ar_distill(int32_t dtype, int64_t T, int64_t V, int64_t K, c
     for (const MatArg& m : {mt, mi, mw, mo}) AR_TRY(check_apart(mg, m));
     for (const MatArg& m : {ml, mt, mi, mw, mo, mg}) AR_TRY(check_apart(ms, m));
     if (T == 0) return AR_OK;
-    const DistillArgs a{ids, weights, loss, T, V, K, logits_stride, teacher_stride, ids_stride,
-                        grad_stride, float(1.4426950408889634 / double(temperature)), temperature};
+    DistillArgs a{};
+    a.ids = ids;
+    a.weights = weights;
+    a.loss = loss;
+    a.T = T;
+    a.V = V;
+    a.K = K;
+    a.logits_stride = logits_stride;
+    a.teacher_stride = teacher_stride;
+    a.ids_stride = ids_stride;
+    a.grad_stride = grad_stride;
+    a.c = float(1.4426950408889634 / double(temperature));
+    a.temperature = temperature;
+    char* const ws = static_cast<char*>(workspace);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == AR_F32)
-        return teacher_dtype == AR_F32 ? run_distill<float, float>(a, logits, teacher, grad, st)
-                                       : run_distill<float, uint16_t>(a, logits, teacher, grad, st);
-    return teacher_dtype == AR_F32 ? run_distill<uint16_t, float>(a, logits, teacher, grad, st)
-                                   : run_distill<uint16_t, uint16_t>(a, logits, teacher, grad, st);
+        return teacher_dtype == AR_F32 ? run_distill<float, float>(a, logits, teacher, grad, ws, st)
+                                       : run_distill<float, uint16_t>(a, logits, teacher, grad, ws, st);
+    return teacher_dtype == AR_F32 ? run_distill<uint16_t, float>(a, logits, teacher, grad, ws, st)
+                                   : run_distill<uint16_t, uint16_t>(a, logits, teacher, grad, ws, st);
 }

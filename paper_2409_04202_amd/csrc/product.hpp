@@ -56,10 +56,6 @@ struct ProductShape {
 __device__ __forceinline__ int swz(int r) { return ((r >> 1) ^ ((r & 1) << 2)) & 7; }
 __device__ __forceinline__ int swzk(int k) { return ((k & 3) ^ ((k & 3) << 1)) & 7; }
 
-__device__ __forceinline__ uint32_t scalar(uint32_t v) {
-    return uint32_t(__builtin_amdgcn_readfirstlane(int(v)));
-}
-
 // One operand's panel: N rows (K-contiguous) or columns (K-major) of the step.
 template <class T, int N, int THREADS, bool KC, bool GATED>
 struct Panel {

@@ -50,6 +50,11 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 typedef u32x4 u32x4_e4 __attribute__((aligned(4)));
 typedef u32x4 u32x4_e2 __attribute__((aligned(2)));
 
+// A value that is the same in every lane, in a scalar register.
+__device__ __forceinline__ uint32_t scalar(uint32_t v) {
+    return uint32_t(__builtin_amdgcn_readfirstlane(int(v)));
+}
+
 template <class T> struct Num;
 template <> struct Num<float> {
     static constexpr int VEC = 4;  // elements of a 16-byte vector

@@ -81,7 +81,8 @@ def test_embed_lookup(T, V, D, kind, dtype, layout):
 @pytest.mark.parametrize("T,V,D,kind", [
     (1, 7, 64, "zipf"), (0, 5, 9, "zipf"), (31, 1, 3, "one"), (32, 3, 16, "one"),
     (33, 3, 16, "one"), (700, 300, 257, "edges"), (1000, 9, 40, "zipf"), (64, 1000, 8, "none"),
-    (4097, 70001, 24, "zipf"), (9000, 2, 12, "zipf"), (20011, 400, 16, "zipf"),
+    (4097, 70001, 24, "zipf"), (9000, 2, 12, "zipf"), (16384, 300000, 4, "zipf"),
+    (16385, 511, 9, "zipf"), (20011, 400, 16, "zipf"), (16383, 512, 5, "one"),
     (40000, 100000, 8, "edges")])
 def test_embed_grad(T, V, D, kind, dtype, layout, accumulate):
     dout, ids = rnd(3, T, D, dtype=dtype), ids_of(4, T, V, kind)
@@ -297,10 +298,12 @@ def test_distill(T, V, K, tau, dtype, tdtype, layout):
     assert torch.equal(gz, there)
 
 
+@pytest.mark.parametrize("V,copies", [(2051, 1), (2051, 13), (20011, 1), (20011, 13), (70001, 13)])
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_distill_masks(dtype):
+def test_distill_masks(dtype, V, copies):
+    """Every kind of mask, in few rows and in many."""
     inf, nan, low = float("inf"), float("nan"), torch.finfo(ref.TORCH[dtype]).min
-    T, V, K = 16, 2051, 6
+    T, K = 16, 6
     z = rnd(1, T, V, dtype=dtype, scale=3.0)
     ids, tea = teacher_of(2, T, V, K)
     w = torch.ones(T)
@@ -327,11 +330,17 @@ def test_distill_masks(dtype):
     (loss, el), (grad, eg) = ref.distill(z, tea.to(ref.TORCH[dtype]), ids, 1.3, w, dtype)
     assert bool(loss[6] == inf) and bool(grad[6].isfinite().all())
     assert bool(loss[10].isnan()) and bool(loss[11].isnan()) and bool(loss[12].isnan())
-    args = z.cuda(), tea.to(ref.TORCH[dtype]).cuda(), ids.cuda()
-    got, g = ops.distill(*args, temperature=1.3, weights=w.cuda(),
-                         grad=torch.empty(T, V, dtype=z.dtype, device="cuda"))
-    only = ops.distill(*args, temperature=1.3, weights=w.cuda())
+    args = [x.cuda().repeat(copies, 1) for x in (z, tea.to(ref.TORCH[dtype]), ids)]
+    weights = w.cuda().repeat(copies)
+    got, g = ops.distill(*args, temperature=1.3, weights=weights,
+                         grad=torch.empty(copies * T, V, dtype=z.dtype, device="cuda"))
+    only = ops.distill(*args, temperature=1.3, weights=weights)
     assert torch.equal(only.nan_to_num(nan=-5.0), got.nan_to_num(nan=-5.0))
+    bits = g.view(torch.int32 if dtype == "f32" else torch.int16).view(copies, T, V)
+    assert bool((bits == bits[:1]).all())
+    ops.distill(*args, temperature=1.3, weights=weights, grad=args[0])
+    assert torch.equal(args[0].view(bits.dtype).view(bits.shape), bits)
+    got, g = got[-T:], g[-T:]
     ref.compare("loss", got, loss, el)
     for t in range(T):
         if t != 12:     # (a NaN in the teacher: below)
