@@ -13,8 +13,9 @@
 // would not do (a mask of the type's lowest value throughout, say).
 //
 // Bound by memory: the row read once and the gradient written once.  Two forms:
-//  * kept: a block a row, which it holds in registers between the sum and the
-//    gradient, so the row is read once;
+//  * kept: a block takes rows in turn and holds each in registers between the
+//    sum and the gradient, so that it is read once; as it stores the gradient
+//    it loads the next row into the registers that become free;
 //  * split: rows longer than a block holds, and rows too few to fill the card.
 //    Each row is cut into parts of a block; one launch leaves the parts' sums,
 //    a second one reads the parts again (as many rows at a time as the
@@ -36,13 +37,6 @@ __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x
 // The sum S of 2^((z - m) c) over some elements; an empty one is (-inf, 0).
 struct PartSum {
     float m, S;
-    __device__ __forceinline__ void add(const PartSum& o, float c) {
-        const float high = fmaxf(m, o.m);
-        // (an empty one adds nothing, not 0 * inf)
-        S = (S == 0.0f ? 0.0f : S * pow2((m - high) * c)) +
-            (o.S == 0.0f ? 0.0f : o.S * pow2((o.m - high) * c));
-        m = high;
-    }
 };
 
 // Whether z c - r with r = m c is near enough to (z - m) c.
@@ -56,25 +50,55 @@ struct DistillArgs {
     int64_t logits_stride, teacher_stride, ids_stride, grad_stride;
     float c;            // log2(e) / temperature
     float temperature;
-    int64_t first;      // the launch's first row
     // split form
-    int64_t parts, part;         // parts of a row, elements of one
+    int64_t first, parts, part;  // the launch's first row; parts of a row, elements of one
     PartSum* sums;               // of each part of each row of the launch
     float* at;                   // the student's logits at the entries, K a row
 };
 
+// Reductions over a wavefront, in the register file: after four shifts within
+// the rows of 16 lanes and two broadcasts from row to row lane 63 has them all.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float from_lane(float v, float none) {
+    return __uint_as_float(uint32_t(__builtin_amdgcn_update_dpp(
+        int(__float_as_uint(none)), int(__float_as_uint(v)), CTRL, ROWS, 0xF, false)));
+}
+template <class F>
+__device__ __forceinline__ float wave_reduce(float v, float none, F&& f) {
+    v = f(v, from_lane<0x111, 0xF>(v, none));
+    v = f(v, from_lane<0x112, 0xF>(v, none));
+    v = f(v, from_lane<0x114, 0xF>(v, none));
+    v = f(v, from_lane<0x118, 0xF>(v, none));
+    v = f(v, from_lane<0x142, 0xA>(v, none));
+    v = f(v, from_lane<0x143, 0xC>(v, none));
+    return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), 63)));
+}
 __device__ __forceinline__ float wave_sum(float v) {
-    for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
-    return v;
+    return wave_reduce(v, 0.0f, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ float wave_max(float v) {
-    for (int d = 32; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
+    return wave_reduce(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// The sum of n parts.
+__device__ __forceinline__ PartSum join(const PartSum* part, int64_t n, float c) {
+    PartSum all{-INFINITY, 0.0f};
+    for (int64_t i = 0; i < n; i += 64) {
+        const int64_t at = i + (threadIdx.x & 63);
+        const PartSum p = at < n ? part[at] : PartSum{-INFINITY, 0.0f};
+        const float high = fmaxf(all.m, wave_max(p.m));
+        // (an empty one adds nothing, not 0 * inf)
+        const float s = wave_sum(p.S == 0.0f ? 0.0f : p.S * pow2((p.m - high) * c));
+        all.S = (all.S == 0.0f ? 0.0f : all.S * pow2((all.m - high) * c)) + s;
+        all.m = high;
+    }
+    return all;
 }
 
 // A block's part of a row, elements [0, len) of z, in its threads' registers:
 // vectors i * B + thread, and up to VEC - 1 elements at the end one a thread.
-// What lies beyond is -inf.
+// A thread with no vector in the last round holds the last one once more, and
+// takes it as -inf.
 template <class T, int B>
 struct Part {
     static constexpr int VEC = Num<T>::VEC;
@@ -82,21 +106,33 @@ struct Part {
     u32x4 v[kKeep];
     float last;
     int vecs, tail, rounds;  // whole vectors, elements after them, rounds of B vectors
+    bool beyond;             // this thread has no vector in the last round
+    uint32_t off, off_last;  // the thread's elements within a round, and the last one
 
     __device__ __forceinline__ void extent(int64_t len) {
         vecs = int(len / VEC);
         tail = int(len % VEC);
         rounds = (vecs + B - 1) / B;
+        last = -INFINITY;
+        beyond = (rounds - 1) * B + int(threadIdx.x) >= vecs;
+        off = threadIdx.x * VEC;
+        off_last = beyond ? uint32_t(vecs - 1 - (rounds - 1) * B) * VEC : off;
+    }
+    __device__ __forceinline__ u32x4 vec_of(const T* z, int i) const {
+        return load_vec(z + i * B * VEC + (i == rounds - 1 ? off_last : off));
     }
     __device__ __forceinline__ void load(const T* z) {
-        constexpr uint32_t none = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
 #pragma unroll
-        for (int i = 0; i < kKeep; ++i) {
-            v[i] = u32x4{none, none, none, none};
-            if (i < rounds && i * B + int(threadIdx.x) < vecs)
-                v[i] = load_vec(z + (i * B + int(threadIdx.x)) * VEC);
-        }
+        for (int i = 0; i < kKeep; ++i)
+            if (i < rounds) v[i] = vec_of(z, i);
         last = int(threadIdx.x) < tail ? Num<T>::up(z[vecs * VEC + int(threadIdx.x)]) : -INFINITY;
+    }
+    // Within a loop over rows: what follows from the extent is worked out where
+    // it is used, not kept in registers for all rounds of the loop.
+    __device__ __forceinline__ void again() { asm volatile("" : "+s"(rounds)); }
+    __device__ __forceinline__ void get(int i, float* x) const {
+        constexpr uint32_t none = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+        Num<T>::unpack(i == rounds - 1 && beyond ? u32x4{none, none, none, none} : v[i], x);
     }
     template <class F>
     __device__ __forceinline__ void each(F&& f) const {
@@ -104,7 +140,7 @@ struct Part {
         for (int i = 0; i < kKeep; ++i) {
             if (i < rounds) {
                 float x[VEC];
-                Num<T>::unpack(v[i], x);
+                get(i, x);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f(x[e]);
             }
@@ -113,17 +149,32 @@ struct Part {
     }
     // This wavefront's sum (the same in every lane).
     __device__ __forceinline__ PartSum sum(float c) const {
-        float x[VEC];
-        Num<T>::unpack(v[0], x);
         float m = last;
+        if (rounds > 0) {
+            float x[VEC];
+            get(0, x);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) m = fmaxf(m, x[e]);
+            for (int e = 0; e < VEC; ++e) m = fmaxf(m, x[e]);
+        }
         m = wave_max(m);
         const float r = m * c;
         if (near_base(r)) {
             float S[2] = {0.0f, 0.0f};
             int n = 0;
-            each([&](float z) { S[n++ & 1] += pow2(fmaf(z, c, -r)); });
+            // (less +inf, what a thread holds once more adds 0; it is finite, or
+            // the sum is of no use anyway)
+            const float r_last = beyond ? INFINITY : r;
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i) {
+                if (i < rounds) {
+                    float x[VEC];
+                    Num<T>::unpack(v[i], x);
+                    const float ri = i == rounds - 1 ? r_last : r;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) S[n++ & 1] += pow2(fmaf(x[e], c, -ri));
+                }
+            }
+            S[0] += pow2(fmaf(last, c, -r));
             const float s = wave_sum(S[0] + S[1]);
             // (the largest of the sample adds 1)
             if (s >= 0.5f && s < 0x1p60f) return {m, s * pow2(-fmaf(m, c, -r))};
@@ -139,20 +190,42 @@ struct Part {
         s = wave_sum(s);
         return {s == 0.0f ? -INFINITY : base, s};
     }
-    // g = f(z).
+    // g = f(z), where g is given; then the registers take `next`, where that is.
     template <class F>
-    __device__ __forceinline__ void store_as(T* g, F&& f) const {
+    __device__ __forceinline__ void store_load(T* g, const T* next, F&& f) {
 #pragma unroll
         for (int i = 0; i < kKeep; ++i) {
-            if (i < rounds && i * B + int(threadIdx.x) < vecs) {
-                float x[VEC];
-                Num<T>::unpack(v[i], x);
+            if (i < rounds) {
+                if (g) {
+                    float x[VEC];
+                    Num<T>::unpack(v[i], x);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) x[e] = f(x[e]);
-                store_vec(g + (i * B + int(threadIdx.x)) * VEC, Num<T>::pack(x));
+                    for (int e = 0; e < VEC; ++e) x[e] = f(x[e]);
+                    if (i < rounds - 1 || !beyond)
+                        store_vec(g + (i * B + int(threadIdx.x)) * VEC, Num<T>::pack(x));
+                }
+                if (next) v[i] = vec_of(next, i);
             }
         }
+        if (int(threadIdx.x) < tail) {
+            if (g) g[vecs * VEC + int(threadIdx.x)] = Num<T>::down(f(last));
+            if (next) last = Num<T>::up(next[vecs * VEC + int(threadIdx.x)]);
+        }
+    }
+    // g = f(z) with z from memory.
+    template <class F>
+    __device__ __forceinline__ void store_from(T* g, const T* z, F&& f) const {
+        for (int i = int(threadIdx.x); i < vecs; i += B) {
+            float x[VEC];
+            Num<T>::unpack(load_vec(z + i * VEC), x);
+            for (int e = 0; e < VEC; ++e) x[e] = f(x[e]);
+            store_vec(g + i * VEC, Num<T>::pack(x));
+        }
         if (int(threadIdx.x) < tail) g[vecs * VEC + int(threadIdx.x)] = Num<T>::down(f(last));
+    }
+    // The thread that holds element j.
+    __device__ __forceinline__ int owner(int j) const {
+        return j < vecs * VEC ? (j / VEC) % B : j - vecs * VEC;
     }
     __device__ __forceinline__ void store_zero(T* g) const {
         for (int i = int(threadIdx.x); i < vecs; i += B) store_vec(g + i * VEC, u32x4{0, 0, 0, 0});
@@ -179,6 +252,7 @@ template <int B>
 struct Shared {
     PartSum part[B / 64];
     float term[B / 64];
+    int any[B / 64];
 };
 
 // Reads the entries; false if none is present (the same for every thread).
@@ -199,14 +273,16 @@ __device__ __forceinline__ bool read_entries(const DistillArgs& a, int64_t t, co
     return __syncthreads_or(any) != 0;
 }
 
-// The entries' p, by differences to their largest; the block's loss, without
-// its factors, in thread 0.
+// The entries' p, by differences to their largest; the row's loss, without its
+// factors.  By the whole block, or, if `alone`, by its first wavefront.
 template <int B>
 __device__ __forceinline__ float finish_entries(const DistillArgs& a, const Entries& e,
-                                                const Row& row, Shared<B>& sh) {
+                                                const Row& row, Shared<B>& sh, bool alone) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t step = alone ? 64 : B;
     auto all = [&](float v, bool max) {
         v = max ? wave_max(v) : wave_sum(v);
+        if (alone) return v;
         __syncthreads();
         if (lane == 0) sh.term[w] = v;
         __syncthreads();
@@ -215,14 +291,14 @@ __device__ __forceinline__ float finish_entries(const DistillArgs& a, const Entr
         return v;
     };
     float top = -INFINITY, sum = 0.0f, loss = 0.0f;
-    for (int64_t k = threadIdx.x; k < a.K; k += B)
+    for (int64_t k = threadIdx.x; k < a.K; k += step)
         if (e.id[k] >= 0) top = fmaxf(top, e.p[k]);
     top = all(top, true);
-    for (int64_t k = threadIdx.x; k < a.K; k += B)
+    for (int64_t k = threadIdx.x; k < a.K; k += step)
         if (e.id[k] >= 0) sum += pow2((e.p[k] - top) * a.c);
     sum = all(sum, false);
     const float ls = __builtin_amdgcn_logf(sum);
-    for (int64_t k = threadIdx.x; k < a.K; k += B) {
+    for (int64_t k = threadIdx.x; k < a.K; k += step) {
         if (e.id[k] < 0) continue;
         const float lp = (e.p[k] - top) * a.c - ls, p = pow2(lp);
         e.p[k] = p;
@@ -247,60 +323,125 @@ __device__ __forceinline__ void store_entries(const DistillArgs& a, const Entrie
     }
 }
 
+// The gradient of a part (z, to g; where g is given), and then the registers'
+// next contents.
 template <class T, int B>
-__device__ __forceinline__ void store_part_gradient(const Part<T, B>& part, const Row& row,
-                                                    float scale, T* g) {
+__device__ __forceinline__ void store_gradient(Part<T, B>& part, const Row& row, float scale,
+                                               const T* z, T* g, const T* next) {
     const float r = row.m * row.c;
-    if (near_base(r)) {
-        const float f = scale / row.S * pow2(-fmaf(row.m, row.c, -r));
-        part.store_as(g, [&](float z) { return f * pow2(fmaf(z, row.c, -r)); });
-    } else {
+    if (g && !near_base(r)) {  // rare: not worth registers
         const float f = scale / row.S;
-        part.store_as(g, [&](float z) { return f * pow2((z - row.m) * row.c); });
+        part.store_from(g, z, [&](float x) { return f * pow2((x - row.m) * row.c); });
+        g = nullptr;
     }
+    const float f = scale / row.S * pow2(-fmaf(row.m, row.c, -r));
+    part.store_load(g, next, [&](float x) { return f * pow2(fmaf(x, row.c, -r)); });
+}
+
+// What a thread reads ahead of a row: its weight, and the thread's entry.
+struct Ahead {
+    float weight;
+    int64_t id;
+    float s;
+};
+template <class S>
+__device__ __forceinline__ Ahead look_ahead(const DistillArgs& a, int64_t t, const S* teacher) {
+    Ahead h{0.0f, -1, 0.0f};
+    if (t >= a.T) return h;
+    h.weight = a.weights ? a.weights[t] : 1.0f;
+    if (h.weight != 0.0f && int64_t(threadIdx.x) < a.K) {
+        h.id = a.ids[t * a.ids_stride + threadIdx.x];
+        h.s = Num<S>::up(teacher[t * a.teacher_stride + threadIdx.x]);
+    }
+    return h;
 }
 
 template <class T, class S, int B>
-__global__ __launch_bounds__(B) void kept_kernel(DistillArgs a, const T* logits, const S* teacher,
+__global__ __launch_bounds__(B, 4) void kept_kernel(DistillArgs a, const T* logits, const S* teacher,
                                                  T* grad) {
     extern __shared__ char lds[];
     __shared__ Shared<B> sh;
+    __shared__ int32_t head[B];  // the entries whose elements a thread stores, chained
     const Entries e{reinterpret_cast<int32_t*>(lds), reinterpret_cast<float*>(lds) + a.K,
                     reinterpret_cast<float*>(lds) + 2 * a.K};
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t t = a.first + blockIdx.x;
-    const T* const z = logits + t * a.logits_stride;
-    T* const g = grad ? grad + t * a.grad_stride : nullptr;
-    const float weight = a.weights ? a.weights[t] : 1.0f;
+    int32_t* const chain = reinterpret_cast<int32_t*>(lds) + 3 * a.K;
+    // few entries are the first wavefront's, and the others go on meanwhile
+    const bool alone = a.K <= 64;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, tid = threadIdx.x;
     Part<T, B> part;
     part.extent(a.V);
-    Row row{};
-    bool live = weight != 0.0f;
-    if (live) {
-        part.load(z);
-        live = read_entries<S, B>(a, t, teacher, e, [&](int64_t, int64_t id) { return Num<T>::up(z[id]); });
-    }
-    if (live) {
-        const PartSum own = part.sum(a.c);
-        if (lane == 0) sh.part[w] = own;
+    Ahead now{0.0f, -1, 0.0f};
+    // (the first round only loads the first row)
+    for (int64_t t = int64_t(blockIdx.x) - gridDim.x; t < a.T; t += gridDim.x) {
+        part.again();
+        const T* const z = logits + t * a.logits_stride;
+        const int64_t tn = t + gridDim.x;
+        T* g = grad && t >= 0 ? grad + t * a.grad_stride : nullptr;
+        const float weight = now.weight, scale = weight * a.temperature;
+        const Ahead was = now;
+        now = look_ahead(a, tn, teacher);
+        Row row{};
+        bool live = false;
+        if (weight != 0.0f) {
+            // the thread's first entry; the student's logit there arrives during the sum
+            float zs = 0.0f;
+            const bool is0 = was.id >= 0 && was.id < a.V && was.s != -INFINITY;
+            if (is0) zs = Num<T>::up(z[was.id]);
+            const PartSum own = part.sum(a.c);
+            if (lane == 0) sh.part[w] = own;
+            head[tid] = -1;
+            int any = is0;
+            if (tid < a.K) {
+                e.id[tid] = is0 ? int32_t(was.id) : -1;
+                e.p[tid] = was.s;
+                e.z[tid] = zs;
+            }
+            for (int64_t k = tid + B; k < a.K; k += B) {
+                const int64_t id = a.ids[t * a.ids_stride + k];
+                const float s = Num<S>::up(teacher[t * a.teacher_stride + k]);
+                const bool is = id >= 0 && id < a.V && s != -INFINITY;
+                e.id[k] = is ? int32_t(id) : -1;
+                e.p[k] = s;
+                e.z[k] = is ? Num<T>::up(z[id]) : 0.0f;
+                any |= is;
+            }
+            const uint64_t some = __ballot(any);
+            if (lane == 0) sh.any[w] = some != 0;
+            __syncthreads();
+            const PartSum s = join(sh.part, B / 64, a.c);
+            row = Row{s.m, s.S, a.c};
+            live = s.S != 0.0f && __ballot(lane < B / 64 ? sh.any[lane % (B / 64)] : 0) != 0;
+        }
+        if (live) {
+            if (!alone || w == 0) {
+                const float loss = finish_entries<B>(a, e, row, sh, alone);
+                if (tid == 0) a.loss[t] = scale * a.temperature * loss;
+                if (!alone) __syncthreads();
+                for (int64_t k = tid; g && k < a.K; k += alone ? 64 : B) {
+                    const int32_t id = e.id[k];
+                    if (id < 0) continue;
+                    // less the p of every entry with this id: each stores the same
+                    float p = 0.0f;
+                    for (int64_t j = 0; j < a.K; ++j)
+                        if (e.id[j] == id) p += e.p[j];
+                    e.z[k] = scale * (pow2(row.log2q(e.z[k])) - p);
+                    chain[k] = atomicExch(&head[part.owner(id)], int32_t(k));
+                }
+            }
+        } else if (t >= 0) {
+            if (tid == 0) a.loss[t] = 0.0f;
+            if (g) part.store_zero(g);
+        }
+        store_gradient(part, row, scale, z, live ? g : nullptr,
+                       now.weight != 0.0f ? logits + tn * a.logits_stride : nullptr);
         __syncthreads();
-        PartSum s = sh.part[0];
-        for (int i = 1; i < B / 64; ++i) s.add(sh.part[i], a.c);
-        row = Row{s.m, s.S, a.c};
-        live = s.S != 0.0f;
+        if (live && g) {
+            // The entries' elements once more, each by the thread that has just
+            // stored what lies around it, so that these stores come second.
+            for (int32_t k = head[tid]; k >= 0; k = chain[k]) g[e.id[k]] = Num<T>::down(e.z[k]);
+        }
+        __syncthreads();  // LDS is free again
     }
-    if (!live) {
-        if (threadIdx.x == 0) a.loss[t] = 0.0f;
-        if (g) part.store_zero(g);
-        return;
-    }
-    const float loss = finish_entries<B>(a, e, row, sh);
-    if (threadIdx.x == 0) a.loss[t] = weight * a.temperature * a.temperature * loss;
-    if (!g) return;
-    const float scale = weight * a.temperature;
-    store_part_gradient(part, row, scale, g);
-    __syncthreads();  // the entries' elements are written once more, after these
-    store_entries<T, B>(a, e, row, scale, 0, a.V, g);
 }
 
 // Split form, first launch: the parts' sums, and the student's logits at the
@@ -321,13 +462,11 @@ __global__ __launch_bounds__(B) void parts_kernel(DistillArgs a, const T* logits
     Part<T, B> part;
     part.extent(a.V - j * a.part < a.part ? a.V - j * a.part : a.part);
     part.load(z + j * a.part);
-    PartSum s = part.sum(a.c);
-    if (lane == 0) sh.part[w] = s;
+    const PartSum own = part.sum(a.c);
+    if (lane == 0) sh.part[w] = own;
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    s = sh.part[0];
-    for (int n = 1; n < B / 64; ++n) s.add(sh.part[n], a.c);
-    a.sums[blockIdx.x] = s;
+    const PartSum s = join(sh.part, B / 64, a.c);
+    if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
 }
 
 // Split form, second launch: every part's block joins its row's sums; the
@@ -339,7 +478,6 @@ __global__ __launch_bounds__(B) void split_kernel(DistillArgs a, const T* logits
     __shared__ Shared<B> sh;
     const Entries e{reinterpret_cast<int32_t*>(lds), reinterpret_cast<float*>(lds) + a.K,
                     reinterpret_cast<float*>(lds) + 2 * a.K};
-    const int lane = threadIdx.x & 63;
     const int64_t blocks = grad ? a.parts : 1;  // a row's
     const int64_t i = blockIdx.x / blocks, t = a.first + i, j = blockIdx.x % blocks;
     const int64_t lo = j * a.part, hi = a.V - lo < a.part ? a.V : lo + a.part;
@@ -355,10 +493,7 @@ __global__ __launch_bounds__(B) void split_kernel(DistillArgs a, const T* logits
         live = read_entries<S, B>(a, t, teacher, e, [&](int64_t k, int64_t) { return a.at[i * a.K + k]; });
     }
     if (live) {
-        const PartSum* const sums = a.sums + i * a.parts;
-        PartSum s{-INFINITY, 0.0f};
-        for (int64_t n = lane; n < a.parts; n += 64) s.add(sums[n], a.c);
-        for (int d = 1; d < 64; d *= 2) s.add({__shfl_xor(s.m, d), __shfl_xor(s.S, d)}, a.c);
+        const PartSum s = join(a.sums + i * a.parts, a.parts, a.c);
         row = Row{s.m, s.S, a.c};
         live = s.S != 0.0f;
     }
@@ -367,11 +502,11 @@ __global__ __launch_bounds__(B) void split_kernel(DistillArgs a, const T* logits
         if (g) part.store_zero(g + lo);
         return;
     }
-    const float loss = finish_entries<B>(a, e, row, sh);
+    const float loss = finish_entries<B>(a, e, row, sh, false);
     if (threadIdx.x == 0 && j == 0) a.loss[t] = weight * a.temperature * a.temperature * loss;
     if (!g) return;
     const float scale = weight * a.temperature;
-    store_part_gradient(part, row, scale, g + lo);
+    store_gradient(part, row, scale, z, g + lo, static_cast<const T*>(nullptr));
     __syncthreads();  // the entries' elements are written once more, after these
     store_entries<T, B>(a, e, row, scale, lo, hi, g);
 }
@@ -415,11 +550,11 @@ Space space_of(const Form& f, int64_t K) {
 }
 
 template <class T, class S, int B>
-void launch_kept(DistillArgs a, const T* z, const S* teacher, T* grad, hipStream_t st) {
-    constexpr int64_t kRows = int64_t(1) << 21;  // a launch's work-items are counted in 32 bits
-    for (a.first = 0; a.first < a.T; a.first += kRows)
-        hipLaunchKernelGGL((kept_kernel<T, S, B>), dim3(unsigned(std::min(kRows, a.T - a.first))),
-                           dim3(B), size_t(12 * a.K), st, a, z, teacher, grad);
+void launch_kept(const DistillArgs& a, const T* z, const S* teacher, T* grad, hipStream_t st) {
+    // as many blocks as the 256 CUs hold at 16 wavefronts each
+    const int64_t blocks = std::min<int64_t>(a.T, 256 * 1024 / B);
+    hipLaunchKernelGGL((kept_kernel<T, S, B>), dim3(unsigned(blocks)), dim3(B), size_t(16 * a.K),
+                       st, a, z, teacher, grad);
 }
 
 template <class T, class S>

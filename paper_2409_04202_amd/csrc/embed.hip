@@ -178,9 +178,10 @@ __global__ __launch_bounds__(256) void sort_move_kernel(SortSrc s, int shift,
 
 // A run: `n` sorted places from `start`, of row v; n < 0: the only run of its
 // row, -n places.
-struct Run {
+struct alignas(16) Run {
     uint32_t v, start;
     int32_t n;
+    uint32_t tok;  // its first token
 };
 // A row of more than one run: its sorted places.
 struct LongRow {
@@ -208,8 +209,8 @@ __device__ __forceinline__ int64_t key_bound(const Key& key, int64_t lo, int64_t
 
 // Lists the run that starts at sorted place i, and the long row; their order
 // in the lists decides nothing.
-template <class Key, class Next>
-__device__ __forceinline__ void list_run(const Key& key, int64_t i, int64_t T, int64_t V,
+template <class Key, class Tok, class Next>
+__device__ __forceinline__ void list_run(const Key& key, const Tok& tok, int64_t i, int64_t T, int64_t V,
                                          const RunList& l, const Next& next) {
     const uint32_t v = key(i);
     if (v >= V) return;
@@ -222,7 +223,7 @@ __device__ __forceinline__ void list_run(const Key& key, int64_t i, int64_t T, i
     const int64_t end = key(cap - 1) == v ? cap : key_bound(key, i, cap, v, false);
     const int n = int(end - i);
     const bool more = end < T && key(end) == v;
-    l.runs[next(0)] = Run{v, uint32_t(i), first && !more ? -n : n};
+    l.runs[next(0)] = Run{v, uint32_t(i), first && !more ? -n : n, tok(i)};
     if (first && more)
         l.rows[next(1)] = LongRow{v, uint32_t(i), uint32_t(key_bound(key, end, T, v, false))};
 }
@@ -330,27 +331,34 @@ __device__ __forceinline__ void small_sort(SmallSort& s, const int64_t* ids, int
     if (threadIdx.x < 2) s.count[threadIdx.x] = 0;
     __syncthreads();
     const auto key = [&](int64_t i) { return s.key[i]; };
+    const auto at = [&](int64_t i) { return uint32_t(s.tok[i]); };
     for (int i = threadIdx.x; i < T; i += 1024) {
         tok[i] = s.tok[i];
-        list_run(key, i, T, V, l, [&](int which) { return atomicAdd(&s.count[which], 1u); });
+        list_run(key, at, i, T, V, l, [&](int which) { return atomicAdd(&s.count[which], 1u); });
     }
     __syncthreads();
     if (threadIdx.x < 2) l.count[threadIdx.x] = s.count[threadIdx.x];
 }
 
-// Zeros over a matrix, by `blocks` blocks of which this is one, a wavefront a
-// slice of 64 vectors of a row.
+// Zeros over a matrix, by `blocks` blocks of which this is one, a wavefront
+// kZeroVecs slices of 64 vectors of a row at a time.
+constexpr int kZeroVecs = 8;
+
 template <class T, int BLOCK>
 __device__ __forceinline__ void zero_rows(T* m, uint32_t rows, int64_t cols, int64_t stride,
                                           uint32_t block, uint32_t blocks) {
-    constexpr int VEC = Num<T>::VEC, WAVES = BLOCK / 64;
-    const uint32_t slices = uint32_t((cols + 64 * VEC - 1) / (64 * VEC)), units = rows * slices;
+    constexpr int VEC = Num<T>::VEC, WAVES = BLOCK / 64, UNIT = kZeroVecs * 64 * VEC;
+    const uint32_t per = uint32_t((cols + UNIT - 1) / UNIT), units = rows * per;
     const uint32_t step = blocks * WAVES;
     for (uint32_t u = block * WAVES + wave_id(); u < units; u += step) {
-        const int64_t at = int64_t(u % slices) * 64 * VEC + int64_t(threadIdx.x & 63) * VEC;
-        T* dst = m + int64_t(u / slices) * stride + at;
-        if (cols - at >= VEC) store_vec(dst, u32x4{0, 0, 0, 0});
-        else if (cols > at) store_part(dst, u32x4{0, 0, 0, 0}, int(cols - at));
+        const int64_t at = int64_t(u % per) * UNIT + int64_t(threadIdx.x & 63) * VEC;
+        T* const dst = m + int64_t(u / per) * stride + at;
+#pragma unroll
+        for (int i = 0; i < kZeroVecs; ++i) {
+            const int64_t left = cols - at - i * 64 * VEC;
+            if (left >= VEC) store_vec(dst + i * 64 * VEC, u32x4{0, 0, 0, 0});
+            else if (left > 0) store_part(dst + i * 64 * VEC, u32x4{0, 0, 0, 0}, int(left));
+        }
         if (units - u <= step) break;  // (u + step may pass 32 bits)
     }
 }
@@ -358,14 +366,14 @@ __device__ __forceinline__ void zero_rows(T* m, uint32_t rows, int64_t cols, int
 // Block 0 sorts; the others, if any, fill the table with zeros.
 template <class T>
 __global__ __launch_bounds__(1024) void sort_zero_kernel(const int64_t* ids, int64_t tokens,
-                                                         int64_t V, int64_t D, uint32_t* tok,
-                                                         RunList l, T* dtable,
-                                                         int64_t dtable_stride) {
+                                                         int64_t V, uint32_t* tok, RunList l,
+                                                         T* m, int64_t rows, int64_t cols,
+                                                         int64_t stride) {
     extern __shared__ char lds[];
     if (blockIdx.x == 0)
         small_sort(*reinterpret_cast<SmallSort*>(lds), ids, int(tokens), V, tok, l);
     else
-        zero_rows<T, 1024>(dtable, uint32_t(V), D, dtable_stride, blockIdx.x - 1, gridDim.x - 1);
+        zero_rows<T, 1024>(m, uint32_t(rows), cols, stride, blockIdx.x - 1, gridDim.x - 1);
 }
 
 template <class T>
@@ -375,12 +383,13 @@ __global__ __launch_bounds__(256) void zero_kernel(T* m, int64_t rows, int64_t c
 }
 
 // More tokens: the list of runs from the sorted keys in memory.
-__global__ __launch_bounds__(256) void list_kernel(const uint32_t* keys, int64_t tokens, int64_t V,
-                                                   RunList l) {
+__global__ __launch_bounds__(256) void list_kernel(const uint32_t* keys, const uint32_t* tok,
+                                                   int64_t tokens, int64_t V, RunList l) {
     const auto key = [&](int64_t i) { return keys[i]; };
+    const auto at = [&](int64_t i) { return tok[i]; };
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < tokens;
          i += int64_t(gridDim.x) * 256)
-        list_run(key, i, tokens, V, l, [&](int which) { return atomicAdd(&l.count[which], 1u); });
+        list_run(key, at, i, tokens, V, l, [&](int which) { return atomicAdd(&l.count[which], 1u); });
 }
 
 // --------------------------------------------------------------- fold
@@ -427,68 +436,90 @@ __device__ __forceinline__ void finish_row(const FoldArgs& a, T* dtable, uint32_
     }
 }
 
-// The sum of N more rows, their loads in flight together; `row(i)` is row i.
-template <class T, int N, class Row>
-__device__ __forceinline__ void add_rows(float* sum, int left, Row&& row) {
+// The sums of N more rows over S slices of 64 vectors, their loads in flight
+// together; `row(i)` is row i, `left` what the matrix has from the lane's first
+// element on.
+template <class T, int N, int S, class Row>
+__device__ __forceinline__ void add_rows(float (*sum)[Num<T>::VEC], int64_t left, Row&& row) {
     constexpr int VEC = Num<T>::VEC;
-    u32x4 x[N];
+    u32x4 x[N][S];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const T* src = row(i);
-        x[i] = u32x4{0, 0, 0, 0};
-        if (left >= VEC) x[i] = load_vec(src);
-        else if (left > 0) x[i] = load_part(src, left);
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int64_t n = left - s * 64 * VEC;
+            x[i][s] = u32x4{0, 0, 0, 0};
+            if (n >= VEC) x[i][s] = load_vec(src + s * 64 * VEC);
+            else if (n > 0) x[i][s] = load_part(src + s * 64 * VEC, int(n));
+        }
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float f[VEC];
-        Num<T>::unpack(x[i], f);
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] += f[e];
-    }
+        for (int s = 0; s < S; ++s) {
+            float f[VEC];
+            Num<T>::unpack(x[i][s], f);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[s][e] += f[e];
+        }
 }
-// The same for n rows, n a scalar.
-template <class T, class Row>
-__device__ __forceinline__ void add_all(float* sum, int left, int n, Row&& row) {
+// The same for n rows, n a scalar, at most kFoldLoads vectors in flight.
+constexpr int kFoldLoads = 8;
+template <class T, int S, class Row>
+__device__ __forceinline__ void add_all(float (*sum)[Num<T>::VEC], int64_t left, int n, Row&& row) {
+    constexpr int N = kFoldLoads / S;
     int j = 0;
     const auto at = [&](int i) { return row(j + i); };
-    for (; j + 8 <= n; j += 8) add_rows<T, 8>(sum, left, at);
-    if (n & 4) {
-        add_rows<T, 4>(sum, left, at);
-        j += 4;
-    }
-    if (n & 2) {
-        add_rows<T, 2>(sum, left, at);
-        j += 2;
-    }
-    if (n & 1) add_rows<T, 1>(sum, left, at);
+    for (; j + N <= n; j += N) add_rows<T, N, S>(sum, left, at);
+    if constexpr (N > 4)
+        if ((n - j) & 4) {
+            add_rows<T, 4, S>(sum, left, at);
+            j += 4;
+        }
+    if constexpr (N > 2)
+        if ((n - j) & 2) {
+            add_rows<T, 2, S>(sum, left, at);
+            j += 2;
+        }
+    if ((n - j) & 1) add_rows<T, 1, S>(sum, left, at);
 }
 
-// One wavefront a (run, slice of 64 vectors of the row).
-template <class T>
+// One wavefront a (run, S slices of 64 vectors of the row).
+template <class T, int S>
 __global__ __launch_bounds__(256) void fold_kernel(FoldArgs a, const T* dout, T* dtable) {
-    constexpr int VEC = Num<T>::VEC;
+    constexpr int VEC = Num<T>::VEC, UNIT = S * 64 * VEC;
     const int lane = threadIdx.x & 63;
-    const uint32_t slices = uint32_t((a.D + 64 * VEC - 1) / (64 * VEC));
-    const uint32_t units = a.l.count[0] * slices, step = gridDim.x * 4;
+    const uint32_t per = uint32_t((a.D + UNIT - 1) / UNIT);
+    const uint32_t units = a.l.count[0] * per, step = gridDim.x * 4;
     for (uint32_t u = blockIdx.x * 4 + wave_id(); u < units; u += step) {
-        const Run* const r = a.l.runs + u / slices;
-        const uint32_t v = scalar(r->v), start = scalar(r->start);
-        const int size = int(scalar(uint32_t(r->n))), n = size < 0 ? -size : size;
-        const int64_t at = int64_t(u % slices) * 64 * VEC + int64_t(lane) * VEC;
-        const int64_t rest = a.D - at;  // of the row, from the lane's vector on
-        const int left = int(rest < VEC ? rest : VEC);
-        const uint32_t mine = lane < n ? a.tok[start + lane] : 0;
-        float sum[VEC] = {};
-        add_all<T>(sum, left, n, [&](int i) {
-            return dout + int64_t(uint32_t(__builtin_amdgcn_readlane(int(mine), i))) * a.dout_stride + at;
-        });
-        if (left > 0 && size < 0) finish_row(a, dtable, v, at, sum);
-        if (left > 0 && size > 0) {
-            float* dst = (n == kRun ? a.full + int64_t(start / kRun) * a.pitch
-                                    : a.tail + int64_t((start - kRun) / kRun) * a.pitch) + at;
+        const Run run = a.l.runs[u / per];
+        const uint32_t v = scalar(run.v), start = scalar(run.start);
+        const int size = int(scalar(uint32_t(run.n))), n = size < 0 ? -size : size;
+        const int64_t at = int64_t(u % per) * UNIT + int64_t(lane) * VEC;
+        const int64_t left = a.D - at;  // of the row, from the lane's first element on
+        float sum[S][VEC] = {};
+        if (n == 1) {
+            const T* const src = dout + int64_t(scalar(run.tok)) * a.dout_stride + at;
+            add_rows<T, 1, S>(sum, left, [&](int) { return src; });
+        } else {
+            const uint32_t mine = lane < n ? a.tok[start + lane] : 0;
+            add_all<T, S>(sum, left, n, [&](int i) {
+                return dout + int64_t(uint32_t(__builtin_amdgcn_readlane(int(mine), i))) * a.dout_stride + at;
+            });
+        }
+        float* const part = (n == kRun ? a.full + int64_t(start / kRun) * a.pitch
+                                       : a.tail + int64_t((start - kRun) / kRun) * a.pitch) + at;
 #pragma unroll
-            for (int e = 0; e < VEC; e += 4) store_vec(dst + e, Num<float>::pack(sum + e));
+        for (int s = 0; s < S; ++s) {
+            if (left <= s * 64 * VEC) continue;
+            if (size < 0) {
+                finish_row(a, dtable, v, at + s * 64 * VEC, sum[s]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; e += 4)
+                    store_vec(part + s * 64 * VEC + e, Num<float>::pack(sum[s] + e));
+            }
         }
         if (units - u <= step) break;  // (u + step may pass 32 bits)
     }
@@ -504,16 +535,16 @@ __global__ __launch_bounds__(256) void join_kernel(FoldArgs a, T* dtable) {
         const LongRow* const r = a.l.rows + u / slices;
         const uint32_t v = scalar(r->v), start = scalar(r->start), end = scalar(r->end);
         const int64_t at = int64_t(u % slices) * 64 * W + int64_t(threadIdx.x & 63) * W;
-        const int left = at < a.D ? W : 0;  // (the sums' rows are padded)
+        const int64_t left = at < a.D ? W : 0;  // (the sums' rows are padded)
         const int full = int((end - start) / kRun), rest = int((end - start) % kRun);
-        float sum[W] = {};
+        float sum[1][W] = {};
         const float* const src = a.full + int64_t(start / kRun) * a.pitch + at;
-        add_all<float>(sum, left, full, [&](int i) { return src + i * a.pitch; });
+        add_all<float, 1>(sum, left, full, [&](int i) { return src + i * a.pitch; });
         if (rest) {
             const float* const last = a.tail + int64_t((end - rest - kRun) / kRun) * a.pitch + at;
-            add_rows<float, 1>(sum, left, [&](int) { return last; });
+            add_rows<float, 1, 1>(sum, left, [&](int) { return last; });
         }
-        if (left) finish_row<T, W>(a, dtable, v, at, sum);
+        if (left) finish_row<T, W>(a, dtable, v, at, sum[0]);
         if (units - u <= step) break;
     }
 }
@@ -570,12 +601,14 @@ ar_status run_grad(int64_t V, int64_t D, int64_t rows, const void* dout, int64_t
                    const int64_t* ids, float scale, int32_t accumulate, void* dtable,
                    int64_t dtable_stride, char* ws, hipStream_t st) {
     T* const out = static_cast<T*>(dtable);
-    const int64_t slices = ceil_div(D, 64 * Num<T>::VEC);
-    const int64_t zeros = accumulate ? 0 : V * slices;  // wavefronts' stores
+    // adjacent rows are zeroed as one
+    const bool flat = dtable_stride == D;
+    const int64_t zr = flat ? 1 : V, zc = flat ? V * D : D;
+    const int64_t zeros = accumulate ? 0 : zr * ceil_div(zc, kZeroVecs * 64 * Num<T>::VEC);
     if (rows == 0) {
         if (zeros)
             hipLaunchKernelGGL((zero_kernel<T>), dim3(grid_of(ceil_div(zeros, 4))), dim3(256), 0,
-                               st, out, V, D, dtable_stride);
+                               st, out, zr, zc, dtable_stride);
         return launch_status("embedding gradient");
     }
     const GradSpace g = grad_space(D, rows);
@@ -589,11 +622,11 @@ ar_status run_grad(int64_t V, int64_t D, int64_t rows, const void* dout, int64_t
     if (rows <= kSmallSort) {
         const unsigned blocks = unsigned(std::min<int64_t>(ceil_div(zeros, 16), kZeroBlocks));
         hipLaunchKernelGGL((sort_zero_kernel<T>), dim3(1 + blocks), dim3(1024), sizeof(SmallSort),
-                           st, ids, rows, V, D, tok[0], l, out, dtable_stride);
+                           st, ids, rows, V, tok[0], l, out, zr, zc, dtable_stride);
     } else {
         if (zeros)
             hipLaunchKernelGGL((zero_kernel<T>), dim3(grid_of(ceil_div(zeros, 4))), dim3(256), 0,
-                               st, out, V, D, dtable_stride);
+                               st, out, zr, zc, dtable_stride);
         uint32_t* hist = reinterpret_cast<uint32_t*>(ws + g.hist);
         SortSrc src{ids, nullptr, nullptr, V, rows};
         int to = 0;
@@ -607,7 +640,7 @@ ar_status run_grad(int64_t V, int64_t D, int64_t rows, const void* dout, int64_t
             src = SortSrc{nullptr, key[to], tok[to], V, rows};
         }
         hipLaunchKernelGGL(list_kernel, dim3(grid_of(ceil_div(rows, 256))), dim3(256), 0, st,
-                           src.key, rows, V, l);
+                           src.key, src.tok, rows, V, l);
         sorted = src.tok;
     }
     const FoldArgs a{l, sorted, D, dout_stride, dtable_stride, scale, accumulate,
@@ -616,8 +649,14 @@ ar_status run_grad(int64_t V, int64_t D, int64_t rows, const void* dout, int64_t
     const auto grid = [](int64_t units) {  // at most so many wavefronts, which then loop
         return dim3(unsigned(std::min<int64_t>(ceil_div(units, 4), kFoldBlocks)));
     };
-    hipLaunchKernelGGL((fold_kernel<T>), grid(rows * slices), dim3(256), 0, st, a,
-                       static_cast<const T*>(dout), out);
+    // two slices a wavefront where a row has them: twice the loads in flight for
+    // the rows of one token, most of all
+    if (D > 64 * Num<T>::VEC)
+        hipLaunchKernelGGL((fold_kernel<T, 2>), grid(rows * ceil_div(D, 128 * Num<T>::VEC)), dim3(256),
+                           0, st, a, static_cast<const T*>(dout), out);
+    else
+        hipLaunchKernelGGL((fold_kernel<T, 1>), grid(rows), dim3(256), 0, st, a,
+                           static_cast<const T*>(dout), out);
     if (rows > kRun)
         hipLaunchKernelGGL((join_kernel<T>), grid(ceil_div(rows, kRun) * ceil_div(D, 256)), dim3(256),
                            0, st, a, out);
