@@ -27,32 +27,43 @@ struct ForwardArgs {
     int act;
 };
 
+// h, and the saved factors where they are wanted, of a tile; or, split along k,
+// the tile's sums of g and of u.
 template <class T, int BR, int BC, int WR, int WC, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, ForwardArgs a,
                                                                Side<T> x, Side<T> w, T* h, T* sg,
                                                                T* su) {
     using P = Tile<T, BR, BC, WR, WC, true, true, true, DIRECT>;
     using S = Store<1>;
-    static_assert(P::LDS >= WR * WC * S::BYTES, "");
-    __shared__ __attribute__((aligned(16))) char lds[P::LDS];
-    int64_t rt, ct;
-    if (!tile_of(p, blockIdx.x, &rt, &ct)) return;
+    constexpr int LDS = P::LDS > WR * WC * S::BYTES ? P::LDS : WR * WC * S::BYTES;
+    __shared__ __attribute__((aligned(16))) char lds[LDS];
+    const int64_t tiles = p.row_tiles * p.col_tiles;
+    int64_t t, rt, ct;
+    if (!tile_of(p, tiles * p.splits, blockIdx.x, &t)) return;
+    const int split = int(t / tiles);
+    place_of(p, t % tiles, &rt, &ct);
     f32x16 acc[P::SR][2] = {};
-    P::run(p, x, w, rt * BR, ct * (BC / 2), (AR_LDS char*)lds, acc);
+    P::run(p, x, w, rt * BR, ct * (BC / 2), split, (AR_LDS char*)lds, acc);
     const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
     AR_LDS float* const part = (AR_LDS float*)((AR_LDS char*)lds + wave * S::BYTES);
 #pragma unroll
     for (int i = 0; i < P::SR; ++i) {
         const int64_t r0 = rt * BR + (wr * P::SR + i) * 32, c0 = ct * (BC / 2) + wc * 32;
+        auto pass = [&](auto* out, int64_t stride, auto f) {
+            S::fill(part, f);
+            wave_sync();
+            S::store(part, out, stride, r0, p.rows, c0, p.cols, false, 0, 0, 0, 0);
+            wave_sync();
+        };
+        if (p.splits > 1) {
+            float* const to = p.part + int64_t(split) * 2 * p.rows * p.pitch;
+            pass(to, p.pitch, [&](int, int e) { return acc[i][0][e]; });
+            pass(to + p.rows * p.pitch, p.pitch, [&](int, int e) { return acc[i][1][e]; });
+            continue;
+        }
         float value[16], slope[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) activate(a.act, acc[i][0][e], &value[e], &slope[e]);
-        auto pass = [&](T* out, int64_t stride, auto f) {
-            S::fill(part, f);
-            wave_sync();
-            S::store(part, out, stride, r0, p.rows, c0, p.cols, false);
-            wave_sync();
-        };
         pass(h, a.h_stride, [&](int, int e) { return value[e] * acc[i][1][e]; });
         if (sg) {
             pass(sg, a.saved_stride, [&](int, int e) { return slope[e] * acc[i][1][e]; });
@@ -61,103 +72,267 @@ __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, F
     }
 }
 
-// dg = dh * saved_gate and du = dh * saved_up.
+// The sums of a product split along k, added in order, to its output.
+template <class T>
+__global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, ForwardArgs a, T* h,
+                                                           T* sg, T* su) {
+    const int64_t per = p.pitch / 4, step = int64_t(gridDim.x) * 256, one = p.rows * p.pitch;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < p.rows * per; i += step) {
+        const int64_t r = i / per, c = i % per * 4;
+        float g[4] = {}, u[4] = {};
+        for (int s = 0; s < p.splits; ++s) {
+            float x[4], y[4];
+            Num<float>::unpack(load_vec(p.part + 2 * s * one + r * p.pitch + c), x);
+            Num<float>::unpack(load_vec(p.part + (2 * s + 1) * one + r * p.pitch + c), y);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                g[e] += x[e];
+                u[e] += y[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (c + e >= p.cols) continue;
+            float value, slope;
+            activate(a.act, g[e], &value, &slope);
+            h[r * a.h_stride + c + e] = Num<T>::down(value * u[e]);
+            if (sg) {
+                sg[r * a.saved_stride + c + e] = Num<T>::down(slope * u[e]);
+                su[r * a.saved_stride + c + e] = Num<T>::down(value);
+            }
+        }
+    }
+}
+
+// dg = dh * saved_gate and du = dh * saved_up, a vector a lane.  Bound by
+// memory: five matrices pass once.
 template <class T>
 __global__ __launch_bounds__(256) void factors_kernel(int64_t M, int64_t F, const T* dh,
                                                       int64_t dh_stride, const T* sg, const T* su,
                                                       int64_t saved_stride, T* dg, T* du,
                                                       int64_t stride) {
-    for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < M * F;
-         e += int64_t(gridDim.x) * 256) {
-        const int64_t r = e / F, c = e % F;
-        const float d = Num<T>::up(dh[r * dh_stride + c]);
-        dg[r * stride + c] = Num<T>::down(d * Num<T>::up(sg[r * saved_stride + c]));
-        du[r * stride + c] = Num<T>::down(d * Num<T>::up(su[r * saved_stride + c]));
+    constexpr int VEC = Num<T>::VEC;
+    const int64_t per = (F + VEC - 1) / VEC, step = int64_t(gridDim.x) * 256;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < M * per; i += step) {
+        const int64_t r = i / per, c = i % per * VEC;
+        const int n = int(F - c < VEC ? F - c : VEC);
+        const T *pd = dh + r * dh_stride + c, *pg = sg + r * saved_stride + c,
+                *pu = su + r * saved_stride + c;
+        float d[VEC], g[VEC], u[VEC];
+        Num<T>::unpack(n == VEC ? load_vec(pd) : load_part(pd, n), d);
+        Num<T>::unpack(n == VEC ? load_vec(pg) : load_part(pg, n), g);
+        Num<T>::unpack(n == VEC ? load_vec(pu) : load_part(pu, n), u);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            g[e] *= d[e];
+            u[e] *= d[e];
+        }
+        // (their rows are whole vectors: the last one's rest is zero)
+        store_vec(dg + r * stride + c, Num<T>::pack(g));
+        store_vec(du + r * stride + c, Num<T>::pack(u));
     }
 }
 
-// C = R L^T, or C += with accumulate.
+// One or two products C = R L^T of one shape (the two weight gradients have
+// row operands of their own), or C += with accumulate.
+template <class T>
+struct Products {
+    Side<T> r[2], l;
+    T* out[2];
+    int64_t stride;
+    int count, accumulate;
+};
+
 template <class T, int BR, int BC, int WR, int WC, bool RKC, bool DIRECT>
-__global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductShape p, Side<T> r, Side<T> l,
-                                                               int accumulate, T* out,
-                                                               int64_t stride) {
+__global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductShape p, Products<T> a) {
     using P = Tile<T, BR, BC, WR, WC, RKC, false, false, DIRECT>;
     using S = Store<P::SC>;
-    static_assert(P::LDS >= WR * WC * S::BYTES, "");
-    __shared__ __attribute__((aligned(16))) char lds[P::LDS];
-    int64_t rt, ct;
-    if (!tile_of(p, blockIdx.x, &rt, &ct)) return;
+    constexpr int LDS = P::LDS > WR * WC * S::BYTES ? P::LDS : WR * WC * S::BYTES;
+    __shared__ __attribute__((aligned(16))) char lds[LDS];
+    constexpr int VEC = Num<T>::VEC;
+    const int64_t tiles = p.row_tiles * p.col_tiles;
+    int64_t t, rt, ct;
+    if (!tile_of(p, tiles * p.splits * a.count, blockIdx.x, &t)) return;
+    const bool second = t >= tiles * p.splits;
+    if (second) t -= tiles * p.splits;
+    const int split = int(t / tiles);
+    place_of(p, t % tiles, &rt, &ct);
     f32x16 acc[P::SR][P::SC] = {};
-    P::run(p, r, l, rt * BR, ct * BC, (AR_LDS char*)lds, acc);
+    P::run(p, second ? a.r[1] : a.r[0], a.l, rt * BR, ct * BC, split, (AR_LDS char*)lds, acc);
     const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
     AR_LDS float* const part = (AR_LDS float*)((AR_LDS char*)lds + wave * S::BYTES);
+    const int rshift = DIRECT && !RKC ? int((VEC - p.rows % VEC) % VEC) : 0,
+              cshift = DIRECT ? int((VEC - p.cols % VEC) % VEC) : 0;
 #pragma unroll
     for (int i = 0; i < P::SR; ++i) {
         S::fill(part, [&](int j, int e) { return acc[i][j][e]; });
         wave_sync();
-        S::store(part, out, stride, rt * BR + (wr * P::SR + i) * 32, p.rows,
-                 ct * BC + wc * P::SC * 32, p.cols, accumulate);
+        const int64_t r0 = rt * BR + (wr * P::SR + i) * 32, c0 = ct * BC + wc * P::SC * 32;
+        if (p.splits > 1)
+            S::store(part, p.part + (int64_t(split) * a.count + second) * p.rows * p.pitch, p.pitch,
+                     r0, p.rows, c0, p.cols, false, VEC, rshift, VEC, cshift);
+        else
+            S::store(part, second ? a.out[1] : a.out[0], a.stride, r0, p.rows, c0, p.cols,
+                     a.accumulate, VEC, rshift, VEC, cshift);
         wave_sync();
     }
 }
 
-// Whether a tile's copies may go straight to LDS: 16-byte chunks at 16-byte
-// places, within 32-bit offsets of the tile's first row.
 template <class T>
-bool direct(const void* a, const void* b, int64_t stride, int64_t extent, bool kc) {
+__global__ __launch_bounds__(256) void product_join_kernel(ProductShape p, Products<T> a) {
+    const int64_t per = p.pitch / 4, step = int64_t(gridDim.x) * 256, one = p.rows * p.pitch;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < p.rows * per * a.count; i += step) {
+        const bool second = i >= p.rows * per;
+        const int64_t j = second ? i - p.rows * per : i, r = j / per, c = j % per * 4;
+        float v[4] = {};
+        for (int s = 0; s < p.splits; ++s) {
+            float x[4];
+            Num<float>::unpack(load_vec(p.part + (s * a.count + second) * one + r * p.pitch + c), x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += x[e];
+        }
+        T* const at = (second ? a.out[1] : a.out[0]) + r * a.stride + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < p.cols) at[e] = Num<T>::down(a.accumulate ? Num<T>::up(at[e]) + v[e] : v[e]);
+    }
+}
+
+// Whether a tile's copies may go straight to LDS: 16-byte chunks at 16-byte
+// places (fp32: at any element), within 32-bit offsets of the tile's first row,
+// and, K-major, at least one chunk a row (fp32) or whole ones (bf16).
+template <class T>
+bool direct(const Side<T>& s, int64_t extent, bool kc) {
     constexpr int VEC = Num<T>::VEC;
-    if ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % kChunk) return false;
-    if (stride % VEC || stride * int64_t(sizeof(T)) > (int64_t(1) << 22)) return false;
-    return kc || extent % VEC == 0;
+    if (s.stride * int64_t(sizeof(T)) > (int64_t(1) << 22)) return false;
+    if (sizeof(T) == 2 &&
+        (s.stride % VEC ||
+         (reinterpret_cast<uintptr_t>(s.p[0]) | reinterpret_cast<uintptr_t>(s.p[1])) % kChunk))
+        return false;
+    return kc || (sizeof(T) == 4 ? extent >= VEC : extent % VEC == 0);
 }
 
 int64_t factor_stride(int64_t F) { return round_up(F, 8); }
 
-ProductShape shape(int64_t rows, int64_t cols, int64_t K, int segments, int br, int bc) {
-    return ProductShape{rows, cols, K, segments, ceil_div(rows, br), ceil_div(cols, bc)};
+// How a product is cut: square tiles of 256, 128 or 64, and parts along k.
+// The time is estimated as the most that one of the 256 CUs gets, at a rate a CU
+// that grows with the tile (a larger tile reads less from LDS for its
+// products), and, where k is split, the parts' way through memory and a launch.
+struct Cut {
+    int tile, splits;
+};
+
+constexpr double kCuFlops[2][3] = {
+    // 64, 128, 256, in 1e12 a second
+    {0.45, 0.54, 0.54},  // fp32
+    {1.7, 3.4, 4.3},     // bf16
+};
+
+Cut cut_of(int64_t rows, int64_t cols, int64_t K, int outputs, int esize, bool gated) {
+    Cut best{64, 1};
+    double least = 0;
+    for (int i = 0; i < 3; ++i) {
+        const int tile = 64 << i;
+        const int64_t tiles = ceil_div(rows, tile) * ceil_div(cols, gated ? tile / 2 : tile) * outputs;
+        const double one = 2.0 * tile * tile * double(K) / (kCuFlops[esize == 2][i] * 1e12);
+        for (int s = 1; s <= 16; s *= 2) {
+            if (s > 1 && K / s < 4 * (kStepBytes / esize)) break;
+            double t = double(ceil_div(tiles * s, 256)) * (one / s + 1.5e-6);
+            if (s > 1)
+                t += 4e-6 + 8.0 * s * double(rows) * double(cols) * outputs * (gated ? 2 : 1) / 4e12;
+            if (least == 0 || t < least) {
+                least = t;
+                best = Cut{tile, s};
+            }
+        }
+    }
+    return best;
 }
 
-dim3 grid_of(const ProductShape& p) {
-    return dim3(unsigned(tile_blocks(p.row_tiles * p.col_tiles)));
+int64_t part_pitch(int64_t cols) { return round_up(cols, 4); }
+// The workspace of a cut's parts.
+int64_t part_bytes(const Cut& c, int64_t rows, int64_t cols, int outputs) {
+    return c.splits > 1 ? round_up(4 * c.splits * outputs * rows * part_pitch(cols), 256) : 0;
 }
 
-template <class T, bool RKC, int BR, int BC, int WR, int WC>
-void launch_product(const ProductShape& p, const Side<T>& r, const Side<T>& l, int accumulate,
-                    T* out, int64_t stride, hipStream_t st) {
-    const bool fast = direct<T>(r.p[0], r.p[1], r.stride, p.rows, RKC) &&
-                      direct<T>(l.p[0], l.p[1], l.stride, p.cols, false);
-    const dim3 block(64 * WR * WC);
+ProductShape shape(int64_t rows, int64_t cols, int64_t K, int segments, const Cut& c, int width,
+                   void* part) {
+    return ProductShape{rows, cols, K, segments, ceil_div(rows, c.tile), ceil_div(cols, width),
+                        c.splits, static_cast<float*>(part), part_pitch(cols)};
+}
+
+dim3 grid_of(int64_t tiles) { return dim3(unsigned(tile_blocks(tiles))); }
+dim3 join_grid(int64_t vecs) {
+    return dim3(unsigned(std::min<int64_t>(ceil_div(vecs, 256), 1 << 14)));
+}
+
+template <class T, bool RKC, int B, int WR, int WC>
+void launch_product(const ProductShape& p, const Products<T>& a, bool fast, hipStream_t st) {
+    const dim3 grid = grid_of(p.row_tiles * p.col_tiles * p.splits * a.count), block(64 * WR * WC);
     if (fast)
-        hipLaunchKernelGGL((product_kernel<T, BR, BC, WR, WC, RKC, true>), grid_of(p), block, 0, st,
-                           p, r, l, accumulate, out, stride);
+        hipLaunchKernelGGL((product_kernel<T, B, B, WR, WC, RKC, true>), grid, block, 0, st, p, a);
     else
-        hipLaunchKernelGGL((product_kernel<T, BR, BC, WR, WC, RKC, false>), grid_of(p), block, 0,
-                           st, p, r, l, accumulate, out, stride);
+        hipLaunchKernelGGL((product_kernel<T, B, B, WR, WC, RKC, false>), grid, block, 0, st, p, a);
 }
 
-template <class T, int BR, int BC, int WR, int WC>
-void launch_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Side<T>& x,
-                    const Side<T>& w, T* h, T* sg, T* su, hipStream_t st) {
-    const ProductShape p = shape(M, F, D, 1, BR, BC / 2);
-    const bool fast = direct<T>(x.p[0], x.p[1], x.stride, M, true) &&
-                      direct<T>(w.p[0], w.p[1], w.stride, F, true);
-    const dim3 block(64 * WR * WC);
+template <class T, bool RKC>
+void run_product(int64_t rows, int64_t cols, int64_t K, int segments, const Products<T>& a,
+                 void* part, hipStream_t st) {
+    const Cut c = cut_of(rows, cols, K * segments, a.count, int(sizeof(T)), false);
+    const ProductShape p = shape(rows, cols, K, segments, c, c.tile, part);
+    bool fast = direct(a.l, cols, false);
+    for (int i = 0; i < a.count; ++i) fast = fast && direct(a.r[i], rows, RKC);
+    if (c.tile == 256) launch_product<T, RKC, 256, 2, 4>(p, a, fast, st);
+    else if (c.tile == 128) launch_product<T, RKC, 128, 2, 2>(p, a, fast, st);
+    else launch_product<T, RKC, 64, 2, 2>(p, a, fast, st);
+    if (c.splits > 1)
+        hipLaunchKernelGGL((product_join_kernel<T>), join_grid(rows * p.pitch / 4 * a.count), dim3(256),
+                           0, st, p, a);
+}
+
+template <class T, int B, int WR, int WC>
+void launch_forward(const ProductShape& p, const ForwardArgs& a, const Side<T>& x, const Side<T>& w,
+                    T* h, T* sg, T* su, bool fast, hipStream_t st) {
+    const dim3 grid = grid_of(p.row_tiles * p.col_tiles * p.splits), block(64 * WR * WC);
     if (fast)
-        hipLaunchKernelGGL((forward_kernel<T, BR, BC, WR, WC, true>), grid_of(p), block, 0, st, p, a,
-                           x, w, h, sg, su);
+        hipLaunchKernelGGL((forward_kernel<T, B, B, WR, WC, true>), grid, block, 0, st, p, a, x, w, h,
+                           sg, su);
     else
-        hipLaunchKernelGGL((forward_kernel<T, BR, BC, WR, WC, false>), grid_of(p), block, 0, st, p,
-                           a, x, w, h, sg, su);
+        hipLaunchKernelGGL((forward_kernel<T, B, B, WR, WC, false>), grid, block, 0, st, p, a, x, w,
+                           h, sg, su);
+}
+
+template <class T>
+void run_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Side<T>& x,
+                 const Side<T>& w, T* h, T* sg, T* su, void* part, hipStream_t st) {
+    const Cut c = cut_of(M, F, D, 1, int(sizeof(T)), true);
+    const ProductShape p = shape(M, F, D, 1, c, c.tile / 2, part);
+    const bool fast = direct(x, M, true) && direct(w, F, true);
+    if (c.tile == 256) launch_forward<T, 256, 2, 4>(p, a, x, w, h, sg, su, fast, st);
+    else if (c.tile == 128) launch_forward<T, 128, 2, 2>(p, a, x, w, h, sg, su, fast, st);
+    else launch_forward<T, 64, 2, 1>(p, a, x, w, h, sg, su, fast, st);
+    if (c.splits > 1)
+        hipLaunchKernelGGL((forward_join_kernel<T>), join_grid(M * p.pitch / 4), dim3(256), 0, st, p, a,
+                           h, sg, su);
+}
+
+// The backward call's workspace: the factors, then the parts of dx, then those
+// of dwg and dwu.
+struct BackSpace {
+    int64_t dx, dw, end;
+};
+BackSpace back_space(int64_t M, int64_t D, int64_t F, int esize) {
+    BackSpace b{};
+    b.dx = round_up(2 * M * factor_stride(F) * esize, 256);
+    b.dw = b.dx + part_bytes(cut_of(M, D, 2 * F, 1, esize, false), M, D, 1);
+    b.end = b.dw + part_bytes(cut_of(F, D, M, 2, esize, false), F, D, 2);
+    return b;
 }
 
 }  // namespace
 }  // namespace arp
 
 using namespace arp;
-
-// Whether a product of so many 256 x 256 tiles takes those, and not four times
-// as many of 128 x 128: where they fill the card's 256 CUs.
-static bool large_tiles(int64_t tiles) { return tiles >= 192; }
 
 static ar_status check_glu_sizes(int64_t M, int64_t D, int64_t F) {
     AR_TRY(check_extent("M", M));
@@ -176,7 +351,8 @@ AR_EXPORT ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_
     int32_t es = 0;
     AR_TRY(check_dtype("dtype", dtype, &es));
     AR_TRY(check_glu_sizes(M, D, F));
-    *bytes = backward ? round_up(2 * M * factor_stride(F) * es, 256) : 0;
+    *bytes = M == 0 || D == 0 || F == 0 ? 0 : part_bytes(cut_of(M, F, D, 1, es, true), M, F, 2);
+    if (backward) *bytes = std::max(*bytes, back_space(M, D, F, es).end);
     return AR_OK;
 }
 
@@ -216,10 +392,7 @@ AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_
             sw{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride};
         T *const oh = static_cast<T*>(h), *const og = static_cast<T*>(saved_gate),
                  *const ou = static_cast<T*>(saved_up);
-        if (large_tiles(ceil_div(M, 256) * ceil_div(F, 128)))
-            launch_forward<T, 256, 256, 2, 4>(a, M, D, F, sx, sw, oh, og, ou, st);
-        else
-            launch_forward<T, 128, 128, 2, 2>(a, M, D, F, sx, sw, oh, og, ou, st);
+        run_forward<T>(a, M, D, F, sx, sw, oh, og, ou, workspace, st);
         return launch_status("gated feed-forward");
     };
     return dtype == AR_F32 ? go(float(0)) : go(uint16_t(0));
@@ -262,31 +435,27 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
         T* const du = dg + M * fs;
         if (M > 0 && F > 0)
             hipLaunchKernelGGL((factors_kernel<T>),
-                               dim3(unsigned(std::min<int64_t>(ceil_div(M * F, 256), 1 << 16))),
+                               dim3(unsigned(std::min<int64_t>(ceil_div(M * ceil_div(F, Num<T>::VEC), 256), 1 << 16))),
                                dim3(256), 0, st, M, F, static_cast<const T*>(dh), dh_stride,
                                static_cast<const T*>(saved_gate), static_cast<const T*>(saved_up),
                                saved_stride, dg, du, fs);
-        auto product = [&](auto rkc, const Side<T>& r, const Side<T>& l, int64_t rows, int64_t K,
-                           int segments, int acc, void* out, int64_t stride) {
-            constexpr bool RKC = decltype(rkc)::value;
-            T* const o = static_cast<T*>(out);
-            if (large_tiles(ceil_div(rows, 256) * ceil_div(D, 256)))
-                launch_product<T, RKC, 256, 256, 2, 4>(shape(rows, D, K, segments, 256, 256), r, l,
-                                                       acc, o, stride, st);
-            else
-                launch_product<T, RKC, 128, 128, 2, 2>(shape(rows, D, K, segments, 128, 128), r, l,
-                                                       acc, o, stride, st);
-        };
-        if (dx && M > 0)
-            product(std::true_type{}, Side<T>{{dg, du}, fs},
-                    Side<T>{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride}, M, F,
-                    2, 0, dx, dx_stride);
+        const BackSpace space = back_space(M, D, F, es);
+        char* const ws = static_cast<char*>(workspace);
+        if (dx && M > 0) {
+            const Side<T> r{{dg, du}, fs},
+                l{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride};
+            run_product<T, true>(M, D, F, 2,
+                                 Products<T>{{r, r}, l, {static_cast<T*>(dx), nullptr}, dx_stride, 1, 0},
+                                 ws + space.dx, st);
+        }
         if (dwg && F > 0) {
-            const Side<T> sx{{static_cast<const T*>(x), static_cast<const T*>(x)}, x_stride};
-            product(std::false_type{}, Side<T>{{dg, dg}, fs}, sx, F, M, 1, accumulate, dwg,
-                    dw_stride);
-            product(std::false_type{}, Side<T>{{du, du}, fs}, sx, F, M, 1, accumulate, dwu,
-                    dw_stride);
+            const T* const px = static_cast<const T*>(x);
+            run_product<T, false>(F, D, M, 1,
+                                  Products<T>{{Side<T>{{dg, dg}, fs}, Side<T>{{du, du}, fs}},
+                                              Side<T>{{px, px}, x_stride},
+                                              {static_cast<T*>(dwg), static_cast<T*>(dwu)},
+                                              dw_stride, 2, accumulate},
+                                  ws + space.dw, st);
         }
         return launch_status("gated feed-forward gradients");
     };

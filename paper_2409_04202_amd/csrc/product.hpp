@@ -14,14 +14,20 @@
 // chunk c of row r at place c ^ swz(r), so that any 8 and any 16 successive
 // rows' chunks of one k lie in different banks.  K-major bf16: a row is one k,
 // read with the transposing LDS load (16 lanes read 4 k of 16 columns and each
-// receives 4 k of its column); chunk c of row k at c ^ 2 swzk(k), which puts the
+// receives 4 k of its column); chunk c of row k at c ^ swzk(k), which puts the
 // 32-byte pieces of 4 successive k, and of two neighbouring squares, into
 // different banks.  K-major fp32: a row is one k, unswizzled; a lane reads
 // single elements, 32 lanes 128 adjacent bytes.
 //
 // Edges.  Rows beyond an operand's end repeat its last row (their results are
 // not stored); a step's k beyond the end reads as zero in both operands, so
-// what lies there, NaN included, has no effect.
+// what lies there, NaN included, has no effect.  Where copies go straight to
+// LDS, the last chunk of a K-major row that has fewer elements is moved back to
+// end with the row: what it holds lies `shift` further on, in the accumulators
+// too, and the store reads it from there.
+//
+// Few tiles.  A product may be split along k (`splits`), each part's sums going
+// to memory in fp32; a second kernel adds them in order.
 #pragma once
 
 #include "replica.hpp"
@@ -51,10 +57,16 @@ struct ProductShape {
     int64_t K;           // of one segment
     int segments;        // 1 or 2
     int64_t row_tiles, col_tiles;
+    int splits;          // parts along k
+    float* part;         // their sums (splits > 1), [split][output][rows][pitch]
+    int64_t pitch;
 };
 
 __device__ __forceinline__ int swz(int r) { return ((r >> 1) ^ ((r & 1) << 2)) & 7; }
-__device__ __forceinline__ int swzk(int k) { return ((k & 3) ^ ((k & 3) << 1)) & 7; }
+// (of a K-major row of `chunks` chunks)
+__device__ __forceinline__ int swzk(int k, int chunks) {
+    return 2 * ((k & 3) ^ ((k & 3) << 1)) & (chunks - 1);
+}
 
 // One operand's panel: N rows (K-contiguous) or columns (K-major) of the step.
 template <class T, int N, int THREADS, bool KC, bool GATED>
@@ -72,7 +84,7 @@ struct Panel {
     int64_t first;      // the panel's first row (column) in the operand
     int64_t end;        // the operand's rows (columns)
     uint32_t off[LOADS];
-    int chunk;          // K-contiguous: the thread's chunk, in elements of k
+    int back;           // columns that the copies' origin lies before the first one
 
     // The thread's place in load i: panel row and chunk (logical).
     static __device__ __forceinline__ int row_of(int i) {
@@ -80,7 +92,7 @@ struct Panel {
     }
     static __device__ __forceinline__ int chunk_of(int i) {
         const int phys = int(threadIdx.x) % ROWCHUNKS, r = row_of(i);
-        return KC ? phys ^ swz(r) : (E == 2 ? phys ^ (2 * swzk(r)) : phys);
+        return KC ? phys ^ swz(r) : (E == 2 ? phys ^ swzk(r, ROWCHUNKS) : phys);
     }
     // The matrix and its row behind panel row r.
     __device__ __forceinline__ int64_t source(int r, int seg, const T** p) const {
@@ -94,7 +106,7 @@ struct Panel {
     }
 
     __device__ __forceinline__ Panel(const Side<T>& side, int64_t f, int64_t e)
-        : s(side), first(f), end(e) {
+        : s(side), first(f), end(e), back(0) {
         if constexpr (KC) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
@@ -103,11 +115,13 @@ struct Panel {
                 off[i] = uint32_t((r < last ? r : last) * s.stride * E) + chunk_of(i) * kChunk;
             }
         } else {
+            // a chunk that ends behind the row: its last whole one
+            const int64_t last = end - VEC - first;
+            if (last < 0) back = int(-last);
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                // columns beyond the end: the row's last whole chunk
-                const int64_t c = int64_t(chunk_of(i)) * VEC, last = end - VEC - first;
-                off[i] = uint32_t(row_of(i) * s.stride * E) + uint32_t((c < last ? c : last) * E);
+                const int64_t c = int64_t(chunk_of(i)) * VEC;
+                off[i] = uint32_t((row_of(i) * s.stride + (c < last ? c : last) + back) * E);
             }
         }
     }
@@ -126,7 +140,7 @@ struct Panel {
             const T* p;
             if constexpr (GATED) p = s.p[i * ROWSTEP >= N / 2];
             else p = seg ? s.p[1] : s.p[0];
-            p += KC ? first * s.stride + k0 : k0 * s.stride + first;
+            p += KC ? first * s.stride + k0 : k0 * s.stride + first - back;
             const uint64_t at = reinterpret_cast<uint64_t>(p);
             // a raw buffer from there on, without a bound below 4 GiB
             const u32x4 rsrc = {scalar(uint32_t(at)), scalar(uint32_t(at >> 32) & 0xFFFFu),
@@ -139,6 +153,8 @@ struct Panel {
 
     // The same through registers, for any alignment and with elements beyond
     // the ends of k and of a K-major row as zeros.
+    // MOVE: a K-major row's last chunk as the copies place it.
+    template <bool MOVE>
     __device__ __forceinline__ void fetch(int seg, int64_t k0, int64_t K, u32x4* v) const {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
@@ -150,8 +166,9 @@ struct Panel {
                 p += at * s.stride + k0 + c;
                 n = K - k0 - c;
             } else {
-                p += (k0 + r) * s.stride + first + c;
-                n = k0 + r < K ? end - first - c : 0;
+                const int64_t last = end - VEC - first, cc = MOVE && c > last ? last : c;
+                p += (k0 + r) * s.stride + first + cc;
+                n = k0 + r < K ? end - first - cc : 0;
             }
             if (n >= VEC) v[i] = load_vec(p);
             else if (n > 0) v[i] = load_part(p, int(n));
@@ -186,7 +203,7 @@ struct Frags {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int c = base / 8 + 4 * j + 2 * (g & 1) + ((l & 3) >> 1);
-                lane_off[j] = k * (N * 2) + ((c ^ (2 * swzk(k))) * kChunk) + (l & 1) * 8;
+                lane_off[j] = k * (N * 2) + ((c ^ swzk(k, N / 8)) * kChunk) + (l & 1) * 8;
             }
         } else {
             lane_off[0] = (4 * (lane >> 5)) * (N * 4) + (base + (lane & 31)) * 4;
@@ -231,16 +248,18 @@ __device__ __forceinline__ void multiply(const u32x4 l, const u32x4 r, f32x16& a
 // walked along the columns: what its 32 CUs work on at a time shares panels
 // in its L2.
 constexpr int kStrip = 4;
-__device__ __forceinline__ bool tile_of(const ProductShape& p, int64_t block, int64_t* r,
-                                        int64_t* c) {
-    const int64_t tiles = p.row_tiles * p.col_tiles, share = (tiles + 7) / 8;
-    const int64_t t = (block & 7) * share + (block >> 3);
-    if ((block >> 3) >= share || t >= tiles) return false;
+__device__ __forceinline__ bool tile_of(const ProductShape& p, int64_t tiles, int64_t block,
+                                        int64_t* tile) {
+    const int64_t share = (tiles + 7) / 8;
+    *tile = (block & 7) * share + (block >> 3);
+    return (block >> 3) < share && *tile < tiles;
+}
+// Where the tile lies in its product.
+__device__ __forceinline__ void place_of(const ProductShape& p, int64_t t, int64_t* r, int64_t* c) {
     const int64_t per = kStrip * p.col_tiles, strip = t / per, in = t % per;
     const int64_t h = p.row_tiles - strip * kStrip < kStrip ? p.row_tiles - strip * kStrip : kStrip;
     *r = strip * kStrip + in % h;
     *c = in / h;
-    return true;
 }
 inline int64_t tile_blocks(int64_t tiles) { return ceil_div(tiles, 8) * 8; }
 
@@ -263,7 +282,7 @@ struct Tile {
     static constexpr int LDS = 2 * HALF;
 
     static __device__ __forceinline__ void run(const ProductShape& p, const Side<T>& R,
-                                               const Side<T>& L, int64_t r0, int64_t c0,
+                                               const Side<T>& L, int64_t r0, int64_t c0, int split,
                                                AR_LDS char* lds, f32x16 (&acc)[SR][SC]) {
         const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
         const RP rp(R, r0, p.rows);
@@ -271,7 +290,10 @@ struct Tile {
         const Frags<T, BR, RKC> rf(wr * SR * 32);
         const Frags<T, BC, LKC> lf(wc * (GATED ? 32 : SC * 32));
         constexpr int KS = StepOf<T>::K;
-        const int steps = int((p.K + KS - 1) / KS) * p.segments;
+        const int per = int((p.K + KS - 1) / KS), all = per * p.segments;
+        // this part's steps
+        const int from = int(int64_t(all) * split / p.splits);
+        const int steps = int(int64_t(all) * (split + 1) / p.splits) - from;
         u32x4 rv[DIRECT ? 1 : RP::LOADS], lv[DIRECT ? 1 : LP::LOADS];
 
         auto start = [&](int seg, int64_t k0, int at) {
@@ -283,14 +305,14 @@ struct Tile {
                     lp.copy(seg, k0, to + RP::BYTES);
                 } else {  // the last, partial step
                     u32x4 a[RP::LOADS], b[LP::LOADS];
-                    rp.fetch(seg, k0, p.K, a);
-                    lp.fetch(seg, k0, p.K, b);
+                    rp.template fetch<true>(seg, k0, p.K, a);
+                    lp.template fetch<true>(seg, k0, p.K, b);
                     RP::put(buf, a);
                     LP::put(buf + RP::BYTES, b);
                 }
             } else {
-                rp.fetch(seg, k0, p.K, rv);
-                lp.fetch(seg, k0, p.K, lv);
+                rp.template fetch<false>(seg, k0, p.K, rv);
+                lp.template fetch<false>(seg, k0, p.K, lv);
             }
         };
         auto finish = [&](int at) {
@@ -316,9 +338,9 @@ struct Tile {
             }
         };
         if (steps == 0) return;
-        int seg = 0, at = 0;
-        int64_t k0 = 0;
-        start(0, 0, 0);
+        int seg = from >= per, at = 0;
+        int64_t k0 = int64_t(from - seg * per) * KS;
+        start(seg, k0, 0);
         finish(0);
         landed();
         __builtin_amdgcn_s_barrier();
@@ -360,11 +382,13 @@ struct Store {
                 *(AR_LDS f4*)(part + (lane & 31) * PITCH + j * 32 + 8 * q + 4 * (lane >> 5)) = v;
             }
     }
-    // rows r0 .. of `out`, columns c0 .. of the SC * 32
+    // rows r0 .. of `out`, columns c0 .. of the SC * 32; the last rows (columns)
+    // of an incomplete chunk of rshift (cshift) fewer lie so much further on
     template <class T>
     static __device__ __forceinline__ void store(const AR_LDS float* part, T* out, int64_t stride,
                                                  int64_t r0, int64_t rows, int64_t c0, int64_t cols,
-                                                 bool accumulate) {
+                                                 bool accumulate, int rchunk, int rshift,
+                                                 int cchunk, int cshift) {
         constexpr int VEC = Num<T>::VEC, PER = SC * 32 / VEC, ROWS = 64 / PER;
         const int lane = int(threadIdx.x) & 63;
 #pragma unroll
@@ -373,9 +397,12 @@ struct Store {
             const int64_t left = cols - c0 - c;
             if (r0 + r >= rows || left <= 0) continue;
             T* const at = out + (r0 + r) * stride + c0 + c;
+            const AR_LDS float* const row =
+                part + (rshift && rows - (r0 + r) <= rchunk - rshift ? r + rshift : r) * PITCH;
             float v[VEC];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = part[r * PITCH + c + e];
+            for (int e = 0; e < VEC; ++e)
+                v[e] = row[c + e + (cshift && left - e <= cchunk - cshift ? cshift : 0)];
             const int n = int(left < VEC ? left : VEC);
             if (accumulate) {
                 float old[VEC];

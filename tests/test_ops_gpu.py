@@ -176,6 +176,40 @@ def test_glu(M, D, F, dtype, act, layout):
 
 @pytest.mark.parametrize("layout", ("rows", "wide"))
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,D,F", [(20, 3000, 70), (70, 130, 2500), (1500, 65, 130), (130, 2, 67),
+                                   (5000, 65, 9), (3, 2049, 4097)])
+def test_glu_long_sums(M, D, F, dtype, layout):
+    """Products of few tiles and long sums, which are split, and of a few
+    columns beyond a tile."""
+    test_glu(M, D, F, dtype, "gelu", layout)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_glu_rows_within_a_matrix(dtype):
+    """Row strides at 16 bytes with widths that are not: the last chunk of a
+    row is incomplete, and what follows it in memory is NaN."""
+    M, D, F = 203, 133, 301
+    x, wg = rnd(1, M, D, dtype=dtype), rnd(2, F, D, dtype=dtype, scale=D ** -0.5)
+    wu, dh = rnd(3, F, D, dtype=dtype, scale=D ** -0.5), rnd(4, M, F, dtype=dtype)
+    want = ref.glu(x, wg, wu, "silu", dh, dtype)
+
+    def inside(t):
+        m = torch.full((t.shape[0], -(-t.shape[1] // 16) * 16 + 16), float("nan"), dtype=t.dtype,
+                       device="cuda")
+        m[:, :t.shape[1]] = t.cuda()
+        return m[:, :t.shape[1]]
+    x, wg, wu, dh = (inside(t) for t in (x, wg, wu, dh))
+    h, saved = ops.glu_forward(x, wg, wu, save=True)
+    got = (h,) + ops.glu_backward(dh, x, wg, wu, saved)
+    for name, g, w in zip(("h", "dx", "dwg", "dwu"), got, want):
+        ref.compare(name, g, *w)
+    more = ops.glu_backward(dh, x, wg, wu, saved, dwg=got[2], dwu=got[3], accumulate=True)
+    for name, g, w in zip(("dwg", "dwu"), more[1:], want[2:]):
+        ref.compare(name, g, 2 * w[0], 2 * w[1] + ref.stored(2 * w[0], dtype))
+
+
+@pytest.mark.parametrize("layout", ("rows", "wide"))
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("M,D,F", [(2050, 72, 3000), (2309, 5800, 40), (50, 3849, 3081)])
 def test_glu_many_tiles(M, D, F, dtype, layout):
     """Products of so many tiles that the largest ones are taken: h's, dx's and
