@@ -6,9 +6,10 @@
 // A block computes a tile of C; its wavefronts split it into 32 x 32 squares
 // of accumulators.  Per step of 128 bytes of k (64 bf16 or 32 fp32) the
 // operands' panels are copied into LDS, two buffers in turn: the copies of
-// the next step run while this one's products do.  The column operand is the
-// matrix instruction's first, so a lane holds, of one row of C, runs of four
-// adjacent columns.
+// the next step run while this one's products do, and the fragments of the next
+// quarter of a step are read while this quarter's products run.  The column
+// operand is the matrix instruction's first, so a lane holds, of one row of C,
+// runs of four adjacent columns.
 //
 // LDS layouts.  K-contiguous: a row of the panel is 8 chunks of 16 bytes,
 // chunk c of row r at place c ^ swz(r), so that any 8 and any 16 successive
@@ -321,44 +322,63 @@ struct Tile {
                 LP::put(lds + at + RP::BYTES, lv);
             }
         };
-        auto compute = [&](int at) {
+        // Fragments in two sets: one is read while the other's products run.
+        u32x4 rf_[2][SR], lf_[2][SC];
+        auto read = [&](int at, int s, int set) {
             const AR_LDS char* const buf = lds + at;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                u32x4 r[SR], l[SC];
+            for (int j = 0; j < SC; ++j)
+                lf_[set][j] = lf.read(buf + RP::BYTES, GATED ? j * (BC / 64) : j, s);
 #pragma unroll
-                for (int j = 0; j < SC; ++j)
-                    l[j] = lf.read(buf + RP::BYTES, GATED ? j * (BC / 64) : j, s);
+            for (int i = 0; i < SR; ++i) rf_[set][i] = rf.read(buf, i, s);
+            // a phase's reads stay ahead of its products, and out of the next one's
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto products = [&](int set) {
 #pragma unroll
-                for (int i = 0; i < SR; ++i) r[i] = rf.read(buf, i, s);
+            for (int i = 0; i < SR; ++i)
 #pragma unroll
-                for (int i = 0; i < SR; ++i)
-#pragma unroll
-                    for (int j = 0; j < SC; ++j) multiply<T>(l[j], r[i], acc[i][j]);
-            }
+                for (int j = 0; j < SC; ++j) multiply<T>(lf_[set][j], rf_[set][i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
         };
         if (steps == 0) return;
         int seg = from >= per, at = 0;
         int64_t k0 = int64_t(from - seg * per) * KS;
+        auto advance = [&]() {
+            k0 += KS;
+            if (k0 >= p.K) {
+                k0 = 0;
+                ++seg;
+            }
+        };
         start(seg, k0, 0);
         finish(0);
         landed();
         __builtin_amdgcn_s_barrier();
+        if (steps > 1) {
+            advance();
+            start(seg, k0, HALF);
+        }
+        read(0, 0, 0);
         for (int t = 0; t < steps; ++t) {
-            const bool more = t + 1 < steps;
-            if (more) {
-                k0 += KS;
-                if (k0 >= p.K) {
-                    k0 = 0;
-                    ++seg;
-                }
-                start(seg, k0, HALF - at);
-            }
-            compute(at);
-            at = HALF - at;
-            if (more) finish(at);
+            read(at, 1, 1);
+            products(0);
+            read(at, 2, 0);
+            products(1);
+            read(at, 3, 1);
+            products(0);
+            // The step's last fragments are here, and the next step's panels: after
+            // the barrier this buffer is free, and the other one whole.
+            if (t + 1 < steps) finish(HALF - at);
             landed();
             __builtin_amdgcn_s_barrier();
+            if (t + 2 < steps) {
+                advance();
+                start(seg, k0, at);
+            }
+            at = HALF - at;
+            if (t + 1 < steps) read(at, 0, 0);
+            products(1);
         }
     }
 };
