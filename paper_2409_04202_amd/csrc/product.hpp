@@ -127,30 +127,35 @@ struct Panel {
         }
     }
 
-    // Start the copies of the step at k0 (whole) straight into LDS, `lds` the
-    // address there: lane l's 16 bytes go to the wavefront's 1 KiB at 16 l.
-    // They are written as assembly because of the waits: the compiler would
-    // hold every LDS read back until all copies have landed, those of the
-    // other buffer among them.  Whoever reads what they bring waits for the
-    // vector memory counter and passes a barrier first (see landed()).  (m0 is
-    // never allocated: nothing else here uses it.)
-    __device__ __forceinline__ void copy(int seg, int64_t k0, uint32_t lds) const {
-        const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const T* p;
-            if constexpr (GATED) p = s.p[i * ROWSTEP >= N / 2];
-            else p = seg ? s.p[1] : s.p[0];
-            p += KC ? first * s.stride + k0 : k0 * s.stride + first - back;
-            const uint64_t at = reinterpret_cast<uint64_t>(p);
-            // a raw buffer from there on, without a bound below 4 GiB
-            const u32x4 rsrc = {scalar(uint32_t(at)), scalar(uint32_t(at >> 32) & 0xFFFFu),
-                                0xFFFFFFFFu, 0x00020000u};
-            const uint32_t to = scalar(lds + uint32_t(i * THREADS + wave * 64) * kChunk);
-            asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                         :: "s"(to), "v"(off[i]), "s"(rsrc) : "memory");
-        }
+    // Where the copies of the first step of segment `seg` (of half `seg` of a
+    // gated panel) start, as a scalar, and how far on the next step's do.
+    __device__ __forceinline__ uint64_t origin(int seg, int64_t k0) const {
+        const T* const p = (seg ? s.p[1] : s.p[0]) +
+                           (KC ? first * s.stride + k0 : k0 * s.stride + first - back);
+        const uint64_t at = reinterpret_cast<uint64_t>(p);
+        return uint64_t(scalar(uint32_t(at >> 32))) << 32 | scalar(uint32_t(at));
     }
+    __device__ __forceinline__ uint64_t advance() const {
+        return KC ? kStepBytes : uint64_t(s.stride) * kStepBytes;
+    }
+    // Start copy i of a whole step straight into LDS, `lds` the panel's address
+    // there: lane l's 16 bytes go to the wavefront's 1 KiB at 16 l.  It is
+    // written as assembly because of the waits: the compiler would hold every
+    // LDS read back until all copies have landed, those of the other buffer
+    // among them.  Whoever reads what they bring waits for the vector memory
+    // counter and passes a barrier first (see landed()).  (m0 is never
+    // allocated: nothing else here uses it.)
+    __device__ __forceinline__ void copy(int i, uint64_t at, uint32_t lds) const {
+        // a raw buffer from there on, without a bound below 4 GiB
+        const u32x4 rsrc = {uint32_t(at), uint32_t(at >> 32) & 0xFFFFu, 0xFFFFFFFFu, 0x00020000u};
+        const uint32_t to = lds + uint32_t(i * THREADS) * kChunk;
+        // (a write of m0 has to be a state old, a scalar that a vector
+        // instruction wrote five, before the load reads them)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :: "s"(to), "v"(off[i]), "s"(rsrc) : "memory");
+    }
+    // Whether copy i belongs to the second half of a gated panel.
+    static __device__ __forceinline__ bool upper(int i) { return GATED && i * ROWSTEP >= N / 2; }
 
     // The same through registers, for any alignment and with elements beyond
     // the ends of k and of a K-major row as zeros.
@@ -295,31 +300,54 @@ struct Tile {
         // this part's steps
         const int from = int(int64_t(all) * split / p.splits);
         const int steps = int(int64_t(all) * (split + 1) / p.splits) - from;
+        if (steps == 0) return;
         u32x4 rv[DIRECT ? 1 : RP::LOADS], lv[DIRECT ? 1 : LP::LOADS];
-
-        auto start = [&](int seg, int64_t k0, int at) {
-            AR_LDS char* const buf = lds + at;
+        // The step whose copies come next: its segment and number there, and where
+        // it lies in the operands.
+        int seg = from >= per, k = from - seg * per;
+        const int whole = int(p.K / KS);  // steps of a segment that are whole
+        uint64_t ra = rp.origin(seg, int64_t(k) * KS), la[2];
+        la[0] = lp.origin(GATED ? 0 : seg, int64_t(k) * KS);
+        la[1] = GATED ? lp.origin(1, int64_t(k) * KS) : 0;
+        const uint64_t rstep = rp.advance(), lstep = lp.advance();
+        const uint32_t mine =
+            scalar(uint32_t(reinterpret_cast<uintptr_t>(lds)) + uint32_t(wave) * 64 * kChunk);
+        constexpr int COPIES = RP::LOADS + LP::LOADS;
+        auto copy = [&](int n, int at) {
+            if (n < RP::LOADS) rp.copy(n, ra, mine + at);
+            else if (n < COPIES)
+                lp.copy(n - RP::LOADS, LP::upper(n - RP::LOADS) ? la[1] : la[0],
+                        mine + at + RP::BYTES);
+        };
+        // Any step but a whole one straight to LDS: through registers.
+        auto fetch = [&](int at) {
+            const int64_t k0 = int64_t(k) * KS;
             if constexpr (DIRECT) {
-                if (k0 + KS <= p.K) {
-                    const uint32_t to = uint32_t(reinterpret_cast<uintptr_t>(buf));
-                    rp.copy(seg, k0, to);
-                    lp.copy(seg, k0, to + RP::BYTES);
-                } else {  // the last, partial step
-                    u32x4 a[RP::LOADS], b[LP::LOADS];
-                    rp.template fetch<true>(seg, k0, p.K, a);
-                    lp.template fetch<true>(seg, k0, p.K, b);
-                    RP::put(buf, a);
-                    LP::put(buf + RP::BYTES, b);
-                }
+                u32x4 a[RP::LOADS], b[LP::LOADS];
+                rp.template fetch<true>(seg, k0, p.K, a);
+                lp.template fetch<true>(seg, k0, p.K, b);
+                RP::put(lds + at, a);
+                LP::put(lds + at + RP::BYTES, b);
             } else {
                 rp.template fetch<false>(seg, k0, p.K, rv);
                 lp.template fetch<false>(seg, k0, p.K, lv);
             }
         };
-        auto finish = [&](int at) {
+        auto put = [&](int at) {
             if constexpr (!DIRECT) {
                 RP::put(lds + at, rv);
                 LP::put(lds + at + RP::BYTES, lv);
+            }
+        };
+        auto next = [&]() {
+            ra += rstep;
+            la[0] += lstep;
+            la[1] += lstep;
+            if (++k == per) {
+                k = 0;
+                ++seg;
+                ra = rp.origin(1, 0);
+                if constexpr (!GATED) la[0] = lp.origin(1, 0);
             }
         };
         // Fragments in two sets: one is read while the other's products run.
@@ -334,51 +362,60 @@ struct Tile {
             // a phase's reads stay ahead of its products, and out of the next one's
             __builtin_amdgcn_sched_barrier(0);
         };
-        auto products = [&](int set) {
+        // The products of a set; with `copies` the next step's copies among them,
+        // so that the matrix unit does not wait for their issue.
+        auto products = [&](int set, bool copies, int at) {
+            constexpr int PER = (COPIES + SR * SC - 1) / (SR * SC);
 #pragma unroll
-            for (int i = 0; i < SR; ++i)
+            for (int n = 0; n < SR * SC; ++n) {
+                multiply<T>(lf_[set][n % SC], rf_[set][n / SC], acc[n / SC][n % SC]);
+                if (DIRECT && copies) {
 #pragma unroll
-                for (int j = 0; j < SC; ++j) multiply<T>(lf_[set][j], rf_[set][i], acc[i][j]);
+                    for (int c = 0; c < PER; ++c) copy(n * PER + c, at);
+                }
+            }
             __builtin_amdgcn_sched_barrier(0);
         };
-        if (steps == 0) return;
-        int seg = from >= per, at = 0;
-        int64_t k0 = int64_t(from - seg * per) * KS;
-        auto advance = [&]() {
-            k0 += KS;
-            if (k0 >= p.K) {
-                k0 = 0;
-                ++seg;
+        for (int n = 0; n < 2; ++n) {  // the first two steps
+            if (n == 1) {
+                put(0);
+                landed();
+                __builtin_amdgcn_s_barrier();
+                if (steps == 1) break;
+                next();
             }
-        };
-        start(seg, k0, 0);
-        finish(0);
-        landed();
-        __builtin_amdgcn_s_barrier();
-        if (steps > 1) {
-            advance();
-            start(seg, k0, HALF);
+            if (DIRECT && k < whole) {
+#pragma unroll
+                for (int c = 0; c < COPIES; ++c) copy(c, n * HALF);
+            } else {
+                fetch(n * HALF);
+            }
         }
         read(0, 0, 0);
+        int at = 0;
         for (int t = 0; t < steps; ++t) {
             read(at, 1, 1);
-            products(0);
+            products(0, false, 0);
             read(at, 2, 0);
-            products(1);
+            products(1, false, 0);
             read(at, 3, 1);
-            products(0);
+            products(0, false, 0);
             // The step's last fragments are here, and the next step's panels: after
             // the barrier this buffer is free, and the other one whole.
-            if (t + 1 < steps) finish(HALF - at);
+            if (t + 1 < steps) put(HALF - at);
             landed();
             __builtin_amdgcn_s_barrier();
-            if (t + 2 < steps) {
-                advance();
-                start(seg, k0, at);
+            bool copies = t + 2 < steps;
+            if (copies) {
+                next();
+                if (!DIRECT || k >= whole) {
+                    fetch(at);
+                    copies = false;
+                }
             }
+            if (t + 1 < steps) read(HALF - at, 0, 0);
+            products(1, copies, at);
             at = HALF - at;
-            if (t + 1 < steps) read(at, 0, 0);
-            products(1);
         }
     }
 };
