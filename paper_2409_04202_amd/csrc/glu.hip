@@ -7,16 +7,33 @@
 namespace arp {
 namespace {
 
-// a(g) and a'(g).
+// exp(x), to a few units in the last place: 2^(x log2 e) with what the product
+// was rounded by put back.
+__device__ __forceinline__ float exp_of(float x) {
+    const float t = x * 1.44269504f, lost = fmaf(x, 1.44269504f, -t) + x * 1.92596299e-8f;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return fabsf(t) < 127.0f ? fmaf(e, lost * 0.69314718f, e) : e;
+}
+// 1 / x for x >= 1, to a unit in the last place.
+__device__ __forceinline__ float inverse(float x) {
+    const float r = __builtin_amdgcn_rcpf(x);
+    return r == 0.0f ? r : fmaf(fmaf(-x, r, 1.0f), r, r);
+}
+
+// a(g) and a'(g).  For bf16 the hardware's exponential and reciprocal as they
+// are: their errors, some units of fp32, are far below its rounding.
+template <class T>
 __device__ __forceinline__ void activate(int act, float g, float* value, float* slope) {
     if (act == AR_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-g));
+        float s;
+        if constexpr (sizeof(T) == 2) s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
+        else s = inverse(1.0f + exp_of(-g));
         // at infinities the limits, not inf * 0
         *value = g == -INFINITY ? 0.0f : g * s;
         *slope = s == 0.0f ? 0.0f : s * (1.0f + (s == 1.0f ? 0.0f : g * (1.0f - s)));
     } else {
         const float cdf = 0.5f * erfcf(g * -0.70710678118654752f);
-        const float pdf = 0.39894228040143268f * expf(-0.5f * g * g);
+        const float pdf = 0.39894228040143268f * exp_of(-0.5f * g * g);
         *value = g == -INFINITY ? 0.0f : g * cdf;
         *slope = cdf + (pdf == 0.0f ? 0.0f : g * pdf);
     }
@@ -63,7 +80,7 @@ __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, F
         }
         float value[16], slope[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) activate(a.act, acc[i][0][e], &value[e], &slope[e]);
+        for (int e = 0; e < 16; ++e) activate<T>(a.act, acc[i][0][e], &value[e], &slope[e]);
         pass(h, a.h_stride, [&](int, int e) { return value[e] * acc[i][1][e]; });
         if (sg) {
             pass(sg, a.saved_stride, [&](int, int e) { return slope[e] * acc[i][1][e]; });
@@ -94,7 +111,7 @@ __global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, Forwa
         for (int e = 0; e < 4; ++e) {
             if (c + e >= p.cols) continue;
             float value, slope;
-            activate(a.act, g[e], &value, &slope);
+            activate<T>(a.act, g[e], &value, &slope);
             h[r * a.h_stride + c + e] = Num<T>::down(value * u[e]);
             if (sg) {
                 sg[r * a.saved_stride + c + e] = Num<T>::down(slope * u[e]);

@@ -313,6 +313,7 @@ struct Tile {
         const uint32_t mine =
             scalar(uint32_t(reinterpret_cast<uintptr_t>(lds)) + uint32_t(wave) * 64 * kChunk);
         constexpr int COPIES = RP::LOADS + LP::LOADS;
+        constexpr bool SPREAD = !(RKC && LKC);
         auto copy = [&](int n, int at) {
             if (n < RP::LOADS) rp.copy(n, ra, mine + at);
             else if (n < COPIES)
@@ -362,16 +363,22 @@ struct Tile {
             // a phase's reads stay ahead of its products, and out of the next one's
             __builtin_amdgcn_sched_barrier(0);
         };
-        // The products of a set; with `copies` the next step's copies among them,
-        // so that the matrix unit does not wait for their issue.
-        auto products = [&](int set, bool copies, int at) {
-            constexpr int PER = (COPIES + SR * SC - 1) / (SR * SC);
+        // The products of a set; with `copies` some of the next step's copies among
+        // them, so that the matrix unit does not wait for their issue.  The 8
+        // wavefronts' copies of a step keep the address unit busy for as long as the
+        // products of two quarters take, and are spread over as many; not where both
+        // operands are K-contiguous, whose copies touch more lines and take longer
+        // to arrive (8192 x 4096 x 16384: dx 1.73 -> 1.69 ms and the weight
+        // gradients 1.78 -> 1.72 with spread copies, but the forward 1.95 -> 2.00).
+        auto products = [&](int set, bool copies, int half, int at) {
+            constexpr int H = SPREAD ? COPIES / 2 : COPIES, S = SR * SC;
+            static_assert(COPIES % 2 == 0, "");
 #pragma unroll
-            for (int n = 0; n < SR * SC; ++n) {
+            for (int n = 0; n < S; ++n) {
                 multiply<T>(lf_[set][n % SC], rf_[set][n / SC], acc[n / SC][n % SC]);
                 if (DIRECT && copies) {
 #pragma unroll
-                    for (int c = 0; c < PER; ++c) copy(n * PER + c, at);
+                    for (int c = n * H / S; c < (n + 1) * H / S; ++c) copy(half * H + c, at);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -393,28 +400,29 @@ struct Tile {
         }
         read(0, 0, 0);
         int at = 0;
+        bool late = false;  // whether the next step's second half is still to come
         for (int t = 0; t < steps; ++t) {
             read(at, 1, 1);
-            products(0, false, 0);
+            products(0, SPREAD && late, 1, HALF - at);
             read(at, 2, 0);
-            products(1, false, 0);
+            products(1, false, 0, 0);
             read(at, 3, 1);
-            products(0, false, 0);
+            products(0, false, 0, 0);
             // The step's last fragments are here, and the next step's panels: after
             // the barrier this buffer is free, and the other one whole.
             if (t + 1 < steps) put(HALF - at);
             landed();
             __builtin_amdgcn_s_barrier();
-            bool copies = t + 2 < steps;
-            if (copies) {
+            late = t + 2 < steps;
+            if (late) {
                 next();
                 if (!DIRECT || k >= whole) {
                     fetch(at);
-                    copies = false;
+                    late = false;
                 }
             }
             if (t + 1 < steps) read(HALF - at, 0, 0);
-            products(1, copies, at);
+            products(1, late, 0, at);
             at = HALF - at;
         }
     }
