@@ -494,15 +494,17 @@ ar_status ar_embed_grad(int32_t dtype, int64_t V, int64_t D, int64_t T, const vo
  *   AR_ACT_SILU   a(g) = g / (1 + exp(-g))
  *   AR_ACT_GELU   a(g) = g (1 + erf(g / sqrt 2)) / 2
  * For a backward pass the call also stores the two factors that the chain
- * rule needs, each rounded once to dtype: saved_gate = a'(g) u and saved_up =
- * a(g) (M x F, a common stride; both NULL for a forward pass alone). */
+ * rule needs: saved_gate = a'(g) u and saved_up = a(g) (M x F, a common
+ * stride; both NULL for a forward pass alone), in saved_dtype: AR_F32, or
+ * dtype, rounded once, which takes half of the memory for bf16 and adds a
+ * rounding to every gradient. */
 typedef enum ar_act { AR_ACT_SILU = 0, AR_ACT_GELU = 1 } ar_act;
 #define AR_GLU_MAX_EXTENT 4194304 /* M, D and F (AR_ERR_UNSUPPORTED above) */
 ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_t D, int64_t F,
                          const void* x, int64_t x_stride, const void* wg, const void* wu,
                          int64_t w_stride, void* h, int64_t h_stride, void* saved_gate,
-                         void* saved_up, int64_t saved_stride, void* workspace,
-                         int64_t workspace_bytes, void* stream);
+                         void* saved_up, int64_t saved_stride, int32_t saved_dtype,
+                         void* workspace, int64_t workspace_bytes, void* stream);
 
 /* The gradients of the block for dh = dL/dh (M x F), from what the forward
  * pass saved: with dg = dh * saved_gate and du = dh * saved_up (rounded once
@@ -513,8 +515,8 @@ ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_t D, int64
 ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t F, const void* dh,
                           int64_t dh_stride, const void* x, int64_t x_stride, const void* wg,
                           const void* wu, int64_t w_stride, const void* saved_gate,
-                          const void* saved_up, int64_t saved_stride, int32_t accumulate,
-                          void* dx, int64_t dx_stride, void* dwg, void* dwu, int64_t dw_stride,
+                          const void* saved_up, int64_t saved_stride, int32_t saved_dtype,
+                          int32_t accumulate, void* dx, int64_t dx_stride, void* dwg, void* dwu, int64_t dw_stride,
                           void* workspace, int64_t workspace_bytes, void* stream);
 
 /* The larger of the two calls' workspaces (backward == 0: the forward

@@ -103,10 +103,10 @@ _sig = {
                       c_int64, _P, c_int64, _P],
     "ar_glu_workspace": [c_int32, c_int64, c_int64, c_int64, c_int32, POINTER(c_int64)],
     "ar_glu_forward": [c_int32, c_int32, c_int64, c_int64, c_int64, _P, c_int64, _P, _P, c_int64,
-                       _P, c_int64, _P, _P, c_int64, _P, c_int64, _P],
+                       _P, c_int64, _P, _P, c_int64, c_int32, _P, c_int64, _P],
     "ar_glu_backward": [c_int32, c_int64, c_int64, c_int64, _P, c_int64, _P, c_int64, _P, _P,
-                        c_int64, _P, _P, c_int64, c_int32, _P, c_int64, _P, _P, c_int64, _P,
-                        c_int64, _P],
+                        c_int64, _P, _P, c_int64, c_int32, c_int32, _P, c_int64, _P, _P, c_int64,
+                        _P, c_int64, _P],
     "ar_distill_workspace": [c_int64, c_int64, c_int64, POINTER(c_int64)],
     "ar_distill": [c_int32, c_int64, c_int64, c_int64, _P, c_int64, c_int32, _P, c_int64, _P,
                    c_int64, c_float, _P, _P, _P, c_int64, _P, c_int64, _P],
@@ -413,19 +413,24 @@ def ar_glu_workspace(dtype, M, D, F, backward):
 
 
 def ar_glu_forward(dtype, act, M, D, F, x, x_stride, wg, wu, w_stride, h, h_stride, saved_gate,
-                   saved_up, saved_stride, workspace, workspace_bytes, stream=None):
+                   saved_up, saved_stride, workspace, workspace_bytes, stream=None,
+                   saved_dtype=None):
+    """``saved_dtype``: by default ``dtype``."""
     _check(_lib.ar_glu_forward(_dtype(dtype), ACTS[act] if isinstance(act, str) else int(act), M, D,
                                F, _ptr(x), x_stride, _ptr(wg), _ptr(wu), w_stride, _ptr(h),
                                h_stride, _ptr(saved_gate), _ptr(saved_up), saved_stride,
+                               _dtype(dtype if saved_dtype is None else saved_dtype),
                                _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def ar_glu_backward(dtype, M, D, F, dh, dh_stride, x, x_stride, wg, wu, w_stride, saved_gate,
                     saved_up, saved_stride, accumulate, dx, dx_stride, dwg, dwu, dw_stride,
-                    workspace, workspace_bytes, stream=None):
+                    workspace, workspace_bytes, stream=None, saved_dtype=None):
+    """``saved_dtype``: by default ``dtype``."""
     _check(_lib.ar_glu_backward(_dtype(dtype), M, D, F, _ptr(dh), dh_stride, _ptr(x), x_stride,
                                 _ptr(wg), _ptr(wu), w_stride, _ptr(saved_gate), _ptr(saved_up),
-                                saved_stride, int(accumulate), _ptr(dx), dx_stride, _ptr(dwg),
+                                saved_stride, _dtype(dtype if saved_dtype is None else saved_dtype),
+                                int(accumulate), _ptr(dx), dx_stride, _ptr(dwg),
                                 _ptr(dwu), dw_stride, _ptr(workspace), workspace_bytes,
                                 _stream(stream)))
 

@@ -42,14 +42,16 @@ __device__ __forceinline__ void activate(int act, float g, float* value, float* 
 struct ForwardArgs {
     int64_t h_stride, saved_stride;
     int act;
+    // the saved factors, or NULL: in fp32, or in the matrices' type
+    void *sg, *su;
+    bool saved_f32;
 };
 
 // h, and the saved factors where they are wanted, of a tile; or, split along k,
 // the tile's sums of g and of u.
 template <class T, int BR, int BC, int WR, int WC, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, ForwardArgs a,
-                                                               Side<T> x, Side<T> w, T* h, T* sg,
-                                                               T* su) {
+                                                               Side<T> x, Side<T> w, T* h) {
     using P = Tile<T, BR, BC, WR, WC, true, true, true, DIRECT>;
     using S = Store<1>;
     constexpr int LDS = P::LDS > WR * WC * S::BYTES ? P::LDS : WR * WC * S::BYTES;
@@ -82,17 +84,18 @@ __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, F
 #pragma unroll
         for (int e = 0; e < 16; ++e) activate<T>(a.act, acc[i][0][e], &value[e], &slope[e]);
         pass(h, a.h_stride, [&](int, int e) { return value[e] * acc[i][1][e]; });
-        if (sg) {
+        auto save = [&](auto* sg, auto* su) {
             pass(sg, a.saved_stride, [&](int, int e) { return slope[e] * acc[i][1][e]; });
             pass(su, a.saved_stride, [&](int, int e) { return value[e]; });
-        }
+        };
+        if (a.sg && a.saved_f32) save(static_cast<float*>(a.sg), static_cast<float*>(a.su));
+        else if (a.sg) save(static_cast<T*>(a.sg), static_cast<T*>(a.su));
     }
 }
 
 // The sums of a product split along k, added in order, to its output.
 template <class T>
-__global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, ForwardArgs a, T* h,
-                                                           T* sg, T* su) {
+__global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, ForwardArgs a, T* h) {
     const int64_t per = p.pitch / 4, step = int64_t(gridDim.x) * 256, one = p.rows * p.pitch;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < p.rows * per; i += step) {
         const int64_t r = i / per, c = i % per * 4;
@@ -113,32 +116,48 @@ __global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, Forwa
             float value, slope;
             activate<T>(a.act, g[e], &value, &slope);
             h[r * a.h_stride + c + e] = Num<T>::down(value * u[e]);
-            if (sg) {
-                sg[r * a.saved_stride + c + e] = Num<T>::down(slope * u[e]);
-                su[r * a.saved_stride + c + e] = Num<T>::down(value);
+            const int64_t at = r * a.saved_stride + c + e;
+            if (a.sg && a.saved_f32) {
+                static_cast<float*>(a.sg)[at] = slope * u[e];
+                static_cast<float*>(a.su)[at] = value;
+            } else if (a.sg) {
+                static_cast<T*>(a.sg)[at] = Num<T>::down(slope * u[e]);
+                static_cast<T*>(a.su)[at] = Num<T>::down(value);
             }
         }
     }
 }
 
-// dg = dh * saved_gate and du = dh * saved_up, a vector a lane.  Bound by
-// memory: five matrices pass once.
-template <class T>
+// dg = dh * saved_gate and du = dh * saved_up (of type S), a vector of T a
+// lane.  Bound by memory: five matrices pass once.
+template <class T, class S>
 __global__ __launch_bounds__(256) void factors_kernel(int64_t M, int64_t F, const T* dh,
-                                                      int64_t dh_stride, const T* sg, const T* su,
+                                                      int64_t dh_stride, const S* sg, const S* su,
                                                       int64_t saved_stride, T* dg, T* du,
                                                       int64_t stride) {
-    constexpr int VEC = Num<T>::VEC;
+    constexpr int VEC = Num<T>::VEC, SV = Num<S>::VEC;
     const int64_t per = (F + VEC - 1) / VEC, step = int64_t(gridDim.x) * 256;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < M * per; i += step) {
         const int64_t r = i / per, c = i % per * VEC;
         const int n = int(F - c < VEC ? F - c : VEC);
-        const T *pd = dh + r * dh_stride + c, *pg = sg + r * saved_stride + c,
-                *pu = su + r * saved_stride + c;
+        const T* pd = dh + r * dh_stride + c;
+        const S *pg = sg + r * saved_stride + c, *pu = su + r * saved_stride + c;
         float d[VEC], g[VEC], u[VEC];
-        Num<T>::unpack(n == VEC ? load_vec(pd) : load_part(pd, n), d);
-        Num<T>::unpack(n == VEC ? load_vec(pg) : load_part(pg, n), g);
-        Num<T>::unpack(n == VEC ? load_vec(pu) : load_part(pu, n), u);
+        if (n == VEC) {
+            Num<T>::unpack(load_vec(pd), d);
+#pragma unroll
+            for (int e = 0; e < VEC; e += SV) {
+                Num<S>::unpack(load_vec(pg + e), g + e);
+                Num<S>::unpack(load_vec(pu + e), u + e);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                d[e] = e < n ? Num<T>::up(pd[e]) : 0.0f;
+                g[e] = e < n ? Num<S>::up(pg[e]) : 0.0f;
+                u[e] = e < n ? Num<S>::up(pu[e]) : 0.0f;
+            }
+        }
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             g[e] *= d[e];
@@ -309,28 +328,25 @@ void run_product(int64_t rows, int64_t cols, int64_t K, int segments, const Prod
 
 template <class T, int B, int WR, int WC>
 void launch_forward(const ProductShape& p, const ForwardArgs& a, const Side<T>& x, const Side<T>& w,
-                    T* h, T* sg, T* su, bool fast, hipStream_t st) {
+                    T* h, bool fast, hipStream_t st) {
     const dim3 grid = grid_of(p.row_tiles * p.col_tiles * p.splits), block(64 * WR * WC);
     if (fast)
-        hipLaunchKernelGGL((forward_kernel<T, B, B, WR, WC, true>), grid, block, 0, st, p, a, x, w, h,
-                           sg, su);
+        hipLaunchKernelGGL((forward_kernel<T, B, B, WR, WC, true>), grid, block, 0, st, p, a, x, w, h);
     else
-        hipLaunchKernelGGL((forward_kernel<T, B, B, WR, WC, false>), grid, block, 0, st, p, a, x, w,
-                           h, sg, su);
+        hipLaunchKernelGGL((forward_kernel<T, B, B, WR, WC, false>), grid, block, 0, st, p, a, x, w, h);
 }
 
 template <class T>
 void run_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Side<T>& x,
-                 const Side<T>& w, T* h, T* sg, T* su, void* part, hipStream_t st) {
+                 const Side<T>& w, T* h, void* part, hipStream_t st) {
     const Cut c = cut_of(M, F, D, 1, int(sizeof(T)), true);
     const ProductShape p = shape(M, F, D, 1, c, c.tile / 2, part);
     const bool fast = direct(x, M, true) && direct(w, F, true);
-    if (c.tile == 256) launch_forward<T, 256, 2, 4>(p, a, x, w, h, sg, su, fast, st);
-    else if (c.tile == 128) launch_forward<T, 128, 2, 2>(p, a, x, w, h, sg, su, fast, st);
-    else launch_forward<T, 64, 2, 1>(p, a, x, w, h, sg, su, fast, st);
+    if (c.tile == 256) launch_forward<T, 256, 2, 4>(p, a, x, w, h, fast, st);
+    else if (c.tile == 128) launch_forward<T, 128, 2, 2>(p, a, x, w, h, fast, st);
+    else launch_forward<T, 64, 2, 1>(p, a, x, w, h, fast, st);
     if (c.splits > 1)
-        hipLaunchKernelGGL((forward_join_kernel<T>), join_grid(M * p.pitch / 4), dim3(256), 0, st, p, a,
-                           h, sg, su);
+        hipLaunchKernelGGL((forward_join_kernel<T>), join_grid(M * p.pitch / 4), dim3(256), 0, st, p, a, h);
 }
 
 // The backward call's workspace: the factors, then the parts of dx, then those
@@ -350,6 +366,13 @@ BackSpace back_space(int64_t M, int64_t D, int64_t F, int esize) {
 }  // namespace arp
 
 using namespace arp;
+
+static ar_status check_saved_dtype(int32_t dtype, int32_t saved, int32_t* esize) {
+    AR_TRY(check_dtype("saved_dtype", saved, esize));
+    if (saved != dtype && saved != AR_F32)
+        return fail(AR_ERR_UNSUPPORTED, "saved_dtype is dtype or AR_F32");
+    return AR_OK;
+}
 
 static ar_status check_glu_sizes(int64_t M, int64_t D, int64_t F) {
     AR_TRY(check_extent("M", M));
@@ -376,22 +399,23 @@ AR_EXPORT ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_
 AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_t D, int64_t F,
                                    const void* x, int64_t x_stride, const void* wg, const void* wu,
                                    int64_t w_stride, void* h, int64_t h_stride, void* saved_gate,
-                                   void* saved_up, int64_t saved_stride, void* workspace,
-                                   int64_t workspace_bytes, void* stream) {
+                                   void* saved_up, int64_t saved_stride, int32_t saved_dtype,
+                                   void* workspace, int64_t workspace_bytes, void* stream) {
     clear_error();
-    int32_t es = 0;
+    int32_t es = 0, ss = 0;
     int64_t need = 0;
     AR_TRY(check_dtype("dtype", dtype, &es));
     if (act != AR_ACT_SILU && act != AR_ACT_GELU)
         return fail(AR_ERR_INVALID_ARG, "unknown activation");
+    AR_TRY(check_saved_dtype(dtype, saved_dtype, &ss));
     AR_TRY(ar_glu_workspace(dtype, M, D, F, 0, &need));
     if (!saved_gate != !saved_up)
         return fail(AR_ERR_INVALID_ARG, "saved_gate and saved_up are given together");
     const int64_t sr = saved_gate ? M : 0;
     const MatArg mx{"x", x, M, D, x_stride, es}, mg{"wg", wg, F, D, w_stride, es},
         mu{"wu", wu, F, D, w_stride, es}, mh{"h", h, M, F, h_stride, es},
-        sg{"saved_gate", saved_gate, sr, F, saved_stride, es},
-        su{"saved_up", saved_up, sr, F, saved_stride, es},
+        sg{"saved_gate", saved_gate, sr, F, saved_stride, ss},
+        su{"saved_up", saved_up, sr, F, saved_stride, ss},
         mw{"the workspace", workspace, 1, need, need, 1};
     for (const MatArg& m : {mx, mg, mu, mh, sg, su}) AR_TRY(check_matrix(m));
     AR_TRY(check_workspace(workspace, workspace_bytes, need));
@@ -401,15 +425,13 @@ AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_
     for (const MatArg& o : {su, mw}) AR_TRY(check_apart(o, sg));
     AR_TRY(check_apart(mw, su));
     if (M == 0 || F == 0) return AR_OK;
-    const ForwardArgs a{h_stride, saved_stride, act};
+    const ForwardArgs a{h_stride, saved_stride, act, saved_gate, saved_up, saved_dtype == AR_F32};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     auto go = [&](auto zero) {
         using T = decltype(zero);
         const Side<T> sx{{static_cast<const T*>(x), static_cast<const T*>(x)}, x_stride},
             sw{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride};
-        T *const oh = static_cast<T*>(h), *const og = static_cast<T*>(saved_gate),
-                 *const ou = static_cast<T*>(saved_up);
-        run_forward<T>(a, M, D, F, sx, sw, oh, og, ou, workspace, st);
+        run_forward<T>(a, M, D, F, sx, sw, static_cast<T*>(h), workspace, st);
         return launch_status("gated feed-forward");
     };
     return dtype == AR_F32 ? go(float(0)) : go(uint16_t(0));
@@ -419,20 +441,22 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
                                     int64_t dh_stride, const void* x, int64_t x_stride,
                                     const void* wg, const void* wu, int64_t w_stride,
                                     const void* saved_gate, const void* saved_up,
-                                    int64_t saved_stride, int32_t accumulate, void* dx,
+                                    int64_t saved_stride, int32_t saved_dtype,
+                                    int32_t accumulate, void* dx,
                                     int64_t dx_stride, void* dwg, void* dwu, int64_t dw_stride,
                                     void* workspace, int64_t workspace_bytes, void* stream) {
     clear_error();
-    int32_t es = 0;
+    int32_t es = 0, ss = 0;
     int64_t need = 0;
     AR_TRY(check_dtype("dtype", dtype, &es));
+    AR_TRY(check_saved_dtype(dtype, saved_dtype, &ss));
     AR_TRY(ar_glu_workspace(dtype, M, D, F, 1, &need));
     if (!dwg != !dwu && F > 0 && D > 0)
         return fail(AR_ERR_INVALID_ARG, "dwg and dwu are given together");
     const MatArg mh{"dh", dh, M, F, dh_stride, es}, mx{"x", x, dwg ? M : 0, D, x_stride, es},
         mg{"wg", wg, dx ? F : 0, D, w_stride, es}, mu{"wu", wu, dx ? F : 0, D, w_stride, es},
-        sg{"saved_gate", saved_gate, M, F, saved_stride, es},
-        su{"saved_up", saved_up, M, F, saved_stride, es},
+        sg{"saved_gate", saved_gate, M, F, saved_stride, ss},
+        su{"saved_up", saved_up, M, F, saved_stride, ss},
         ox{"dx", dx, dx ? M : 0, D, dx_stride, es},
         og{"dwg", dwg, dwg ? F : 0, D, dw_stride, es}, ou{"dwu", dwu, dwg ? F : 0, D, dw_stride, es},
         mw{"the workspace", workspace, 1, need, need, 1};
@@ -450,12 +474,19 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
         const int64_t fs = factor_stride(F);
         T* const dg = static_cast<T*>(workspace);
         T* const du = dg + M * fs;
-        if (M > 0 && F > 0)
-            hipLaunchKernelGGL((factors_kernel<T>),
-                               dim3(unsigned(std::min<int64_t>(ceil_div(M * ceil_div(F, Num<T>::VEC), 256), 1 << 16))),
-                               dim3(256), 0, st, M, F, static_cast<const T*>(dh), dh_stride,
-                               static_cast<const T*>(saved_gate), static_cast<const T*>(saved_up),
+        auto factors = [&](auto saved) {
+            using S = decltype(saved);
+            const int64_t blocks = ceil_div(M * ceil_div(F, Num<T>::VEC), 256);
+            hipLaunchKernelGGL((factors_kernel<T, S>),
+                               dim3(unsigned(std::min<int64_t>(blocks, 1 << 16))), dim3(256), 0, st,
+                               M, F, static_cast<const T*>(dh), dh_stride,
+                               static_cast<const S*>(saved_gate), static_cast<const S*>(saved_up),
                                saved_stride, dg, du, fs);
+        };
+        if (M > 0 && F > 0) {
+            if (saved_dtype == AR_F32) factors(float(0));
+            else factors(T(0));
+        }
         const BackSpace space = back_space(M, D, F, es);
         char* const ws = static_cast<char*>(workspace);
         if (dx && M > 0) {

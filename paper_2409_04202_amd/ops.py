@@ -124,7 +124,8 @@ def embed_grad(dout, ids, dtable, scale=1.0, accumulate=False, workspace=None, s
 
 def glu_forward(x, wg, wu, act="silu", save=False, out=None, workspace=None, stream=None):
     """``act(x wg^T) * (x wu^T)`` for x (M, D) and wg, wu (F, D): (M, F).  With
-    ``save`` returns it and what ``glu_backward`` needs, a (2, M, F) tensor."""
+    ``save`` returns it and what ``glu_backward`` needs, a (2, M, F) tensor:
+    ``True`` in float32, a dtype (float32 or x's) in that."""
     sx = _matrix("x", x)
     M, D = x.shape
     sw = _matrix("wg", wg, None, x)
@@ -139,11 +140,14 @@ def glu_forward(x, wg, wu, act="silu", save=False, out=None, workspace=None, str
     with _on(x, stream, (x, wg, wu, out, workspace)) as s:
         h = torch.empty(M, F, dtype=x.dtype, device=x.device) if out is None else out
         sh = _matrix("out", h, (M, F), x)
-        saved = torch.empty(2, M, F, dtype=x.dtype, device=x.device) if save else None
+        kind = torch.float32 if save in (True, False, None) else save
+        if kind not in (torch.float32, x.dtype):
+            raise ValueError("save: True, float32 or x's type expected")
+        saved = torch.empty(2, M, F, dtype=kind, device=x.device) if save else None
         a, b = (saved[0], saved[1]) if save else (None, None)
         w, n, keep = _space(workspace, arplan.ar_glu_workspace(_DT[x.dtype], M, D, F, False), x)
         arplan.ar_glu_forward(_DT[x.dtype], act, M, D, F, x, sx, wg, wu, sw, h, sh, a, b,
-                              max(F, 1), w, n, s)
+                              max(F, 1), w, n, s, saved_dtype=_DT[kind])
     return (h, saved) if save else h
 
 
@@ -164,8 +168,10 @@ def glu_backward(dh, x, wg, wu, saved, dx=None, dwg=None, dwu=None, accumulate=F
     if (not isinstance(saved, torch.Tensor) or saved.dim() != 3 or saved.shape[0] != 2):
         raise ValueError("saved: what glu_forward saved expected")
     sg, su = saved[0], saved[1]
-    ss = _matrix("saved", sg, (M, F), dh)
-    if _matrix("saved", su, (M, F), dh) != ss:
+    if saved.dtype not in (torch.float32, dh.dtype) or saved.device != dh.device:
+        raise ValueError("saved: float32 or dh's type on dh's device expected")
+    ss = _matrix("saved", sg, (M, F))
+    if _matrix("saved", su, (M, F)) != ss:
         raise ValueError("saved: one row stride expected")
     if (dwg is None) != (dwu is None):
         raise ValueError("dwg and dwu are given together")
@@ -182,7 +188,8 @@ def glu_backward(dh, x, wg, wu, saved, dx=None, dwg=None, dwu=None, accumulate=F
             raise ValueError("dwg and dwu: one row stride expected")
         w, n, keep = _space(workspace, arplan.ar_glu_workspace(_DT[dh.dtype], M, D, F, True), dh)
         arplan.ar_glu_backward(_DT[dh.dtype], M, D, F, dh, sh, x, sx, wg, wu, sw, sg, su, ss,
-                               accumulate, dx, sdx, dwg, dwu, sdw, w, n, s)
+                               accumulate, dx, sdx, dwg, dwu, sdw, w, n, s,
+                               saved_dtype=_DT[saved.dtype])
     return dx, dwg, dwu
 
 

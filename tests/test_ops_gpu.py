@@ -217,6 +217,25 @@ def test_glu_many_tiles(M, D, F, dtype, layout):
     test_glu(M, D, F, dtype, "silu", layout)
 
 
+@pytest.mark.parametrize("M,D,F", [(65, 130, 129), (200, 4000, 70)])
+def test_glu_compact_factors(M, D, F):
+    """Factors saved in bf16, half of the memory: within the bound, which
+    allows them a rounding, and the same where nothing is rounded by it."""
+    x, wg = rnd(1, M, D, dtype="bf16"), rnd(2, F, D, dtype="bf16", scale=D ** -0.5)
+    wu, dh = rnd(3, F, D, dtype="bf16", scale=D ** -0.5), rnd(4, M, F, dtype="bf16")
+    want = ref.glu(x, wg, wu, "silu", dh, "bf16")
+    x, wg, wu, dh = (t.cuda() for t in (x, wg, wu, dh))
+    h, saved = ops.glu_forward(x, wg, wu, save=torch.bfloat16)
+    _, full = ops.glu_forward(x, wg, wu, save=True)
+    assert saved.dtype == torch.bfloat16 and full.dtype == torch.float32
+    assert torch.equal(saved, full.bfloat16())
+    got = (h,) + ops.glu_backward(dh, x, wg, wu, saved)
+    for name, g, w in zip(("h", "dx", "dwg", "dwu"), got, want):
+        ref.compare(name, g, *w)
+    for a, b in zip(ops.glu_backward(dh, x, wg, wu, saved.float()), got[1:]):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_glu_empty(dtype):
     dt = ref.TORCH[dtype]

@@ -110,6 +110,10 @@ def test_refusals_of_one_call():
     refuses(arplan.ar_glu_forward, FORWARD, INVALID, saved_up=None)
     refuses(arplan.ar_glu_forward, FORWARD, UNSUPPORTED, M=arplan.AR_GLU_MAX_EXTENT + 1)
     refuses(arplan.ar_glu_backward, BACKWARD, INVALID, dwu=None)
+    for f, args in ((arplan.ar_glu_forward, FORWARD), (arplan.ar_glu_backward, BACKWARD)):
+        refuses(f, args, UNSUPPORTED, saved_dtype="i32")
+        refuses(f, args, INVALID, saved_dtype=7)
+        refuses(f, dict(args, dtype="f32"), UNSUPPORTED, saved_dtype="bf16")
     refuses(arplan.ar_distill, DISTILL, UNSUPPORTED, K=arplan.AR_DISTILL_MAX_K + 1)
     for t in (0.0, -1.0, float("inf"), float("nan")):
         refuses(arplan.ar_distill, DISTILL, INVALID, temperature=t)
