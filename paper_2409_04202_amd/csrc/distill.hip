@@ -56,30 +56,6 @@ struct DistillArgs {
     float* at;                   // the student's logits at the entries, K a row
 };
 
-// Reductions over a wavefront, in the register file: after four shifts within
-// the rows of 16 lanes and two broadcasts from row to row lane 63 has them all.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float from_lane(float v, float none) {
-    return __uint_as_float(uint32_t(__builtin_amdgcn_update_dpp(
-        int(__float_as_uint(none)), int(__float_as_uint(v)), CTRL, ROWS, 0xF, false)));
-}
-template <class F>
-__device__ __forceinline__ float wave_reduce(float v, float none, F&& f) {
-    v = f(v, from_lane<0x111, 0xF>(v, none));
-    v = f(v, from_lane<0x112, 0xF>(v, none));
-    v = f(v, from_lane<0x114, 0xF>(v, none));
-    v = f(v, from_lane<0x118, 0xF>(v, none));
-    v = f(v, from_lane<0x142, 0xA>(v, none));
-    v = f(v, from_lane<0x143, 0xC>(v, none));
-    return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), 63)));
-}
-__device__ __forceinline__ float wave_sum(float v) {
-    return wave_reduce(v, 0.0f, [](float a, float b) { return a + b; });
-}
-__device__ __forceinline__ float wave_max(float v) {
-    return wave_reduce(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
-}
-
 // The sum of n parts.
 __device__ __forceinline__ PartSum join(const PartSum* part, int64_t n, float c) {
     PartSum all{-INFINITY, 0.0f};

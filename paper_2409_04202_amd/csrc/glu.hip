@@ -93,6 +93,94 @@ __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, F
     }
 }
 
+// Up to kFewRows rows of x: the weights pass once, so a wavefront takes whole
+// rows of them, two of each, its lanes side by side along D, and one
+// accumulator a (weight row, row of x).  Bound by memory: the weights' bytes
+// (beyond 8 rows the products would take longer than those).
+constexpr int kFewRows = 8;
+
+template <class T, int ROWS>
+__global__ __launch_bounds__(256) void few_rows_kernel(int64_t M, int64_t D, int64_t F,
+                                                       ForwardArgs a, Side<T> x, Side<T> w, T* h) {
+    constexpr int VEC = Num<T>::VEC, WIDE = ROWS <= 2 ? 4 : ROWS <= 4 ? 2 : 1;
+    const int lane = threadIdx.x & 63;
+    const int64_t f = (int64_t(blockIdx.x) * 4 + scalar(threadIdx.x >> 6)) * 2;
+    if (f >= F) return;
+    const int64_t next = f + 1 < F ? w.stride : 0;  // (an odd last row: twice)
+    const T* const wr[4] = {w.p[0] + f * w.stride, w.p[0] + f * w.stride + next,
+                            w.p[1] + f * w.stride, w.p[1] + f * w.stride + next};
+    const T* xr[ROWS];
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m) xr[m] = x.p[0] + (m < M ? m : M - 1) * x.stride;
+    float sum[4][ROWS] = {};
+    const int64_t whole = D / VEC * VEC;
+    auto multiply_add = [&](const u32x4* wv, const u32x4* xv) {
+        float a[4][VEC];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) Num<T>::unpack(wv[i], a[i]);
+#pragma unroll
+        for (int m = 0; m < ROWS; ++m) {
+            float b[VEC];
+            Num<T>::unpack(xv[m], b);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[i][m] = fmaf(a[i][e], b[e], sum[i][m]);
+        }
+    };
+    auto add = [&](int64_t d, auto load) {
+        u32x4 wv[4], xv[ROWS];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) wv[i] = load(wr[i] + d);
+#pragma unroll
+        for (int m = 0; m < ROWS; ++m) xv[m] = load(xr[m] + d);
+        multiply_add(wv, xv);
+    };
+    const auto vec = [](const T* p) { return load_vec(p); };
+    int64_t d = int64_t(lane) * VEC;
+    for (; d + (WIDE - 1) * 64 * VEC < whole; d += WIDE * 64 * VEC) {
+        u32x4 wv[WIDE][4], xv[WIDE][ROWS];
+#pragma unroll
+        for (int k = 0; k < WIDE; ++k) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) wv[k][i] = load_vec(wr[i] + d + k * 64 * VEC);
+#pragma unroll
+            for (int m = 0; m < ROWS; ++m) xv[k][m] = load_vec(xr[m] + d + k * 64 * VEC);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // all of them in flight
+#pragma unroll
+        for (int k = 0; k < WIDE; ++k) multiply_add(wv[k], xv[k]);
+    }
+    for (; d < whole; d += 64 * VEC) add(d, vec);
+    const int rest = int(D - whole);
+    if (rest && lane == 63) add(whole, [&](const T* p) { return load_part(p, rest); });
+    // (feature f, row m) to lane 2 m + (0 or 1)
+    float g = 0.0f, u = 0.0f;
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float sg = wave_sum(sum[i][m]), su = wave_sum(sum[2 + i][m]);
+            if (lane == 2 * m + i) {
+                g = sg;
+                u = su;
+            }
+        }
+    const int64_t m = lane >> 1, c = f + (lane & 1);
+    if (m >= M || m >= ROWS || c >= F) return;
+    float value, slope;
+    activate<T>(a.act, g, &value, &slope);
+    h[m * a.h_stride + c] = Num<T>::down(value * u);
+    const int64_t at = m * a.saved_stride + c;
+    if (a.sg && a.saved_f32) {
+        static_cast<float*>(a.sg)[at] = slope * u;
+        static_cast<float*>(a.su)[at] = value;
+    } else if (a.sg) {
+        static_cast<T*>(a.sg)[at] = Num<T>::down(slope * u);
+        static_cast<T*>(a.su)[at] = Num<T>::down(value);
+    }
+}
+
 // The sums of a product split along k, added in order, to its output.
 template <class T>
 __global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, ForwardArgs a, T* h) {
@@ -339,6 +427,18 @@ void launch_forward(const ProductShape& p, const ForwardArgs& a, const Side<T>& 
 template <class T>
 void run_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Side<T>& x,
                  const Side<T>& w, T* h, void* part, hipStream_t st) {
+    if (M <= kFewRows) {
+        const dim3 grid(unsigned(ceil_div(F, 8))), block(256);
+        auto go = [&](auto rows) {
+            hipLaunchKernelGGL((few_rows_kernel<T, decltype(rows)::value>), grid, block, 0, st, M, D,
+                               F, a, x, w, h);
+        };
+        if (M <= 1) go(std::integral_constant<int, 1>{});
+        else if (M <= 2) go(std::integral_constant<int, 2>{});
+        else if (M <= 4) go(std::integral_constant<int, 4>{});
+        else go(std::integral_constant<int, 8>{});
+        return;
+    }
     const Cut c = cut_of(M, F, D, 1, int(sizeof(T)), true);
     const ProductShape p = shape(M, F, D, 1, c, c.tile / 2, part);
     const bool fast = direct(x, M, true) && direct(w, F, true);
@@ -391,7 +491,7 @@ AR_EXPORT ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_
     int32_t es = 0;
     AR_TRY(check_dtype("dtype", dtype, &es));
     AR_TRY(check_glu_sizes(M, D, F));
-    *bytes = M == 0 || D == 0 || F == 0 ? 0 : part_bytes(cut_of(M, F, D, 1, es, true), M, F, 2);
+    *bytes = M <= kFewRows || D == 0 || F == 0 ? 0 : part_bytes(cut_of(M, F, D, 1, es, true), M, F, 2);
     if (backward) *bytes = std::max(*bytes, back_space(M, D, F, es).end);
     return AR_OK;
 }

@@ -115,4 +115,28 @@ __device__ __forceinline__ void store_part(T* p, const u32x4 v, int n) {
         if (i < n) ((AR_GLOBAL T*)p)[i] = Num<T>::down(f[i]);
 }
 
+// Reductions over a wavefront, in the register file: after four shifts within
+// the rows of 16 lanes and two broadcasts from row to row lane 63 has them all.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float from_lane(float v, float none) {
+    return __uint_as_float(uint32_t(__builtin_amdgcn_update_dpp(
+        int(__float_as_uint(none)), int(__float_as_uint(v)), CTRL, ROWS, 0xF, false)));
+}
+template <class F>
+__device__ __forceinline__ float wave_reduce(float v, float none, F&& f) {
+    v = f(v, from_lane<0x111, 0xF>(v, none));
+    v = f(v, from_lane<0x112, 0xF>(v, none));
+    v = f(v, from_lane<0x114, 0xF>(v, none));
+    v = f(v, from_lane<0x118, 0xF>(v, none));
+    v = f(v, from_lane<0x142, 0xA>(v, none));
+    v = f(v, from_lane<0x143, 0xC>(v, none));
+    return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), 63)));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    return wave_reduce(v, 0.0f, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v) {
+    return wave_reduce(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+}
+
 }  // namespace arp
