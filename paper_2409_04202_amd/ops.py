@@ -21,8 +21,6 @@ Wrong shapes, types or devices raise ValueError; what the library refuses
 raises ``arplan.ArError``.
 """
 
-import contextlib
-
 import torch
 
 from . import arplan
@@ -55,19 +53,33 @@ def _ids(name, ids, like):
         raise ValueError("%s: an int64 tensor on the operands' device expected" % name)
 
 
-@contextlib.contextmanager
-def _on(like, stream, tensors):
-    """The stream a call runs on; its allocations are made there, and the
-    tensors it is given are marked as used there."""
-    with torch.cuda.device(like.device):
-        if stream is None or stream == torch.cuda.current_stream():
-            yield torch.cuda.current_stream().cuda_stream
-            return
-        with torch.cuda.stream(stream):
-            yield stream.cuda_stream
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+class _on:
+    """The stream a call runs on, as a handle: its allocations are made there,
+    and the tensors it is given are marked as used there."""
+
+    __slots__ = ("like", "stream", "tensors", "entered")
+
+    def __init__(self, like, stream, tensors):
+        self.like, self.stream, self.tensors, self.entered = like, stream, tensors, ()
+
+    def __enter__(self):
+        if self.stream is None:
+            if self.like.device.index != torch.cuda.current_device():
+                self.entered = (torch.cuda.device(self.like.device),)
+                self.entered[0].__enter__()
+            return torch.cuda.current_stream().cuda_stream
+        self.entered = (torch.cuda.device(self.like.device), torch.cuda.stream(self.stream))
+        for e in self.entered:
+            e.__enter__()
+        return self.stream.cuda_stream
+
+    def __exit__(self, *exc):
+        for e in reversed(self.entered):
+            e.__exit__(*exc)
+        if self.stream is not None:
+            for t in self.tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
 
 
 def _space(workspace, need, like):
