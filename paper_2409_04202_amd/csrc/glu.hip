@@ -181,6 +181,19 @@ __global__ __launch_bounds__(256) void few_rows_kernel(int64_t M, int64_t D, int
     }
 }
 
+// Four values to adjacent elements, of which n are there.
+template <class T>
+__device__ __forceinline__ void store_four(T* p, const float* v, int64_t n) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+    if (n < 4) {
+        for (int e = 0; e < int(n); ++e) p[e] = Num<T>::down(v[e]);
+    } else if constexpr (sizeof(T) == 4) {
+        store_vec(p, Num<T>::pack(v));
+    } else {
+        *(AR_GLOBAL u32x2*)p = u32x2{bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3])};
+    }
+}
+
 // The sums of a product split along k, added in order, to its output.
 template <class T>
 __global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, ForwardArgs a, T* h) {
@@ -198,20 +211,21 @@ __global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, Forwa
                 u[e] += y[e];
             }
         }
+        float value[4], slope[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (c + e >= p.cols) continue;
-            float value, slope;
-            activate<T>(a.act, g[e], &value, &slope);
-            h[r * a.h_stride + c + e] = Num<T>::down(value * u[e]);
-            const int64_t at = r * a.saved_stride + c + e;
-            if (a.sg && a.saved_f32) {
-                static_cast<float*>(a.sg)[at] = slope * u[e];
-                static_cast<float*>(a.su)[at] = value;
-            } else if (a.sg) {
-                static_cast<T*>(a.sg)[at] = Num<T>::down(slope * u[e]);
-                static_cast<T*>(a.su)[at] = Num<T>::down(value);
-            }
+            activate<T>(a.act, g[e], &value[e], &slope[e]);
+            slope[e] *= u[e];
+            g[e] = value[e] * u[e];
+        }
+        const int64_t left = p.cols - c, at = r * a.saved_stride + c;
+        store_four(h + r * a.h_stride + c, g, left);
+        if (a.sg && a.saved_f32) {
+            store_four(static_cast<float*>(a.sg) + at, slope, left);
+            store_four(static_cast<float*>(a.su) + at, value, left);
+        } else if (a.sg) {
+            store_four(static_cast<T*>(a.sg) + at, slope, left);
+            store_four(static_cast<T*>(a.su) + at, value, left);
         }
     }
 }
@@ -285,8 +299,8 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductShape p, P
     P::run(p, second ? a.r[1] : a.r[0], a.l, rt * BR, ct * BC, split, (AR_LDS char*)lds, acc);
     const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
     AR_LDS float* const part = (AR_LDS float*)((AR_LDS char*)lds + wave * S::BYTES);
-    const int rshift = DIRECT && !RKC ? int((VEC - p.rows % VEC) % VEC) : 0,
-              cshift = DIRECT ? int((VEC - p.cols % VEC) % VEC) : 0;
+    const int rshift = DIRECT && !RKC ? int((VEC - a.r[0].extent % VEC) % VEC) : 0,
+              cshift = DIRECT ? int((VEC - a.l.extent % VEC) % VEC) : 0;
 #pragma unroll
     for (int i = 0; i < P::SR; ++i) {
         S::fill(part, [&](int j, int e) { return acc[i][j][e]; });
@@ -316,9 +330,12 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductShape p, Produ
             for (int e = 0; e < 4; ++e) v[e] += x[e];
         }
         T* const at = (second ? a.out[1] : a.out[0]) + r * a.stride + c;
+        if (a.accumulate) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (c + e < p.cols) at[e] = Num<T>::down(a.accumulate ? Num<T>::up(at[e]) + v[e] : v[e]);
+            for (int e = 0; e < 4; ++e)
+                if (c + e < p.cols) v[e] += Num<T>::up(at[e]);
+        }
+        store_four(at, v, p.cols - c);
     }
 }
 
@@ -326,14 +343,14 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductShape p, Produ
 // places (fp32: at any element), within 32-bit offsets of the tile's first row,
 // and, K-major, at least one chunk a row (fp32) or whole ones (bf16).
 template <class T>
-bool direct(const Side<T>& s, int64_t extent, bool kc) {
+bool direct(const Side<T>& s, bool kc) {
     constexpr int VEC = Num<T>::VEC;
     if (s.stride * int64_t(sizeof(T)) > (int64_t(1) << 22)) return false;
     if (sizeof(T) == 2 &&
         (s.stride % VEC ||
          (reinterpret_cast<uintptr_t>(s.p[0]) | reinterpret_cast<uintptr_t>(s.p[1])) % kChunk))
         return false;
-    return kc || (sizeof(T) == 4 ? extent >= VEC : extent % VEC == 0);
+    return kc || (sizeof(T) == 4 ? s.extent >= VEC : s.extent % VEC == 0);
 }
 
 int64_t factor_stride(int64_t F) { return round_up(F, 8); }
@@ -346,10 +363,11 @@ struct Cut {
     int tile, splits;
 };
 
-constexpr double kCuFlops[2][3] = {
-    // 64, 128, 256, in 1e12 a second
-    {0.45, 0.54, 0.54},  // fp32
-    {1.7, 3.4, 4.3},     // bf16
+constexpr double kCuFlops[2][4] = {
+    // 64, 128, 256, and 64 of the gated product (two wavefronts a block), in
+    // 1e12 a second
+    {0.45, 0.54, 0.54, 0.34},  // fp32
+    {1.7, 3.4, 4.6, 1.4},      // bf16
 };
 
 Cut cut_of(int64_t rows, int64_t cols, int64_t K, int outputs, int esize, bool gated) {
@@ -358,7 +376,8 @@ Cut cut_of(int64_t rows, int64_t cols, int64_t K, int outputs, int esize, bool g
     for (int i = 0; i < 3; ++i) {
         const int tile = 64 << i;
         const int64_t tiles = ceil_div(rows, tile) * ceil_div(cols, gated ? tile / 2 : tile) * outputs;
-        const double one = 2.0 * tile * tile * double(K) / (kCuFlops[esize == 2][i] * 1e12);
+        const double one = 2.0 * tile * tile * double(K) /
+                           (kCuFlops[esize == 2][gated && i == 0 ? 3 : i] * 1e12);
         for (int s = 1; s <= 16; s *= 2) {
             if (s > 1 && K / s < 4 * (kStepBytes / esize)) break;
             double t = double(ceil_div(tiles * s, 256)) * (one / s + 1.5e-6);
@@ -404,8 +423,8 @@ void run_product(int64_t rows, int64_t cols, int64_t K, int segments, const Prod
                  void* part, hipStream_t st) {
     const Cut c = cut_of(rows, cols, K * segments, a.count, int(sizeof(T)), false);
     const ProductShape p = shape(rows, cols, K, segments, c, c.tile, part);
-    bool fast = direct(a.l, cols, false);
-    for (int i = 0; i < a.count; ++i) fast = fast && direct(a.r[i], rows, RKC);
+    bool fast = direct(a.l, false);
+    for (int i = 0; i < a.count; ++i) fast = fast && direct(a.r[i], RKC);
     if (c.tile == 256) launch_product<T, RKC, 256, 2, 4>(p, a, fast, st);
     else if (c.tile == 128) launch_product<T, RKC, 128, 2, 2>(p, a, fast, st);
     else launch_product<T, RKC, 64, 2, 2>(p, a, fast, st);
@@ -441,7 +460,7 @@ void run_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Si
     }
     const Cut c = cut_of(M, F, D, 1, int(sizeof(T)), true);
     const ProductShape p = shape(M, F, D, 1, c, c.tile / 2, part);
-    const bool fast = direct(x, M, true) && direct(w, F, true);
+    const bool fast = direct(x, true) && direct(w, true);
     if (c.tile == 256) launch_forward<T, 256, 2, 4>(p, a, x, w, h, fast, st);
     else if (c.tile == 128) launch_forward<T, 128, 2, 2>(p, a, x, w, h, fast, st);
     else launch_forward<T, 64, 2, 1>(p, a, x, w, h, fast, st);
@@ -449,16 +468,62 @@ void run_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Si
         hipLaunchKernelGGL((forward_join_kernel<T>), join_grid(M * p.pitch / 4), dim3(256), 0, st, p, a, h);
 }
 
-// The backward call's workspace: the factors, then the parts of dx, then those
-// of dwg and dwu.
+// bf16 rows that do not lie at 16 bytes cannot be copied straight to LDS: x and
+// the weights are laid out once more, in rows of whole vectors, where the widths
+// say so and the products are long enough to pay for it (6000 x 2051 x 5465:
+// forward 423 -> 374 us; 1531 rows of it: forward 168 -> 163, backward 707 -> 298).
+template <class T>
+__global__ __launch_bounds__(256) void pack_kernel(int64_t rows, int64_t cols, const T* from,
+                                                   int64_t stride, T* to, int64_t pitch) {
+    constexpr int VEC = Num<T>::VEC;
+    const int64_t per = pitch / VEC, step = int64_t(gridDim.x) * 256;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < rows * per; i += step) {
+        const int64_t r = i / per, c = i % per * VEC, left = cols - c;
+        const T* const p = from + r * stride + c;
+        store_vec(to + r * pitch + c, left >= VEC ? load_vec(p) : load_part(p, int(left)));
+    }
+}
+
+bool packs(int64_t M, int64_t D, int64_t F, int esize) {
+    return esize == 2 && D % 8 && double(M) * double(D) * double(F) > 5e8;
+}
+int64_t pack_bytes(int64_t M, int64_t D, int64_t F, int esize) {
+    return packs(M, D, F, esize) ? round_up((M + 2 * F) * round_up(D, 8) * esize, 256) : 0;
+}
+// Replaces x and w by their copies in `space`.
+template <class T>
+void pack(int64_t M, int64_t D, int64_t F, Side<T>* x, Side<T>* w, void* space, hipStream_t st) {
+    const int64_t pitch = round_up(D, 8);
+    T* to = static_cast<T*>(space);
+    auto one = [&](const T* from, int64_t rows, int64_t stride) {
+        hipLaunchKernelGGL((pack_kernel<T>), join_grid(rows * pitch / Num<T>::VEC), dim3(256), 0, st, rows,
+                           D, from, stride, to, pitch);
+        T* const at = to;
+        to += rows * pitch;
+        return at;
+    };
+    if (x && x->p[0]) {
+        const T* const px = one(x->p[0], M, x->stride);
+        *x = Side<T>{{px, px}, pitch, pitch};
+    }
+    if (w && w->p[0]) {
+        const T* const pg = one(w->p[0], F, w->stride);
+        const T* const pu = one(w->p[1], F, w->stride);
+        *w = Side<T>{{pg, pu}, pitch, pitch};
+    }
+}
+
+// The backward call's workspace: the factors, the parts of dx, those of dwg and
+// dwu, and x and the weights laid out anew.
 struct BackSpace {
-    int64_t dx, dw, end;
+    int64_t dx, dw, packed, end;
 };
 BackSpace back_space(int64_t M, int64_t D, int64_t F, int esize) {
     BackSpace b{};
     b.dx = round_up(2 * M * factor_stride(F) * esize, 256);
     b.dw = b.dx + part_bytes(cut_of(M, D, 2 * F, 1, esize, false), M, D, 1);
-    b.end = b.dw + part_bytes(cut_of(F, D, M, 2, esize, false), F, D, 2);
+    b.packed = b.dw + part_bytes(cut_of(F, D, M, 2, esize, false), F, D, 2);
+    b.end = b.packed + pack_bytes(M, D, F, esize);
     return b;
 }
 
@@ -491,7 +556,9 @@ AR_EXPORT ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_
     int32_t es = 0;
     AR_TRY(check_dtype("dtype", dtype, &es));
     AR_TRY(check_glu_sizes(M, D, F));
-    *bytes = M <= kFewRows || D == 0 || F == 0 ? 0 : part_bytes(cut_of(M, F, D, 1, es, true), M, F, 2);
+    *bytes = M <= kFewRows || D == 0 || F == 0
+                 ? 0
+                 : part_bytes(cut_of(M, F, D, 1, es, true), M, F, 2) + pack_bytes(M, D, F, es);
     if (backward) *bytes = std::max(*bytes, back_space(M, D, F, es).end);
     return AR_OK;
 }
@@ -529,8 +596,11 @@ AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_
     const hipStream_t st = static_cast<hipStream_t>(stream);
     auto go = [&](auto zero) {
         using T = decltype(zero);
-        const Side<T> sx{{static_cast<const T*>(x), static_cast<const T*>(x)}, x_stride},
-            sw{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride};
+        Side<T> sx{{static_cast<const T*>(x), static_cast<const T*>(x)}, x_stride, D},
+            sw{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride, D};
+        if (M > kFewRows && packs(M, D, F, es) && !(direct(sx, true) && direct(sw, true)))
+            pack<T>(M, D, F, &sx, &sw,
+                    static_cast<char*>(workspace) + part_bytes(cut_of(M, F, D, 1, es, true), M, F, 2), st);
         run_forward<T>(a, M, D, F, sx, sw, static_cast<T*>(h), workspace, st);
         return launch_status("gated feed-forward");
     };
@@ -589,22 +659,22 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
         }
         const BackSpace space = back_space(M, D, F, es);
         char* const ws = static_cast<char*>(workspace);
-        if (dx && M > 0) {
-            const Side<T> r{{dg, du}, fs},
-                l{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride};
+        Side<T> sx{{static_cast<const T*>(x), static_cast<const T*>(x)}, x_stride, D},
+            sw{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride, D};
+        if (packs(M, D, F, es))
+            pack<T>(M, D, F, dwg && !direct(sx, false) ? &sx : nullptr,
+                    dx && !direct(sw, false) ? &sw : nullptr, ws + space.packed, st);
+        const Side<T> sg{{dg, du}, fs, fs};
+        if (dx && M > 0)
             run_product<T, true>(M, D, F, 2,
-                                 Products<T>{{r, r}, l, {static_cast<T*>(dx), nullptr}, dx_stride, 1, 0},
+                                 Products<T>{{sg, sg}, sw, {static_cast<T*>(dx), nullptr}, dx_stride, 1, 0},
                                  ws + space.dx, st);
-        }
-        if (dwg && F > 0) {
-            const T* const px = static_cast<const T*>(x);
+        if (dwg && F > 0)
             run_product<T, false>(F, D, M, 1,
-                                  Products<T>{{Side<T>{{dg, dg}, fs}, Side<T>{{du, du}, fs}},
-                                              Side<T>{{px, px}, x_stride},
-                                              {static_cast<T*>(dwg), static_cast<T*>(dwu)},
+                                  Products<T>{{Side<T>{{dg, dg}, fs, fs}, Side<T>{{du, du}, fs, fs}},
+                                              sx, {static_cast<T*>(dwg), static_cast<T*>(dwu)},
                                               dw_stride, 2, accumulate},
                                   ws + space.dw, st);
-        }
         return launch_status("gated feed-forward gradients");
     };
     return dtype == AR_F32 ? go(float(0)) : go(uint16_t(0));

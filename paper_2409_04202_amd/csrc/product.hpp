@@ -51,6 +51,7 @@ template <class T>
 struct Side {
     const T* p[2];
     int64_t stride;
+    int64_t extent;  // K-major: the rows' elements in memory, at least the product's
 };
 
 struct ProductShape {
@@ -291,8 +292,8 @@ struct Tile {
                                                const Side<T>& L, int64_t r0, int64_t c0, int split,
                                                AR_LDS char* lds, f32x16 (&acc)[SR][SC]) {
         const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
-        const RP rp(R, r0, p.rows);
-        const LP lp(L, c0, p.cols);
+        const RP rp(R, r0, RKC ? p.rows : R.extent);
+        const LP lp(L, c0, LKC ? p.cols : L.extent);
         const Frags<T, BR, RKC> rf(wr * SR * 32);
         const Frags<T, BC, LKC> lf(wc * (GATED ? 32 : SC * 32));
         constexpr int KS = StepOf<T>::K;
