@@ -4,7 +4,7 @@ Run ``python -m paper_2409_04202_amd.build`` (or ``__graft_entry__.build()``).
 The plan library and the C ABI (plan.cpp, capi.cpp) are compiled with the
 host compiler; the executor (exec.hip, and its host-side planning in
 rewrite.cpp, schedule.cpp, programs.cpp and onepass.cpp, which share its HIP types) and the
-replica operators (embed.hip, distill.hip, glu.hip, their checks in replica.cpp) with
+replica operators (``replica/``: embed.hip, distill.hip, glu.hip, their checks) with
 ``hipcc --offload-arch=gfx950``; hipcc links the shared library.  The
 objects are compiled in parallel and always from scratch.
 
@@ -34,7 +34,7 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 HOST_SRCS = ["plan.cpp", "capi.cpp", "genmodel.cpp"]
 HIP_SRCS = ["exec.hip", "rewrite.cpp", "schedule.cpp", "programs.cpp", "onepass.cpp",
-            "replica.cpp", "embed.hip", "distill.hip", "glu.hip"]
+            "replica/checks.cpp", "replica/embed.hip", "replica/distill.hip", "replica/glu.hip"]
 CHECK_SRCS = ["debug.cpp"]          # compiled as HIP, linked into the check library only
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall",
@@ -67,11 +67,11 @@ def build(verbose=False, jobs=None):
     try:
         cmds, objs = [], {}
         for s in HOST_SRCS:
-            o = os.path.join(tmp, s + ".o")
+            o = os.path.join(tmp, s.replace("/", "_") + ".o")
             cmds.append([cxx, "-c", os.path.join(CSRC, s), "-o", o] + COMMON)
             objs[s] = o
         for s in HIP_SRCS + CHECK_SRCS:
-            o = os.path.join(tmp, s + ".o")
+            o = os.path.join(tmp, s.replace("/", "_") + ".o")
             cmds.append([hipcc, "-c", "-x", "hip", os.path.join(CSRC, s), "-o", o]
                         + COMMON + HIP_FLAGS)
             objs[s] = o
@@ -121,11 +121,11 @@ def build_sanitized(verbose=False, jobs=None):
     try:
         cmds, objs = [], []
         for s in HOST_SRCS:
-            o = os.path.join(tmp, s + ".o")
+            o = os.path.join(tmp, s.replace("/", "_") + ".o")
             cmds.append([clang, "-c", os.path.join(CSRC, s), "-o", o] + SAN_COMMON + SAN)
             objs.append(o)
         for s in HIP_SRCS + CHECK_SRCS:
-            o = os.path.join(tmp, s + ".o")
+            o = os.path.join(tmp, s.replace("/", "_") + ".o")
             cmds.append([hipcc, "-c", "-x", "hip", os.path.join(CSRC, s), "-o", o]
                         + SAN_COMMON + HIP_FLAGS + host_san)
             objs.append(o)

@@ -8,8 +8,8 @@
 #include <cstdint>
 #include <string>
 
-#include "internal.hpp"
-#include "kernels.hpp"
+#include "../internal.hpp"
+#include "../kernels.hpp"
 
 namespace arp {
 
