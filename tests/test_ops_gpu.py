@@ -446,6 +446,21 @@ def test_distill_far_rows():
     ref.compare("gradient", g, grad, eg)
 
 
+def test_distill_more_rows_than_a_pair_of_launches():
+    """Long rows, over 4 GiB of them: every copy of a row has its bits."""
+    T, V, K, copies = 5, (1 << 20) + 3, 7, 206
+    z = rnd(1, T, V, scale=3.0)
+    ids, tea = teacher_of(2, T, V, K)
+    (loss, el), (grad, eg) = ref.distill(z, tea, ids, 2.0, None, "f32")
+    big = z.cuda().repeat(copies, 1)
+    got, g = ops.distill(big, tea.cuda().repeat(copies, 1), ids.cuda().repeat(copies, 1),
+                         temperature=2.0, grad=big)
+    ref.compare("loss", got[-T:], loss, el)
+    ref.compare("gradient", g[-T:], grad, eg)
+    assert torch.equal(got.view(copies, T), got[:T].expand(copies, T))
+    assert all(torch.equal(g[i:i + T], g[:T]) for i in range(0, copies * T, T))
+
+
 # ------------------------------------------------------ streams and graphs
 
 def _pass(dtype="bf16"):
