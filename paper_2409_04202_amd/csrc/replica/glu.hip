@@ -47,12 +47,18 @@ struct ForwardArgs {
     bool saved_f32;
 };
 
+// Where the sums of a part of a tile (rows x cols) are.
+__device__ __forceinline__ int64_t part_at(const ProductShape& p, int64_t tile, int split, int rows,
+                                           int cols) {
+    return ((tile - p.whole) * p.splits + split) * (int64_t(rows) * cols);
+}
+
 // h, and the saved factors where they are wanted, of a tile; or, split along k,
 // the tile's sums of g and of u.  A panel holds rows of both weights, so that a
 // lane has g and u of the same element and the activation is its epilogue.
 // Bound by the matrix cores and the copies' issue: 2048 x 4096 x 16384 bf16 469
 // us, 1172 TFLOP/s; 8192 rows with the factors saved 1.9 ms; 777 x 1003 x 2731
-// fp32 111 us, 77 TFLOP/s, and its join 12.
+// fp32 103 us, 83 TFLOP/s, and its join 6.
 template <class T, int BR, int BC, int WR, int WC, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, ForwardArgs a,
                                                                Side<T> x, Side<T> w, T* h) {
@@ -60,28 +66,34 @@ __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, F
     using S = Store<1>;
     constexpr int LDS = P::LDS > WR * WC * S::BYTES ? P::LDS : WR * WC * S::BYTES;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
-    const int64_t tiles = p.row_tiles * p.col_tiles;
-    int64_t t, rt, ct;
-    if (!tile_of(p, tiles * p.splits, blockIdx.x, &t)) return;
-    const int split = int(t / tiles);
-    place_of(p, t % tiles, &rt, &ct);
+    Unit unit;
+    int64_t rt, ct;
+    if (!unit_of(p, blockIdx.x, &unit)) return;
+    place_of(p, unit.tile, &rt, &ct);
     f32x16 acc[P::SR][2] = {};
-    P::run(p, x, w, rt * BR, ct * (BC / 2), split, (AR_LDS char*)lds, acc);
+    P::run(p, x, w, rt * BR, ct * (BC / 2), unit, (AR_LDS char*)lds, acc);
     const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
     AR_LDS float* const part = (AR_LDS float*)((AR_LDS char*)lds + wave * S::BYTES);
 #pragma unroll
     for (int i = 0; i < P::SR; ++i) {
-        const int64_t r0 = rt * BR + (wr * P::SR + i) * 32, c0 = ct * (BC / 2) + wc * 32;
+        const int64_t tr = (wr * P::SR + i) * 32, tc = wc * 32;  // within the tile
+        const int64_t r0 = rt * BR + tr, c0 = ct * (BC / 2) + tc;
         auto pass = [&](auto* out, int64_t stride, auto f) {
             S::fill(part, f);
             wave_sync();
             S::store(part, out, stride, r0, p.rows, c0, p.cols, false, 0, 0, 0, 0);
             wave_sync();
         };
-        if (p.splits > 1) {
-            float* const to = p.part + int64_t(split) * 2 * p.rows * p.pitch;
-            pass(to, p.pitch, [&](int, int e) { return acc[i][0][e]; });
-            pass(to + p.rows * p.pitch, p.pitch, [&](int, int e) { return acc[i][1][e]; });
+        if (unit.splits > 1) {  // g on the left, u on the right
+            float* const to = p.part + part_at(p, unit.tile, unit.split, BR, BC);
+            auto sums = [&](int j) {
+                S::fill(part, [&](int, int e) { return acc[i][j][e]; });
+                wave_sync();
+                S::store(part, to, BC, tr, BR, tc + j * (BC / 2), BC, false, 0, 0, 0, 0);
+                wave_sync();
+            };
+            sums(0);
+            sums(1);
             continue;
         }
         float value[16], slope[16];
@@ -201,17 +213,25 @@ __device__ __forceinline__ void store_four(T* p, const float* v, int64_t n) {
     }
 }
 
-// The sums of a product split along k, added in order, to its output.
+// The sums of the tiles that are split along k, added in order, to the output:
+// `rows` of a tile and `cols` of the output in it are powers of two.
 template <class T>
-__global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, ForwardArgs a, T* h) {
-    const int64_t per = p.pitch / 4, step = int64_t(gridDim.x) * 256, one = p.rows * p.pitch;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < p.rows * per; i += step) {
-        const int64_t r = i / per, c = i % per * 4;
+__global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, ForwardArgs a, T* h,
+                                                           int rows, int cols) {
+    const int64_t rest = (p.tiles - p.whole) * rows * (cols / 4), step = int64_t(gridDim.x) * 256;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < rest; i += step) {
+        const int n = int(i & (rows * (cols / 4) - 1)), tr = n / (cols / 4), tc = n % (cols / 4) * 4;
+        const int64_t tile = p.whole + i / (rows * (cols / 4));
+        int64_t rt, ct;
+        place_of(p, tile, &rt, &ct);
+        const int64_t r = rt * rows + tr, c = ct * cols + tc;
+        if (r >= p.rows || c >= p.cols) continue;
         float g[4] = {}, u[4] = {};
         for (int s = 0; s < p.splits; ++s) {
+            const float* const from = p.part + part_at(p, tile, s, rows, 2 * cols) + tr * (2 * cols) + tc;
             float x[4], y[4];
-            Num<float>::unpack(load_vec(p.part + 2 * s * one + r * p.pitch + c), x);
-            Num<float>::unpack(load_vec(p.part + (2 * s + 1) * one + r * p.pitch + c), y);
+            Num<float>::unpack(load_vec(from), x);
+            Num<float>::unpack(load_vec(from + cols), y);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 g[e] += x[e];
@@ -300,14 +320,13 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductShape p, P
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     constexpr int VEC = Num<T>::VEC;
     const int64_t tiles = p.row_tiles * p.col_tiles;
-    int64_t t, rt, ct;
-    if (!tile_of(p, tiles * p.splits * a.count, blockIdx.x, &t)) return;
-    const bool second = t >= tiles * p.splits;
-    if (second) t -= tiles * p.splits;
-    const int split = int(t / tiles);
-    place_of(p, t % tiles, &rt, &ct);
+    Unit unit;
+    int64_t rt, ct;
+    if (!unit_of(p, blockIdx.x, &unit)) return;
+    const bool second = unit.tile >= tiles;
+    place_of(p, second ? unit.tile - tiles : unit.tile, &rt, &ct);
     f32x16 acc[P::SR][P::SC] = {};
-    P::run(p, second ? a.r[1] : a.r[0], a.l, rt * BR, ct * BC, split, (AR_LDS char*)lds, acc);
+    P::run(p, second ? a.r[1] : a.r[0], a.l, rt * BR, ct * BC, unit, (AR_LDS char*)lds, acc);
     const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
     AR_LDS float* const part = (AR_LDS float*)((AR_LDS char*)lds + wave * S::BYTES);
     const int rshift = DIRECT && !RKC ? int((VEC - a.r[0].extent % VEC) % VEC) : 0,
@@ -316,10 +335,13 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductShape p, P
     for (int i = 0; i < P::SR; ++i) {
         S::fill(part, [&](int j, int e) { return acc[i][j][e]; });
         wave_sync();
-        const int64_t r0 = rt * BR + (wr * P::SR + i) * 32, c0 = ct * BC + wc * P::SC * 32;
-        if (p.splits > 1)
-            S::store(part, p.part + (int64_t(split) * a.count + second) * p.rows * p.pitch, p.pitch,
-                     r0, p.rows, c0, p.cols, false, VEC, rshift, VEC, cshift);
+        const int64_t tr = (wr * P::SR + i) * 32, tc = wc * P::SC * 32;  // within the tile
+        const int64_t r0 = rt * BR + tr, c0 = ct * BC + tc;
+        if (unit.splits > 1)
+            S::store(part, p.part + part_at(p, unit.tile, unit.split, BR, BC), BC, tr,
+                     p.rows - rt * BR < BR ? p.rows - rt * BR : BR, tc,
+                     p.cols - ct * BC < BC ? p.cols - ct * BC : BC, false, VEC,
+                     rt + 1 == p.row_tiles ? rshift : 0, VEC, ct + 1 == p.col_tiles ? cshift : 0);
         else
             S::store(part, second ? a.out[1] : a.out[0], a.stride, r0, p.rows, c0, p.cols,
                      a.accumulate, VEC, rshift, VEC, cshift);
@@ -328,15 +350,22 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductShape p, P
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void product_join_kernel(ProductShape p, Products<T> a) {
-    const int64_t per = p.pitch / 4, step = int64_t(gridDim.x) * 256, one = p.rows * p.pitch;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < p.rows * per * a.count; i += step) {
-        const bool second = i >= p.rows * per;
-        const int64_t j = second ? i - p.rows * per : i, r = j / per, c = j % per * 4;
+__global__ __launch_bounds__(256) void product_join_kernel(ProductShape p, Products<T> a, int rows,
+                                                           int cols) {
+    const int64_t rest = (p.tiles - p.whole) * rows * (cols / 4), step = int64_t(gridDim.x) * 256;
+    const int64_t tiles = p.row_tiles * p.col_tiles;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < rest; i += step) {
+        const int n = int(i & (rows * (cols / 4) - 1)), tr = n / (cols / 4), tc = n % (cols / 4) * 4;
+        const int64_t tile = p.whole + i / (rows * (cols / 4));
+        const bool second = tile >= tiles;
+        int64_t rt, ct;
+        place_of(p, second ? tile - tiles : tile, &rt, &ct);
+        const int64_t r = rt * rows + tr, c = ct * cols + tc;
+        if (r >= p.rows || c >= p.cols) continue;
         float v[4] = {};
         for (int s = 0; s < p.splits; ++s) {
             float x[4];
-            Num<float>::unpack(load_vec(p.part + (s * a.count + second) * one + r * p.pitch + c), x);
+            Num<float>::unpack(load_vec(p.part + part_at(p, tile, s, rows, cols) + tr * cols + tc), x);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] += x[e];
         }
@@ -366,13 +395,18 @@ bool direct(const Side<T>& s, bool kc) {
 
 int64_t factor_stride(int64_t F) { return round_up(F, 8); }
 
-// How a product is cut: square tiles of 256, 128 or 64, and parts along k.
-// The time is estimated as the most that one of the 256 CUs gets, at a rate a CU
+// How a product is cut: square tiles of 256, 128 or 64, and parts along k, of all
+// tiles or of those that are left after whole rounds of the 256 CUs.
+// The time is estimated as the most that one of the CUs gets, at a rate a CU
 // that grows with the tile (a larger tile reads less from LDS for its
 // products), and, where k is split, the parts' way through memory and a launch.
-// The rates are those of long products that were given each tile in turn.
+// The rates are those of long products that were given each tile in turn.  1531 x
+// 2051 x 5465 bf16: the forward's 258 tiles as 256 whole ones and two split by 8
+// 124 us, as 1032 smaller ones 163; 777 x 1003 x 2731 fp32: 256 of 301 whole and the
+// others split by 5 109 us, all split by 2 122.
 struct Cut {
     int tile, splits;
+    int64_t whole;  // tiles that are not split
 };
 
 constexpr double kCuFlops[2][4] = {
@@ -382,48 +416,62 @@ constexpr double kCuFlops[2][4] = {
     {1.7, 3.4, 4.6, 1.4},      // bf16
 };
 
+// A CU holds two and more blocks of the smaller tiles, and one of them alone,
+// with no part beside it any more, does not reach the rate.
+constexpr double kAlone = 1.2;
+
 Cut cut_of(int64_t rows, int64_t cols, int64_t K, int outputs, int esize, bool gated) {
-    Cut best{64, 1};
+    Cut best{64, 1, 0};
     double least = 0;
     for (int i = 0; i < 3; ++i) {
         const int tile = 64 << i;
         const int64_t tiles = ceil_div(rows, tile) * ceil_div(cols, gated ? tile / 2 : tile) * outputs;
         const double one = 2.0 * tile * tile * double(K) /
                            (kCuFlops[esize == 2][gated && i == 0 ? 3 : i] * 1e12);
-        for (int s = 1; s <= 16; s *= 2) {
-            if (s > 1 && K / s < 4 * (kStepBytes / esize)) break;
-            double t = double(ceil_div(tiles * s, 256)) * (one / s + 1.5e-6);
-            if (s > 1)
-                t += 4e-6 + 8.0 * s * double(rows) * double(cols) * outputs * (gated ? 2 : 1) / 4e12;
+        auto consider = [&](int64_t whole, int s) {
+            const int64_t rest = tiles - whole;
+            double t = double(ceil_div(whole, 256)) * (one + 1.5e-6);
+            if (rest)
+                t += double(ceil_div(rest * s, 256)) * (one / s + 1.5e-6) + 4e-6 +
+                     8.0 * s * double(rest) * tile * tile / 4e12;
+            if (rest && whole && tile < 256) t *= kAlone;
             if (least == 0 || t < least) {
                 least = t;
-                best = Cut{tile, s};
+                best = Cut{tile, s, whole};
             }
+        };
+        consider(tiles, 1);
+        for (int s = 2; s <= 16; ++s) {
+            if (K / s < 4 * (kStepBytes / esize)) break;
+            if ((s & (s - 1)) == 0) consider(0, s);
+            if (tiles > 256 && tiles % 256) consider(tiles / 256 * 256, s);
         }
     }
     return best;
 }
 
-int64_t part_pitch(int64_t cols) { return round_up(cols, 4); }
 // The workspace of a cut's parts.
-int64_t part_bytes(const Cut& c, int64_t rows, int64_t cols, int outputs) {
-    return c.splits > 1 ? round_up(4 * c.splits * outputs * rows * part_pitch(cols), 256) : 0;
+int64_t part_bytes(const Cut& c, int64_t rows, int64_t cols, int outputs, bool gated) {
+    const int64_t tiles = ceil_div(rows, c.tile) * ceil_div(cols, gated ? c.tile / 2 : c.tile) * outputs;
+    return c.splits > 1 ? 4 * c.splits * (tiles - c.whole) * c.tile * c.tile : 0;
 }
 
 ProductShape shape(int64_t rows, int64_t cols, int64_t K, int segments, const Cut& c, int width,
-                   void* part) {
-    return ProductShape{rows, cols, K, segments, ceil_div(rows, c.tile), ceil_div(cols, width),
-                        c.splits, static_cast<float*>(part), part_pitch(cols)};
+                   int outputs, void* part) {
+    const int64_t rt = ceil_div(rows, c.tile), ct = ceil_div(cols, width);
+    return ProductShape{rows, cols, K, segments, rt, ct, rt * ct * outputs,
+                        c.splits > 1 ? c.whole : rt * ct * outputs, c.splits,
+                        static_cast<float*>(part)};
 }
 
-dim3 grid_of(int64_t tiles) { return dim3(unsigned(tile_blocks(tiles))); }
+dim3 grid_of(const ProductShape& p) { return dim3(unsigned(unit_blocks(p))); }
 dim3 join_grid(int64_t vecs) {
     return dim3(unsigned(std::min<int64_t>(ceil_div(vecs, 256), 1 << 14)));
 }
 
 template <class T, bool RKC, int B, int WR, int WC>
 void launch_product(const ProductShape& p, const Products<T>& a, bool fast, hipStream_t st) {
-    const dim3 grid = grid_of(p.row_tiles * p.col_tiles * p.splits * a.count), block(64 * WR * WC);
+    const dim3 grid = grid_of(p), block(64 * WR * WC);
     if (fast)
         hipLaunchKernelGGL((product_kernel<T, B, B, WR, WC, RKC, true>), grid, block, 0, st, p, a);
     else
@@ -434,21 +482,21 @@ template <class T, bool RKC>
 void run_product(int64_t rows, int64_t cols, int64_t K, int segments, const Products<T>& a,
                  void* part, hipStream_t st) {
     const Cut c = cut_of(rows, cols, K * segments, a.count, int(sizeof(T)), false);
-    const ProductShape p = shape(rows, cols, K, segments, c, c.tile, part);
+    const ProductShape p = shape(rows, cols, K, segments, c, c.tile, a.count, part);
     bool fast = direct(a.l, false);
     for (int i = 0; i < a.count; ++i) fast = fast && direct(a.r[i], RKC);
     if (c.tile == 256) launch_product<T, RKC, 256, 2, 4>(p, a, fast, st);
     else if (c.tile == 128) launch_product<T, RKC, 128, 2, 2>(p, a, fast, st);
     else launch_product<T, RKC, 64, 2, 2>(p, a, fast, st);
     if (c.splits > 1)
-        hipLaunchKernelGGL((product_join_kernel<T>), join_grid(rows * p.pitch / 4 * a.count), dim3(256),
-                           0, st, p, a);
+        hipLaunchKernelGGL((product_join_kernel<T>), join_grid((p.tiles - p.whole) * c.tile * c.tile / 4),
+                           dim3(256), 0, st, p, a, c.tile, c.tile);
 }
 
 template <class T, int B, int WR, int WC>
 void launch_forward(const ProductShape& p, const ForwardArgs& a, const Side<T>& x, const Side<T>& w,
                     T* h, bool fast, hipStream_t st) {
-    const dim3 grid = grid_of(p.row_tiles * p.col_tiles * p.splits), block(64 * WR * WC);
+    const dim3 grid = grid_of(p), block(64 * WR * WC);
     if (fast)
         hipLaunchKernelGGL((forward_kernel<T, B, B, WR, WC, true>), grid, block, 0, st, p, a, x, w, h);
     else
@@ -471,19 +519,20 @@ void run_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Si
         return;
     }
     const Cut c = cut_of(M, F, D, 1, int(sizeof(T)), true);
-    const ProductShape p = shape(M, F, D, 1, c, c.tile / 2, part);
+    const ProductShape p = shape(M, F, D, 1, c, c.tile / 2, 1, part);
     const bool fast = direct(x, true) && direct(w, true);
     if (c.tile == 256) launch_forward<T, 256, 2, 4>(p, a, x, w, h, fast, st);
     else if (c.tile == 128) launch_forward<T, 128, 2, 2>(p, a, x, w, h, fast, st);
     else launch_forward<T, 64, 2, 1>(p, a, x, w, h, fast, st);
     if (c.splits > 1)
-        hipLaunchKernelGGL((forward_join_kernel<T>), join_grid(M * p.pitch / 4), dim3(256), 0, st, p, a, h);
+        hipLaunchKernelGGL((forward_join_kernel<T>), join_grid((p.tiles - p.whole) * c.tile * c.tile / 8),
+                           dim3(256), 0, st, p, a, h, c.tile, c.tile / 2);
 }
 
 // bf16 rows that do not lie at 16 bytes cannot be copied straight to LDS: x and
 // the weights are laid out once more, in rows of whole vectors, where the widths
 // say so and the products are long enough to pay for it (6000 x 2051 x 5465:
-// forward 423 -> 374 us; 1531 rows of it: forward 168 -> 163, backward 707 -> 298).
+// forward 423 -> 374 us; 1531 rows of it: backward 707 -> 298).
 template <class T>
 __global__ __launch_bounds__(256) void pack_kernel(int64_t rows, int64_t cols, const T* from,
                                                    int64_t stride, T* to, int64_t pitch) {
@@ -533,8 +582,8 @@ struct BackSpace {
 BackSpace back_space(int64_t M, int64_t D, int64_t F, int esize) {
     BackSpace b{};
     b.dx = round_up(2 * M * factor_stride(F) * esize, 256);
-    b.dw = b.dx + part_bytes(cut_of(M, D, 2 * F, 1, esize, false), M, D, 1);
-    b.packed = b.dw + part_bytes(cut_of(F, D, M, 2, esize, false), F, D, 2);
+    b.dw = b.dx + part_bytes(cut_of(M, D, 2 * F, 1, esize, false), M, D, 1, false);
+    b.packed = b.dw + part_bytes(cut_of(F, D, M, 2, esize, false), F, D, 2, false);
     b.end = b.packed + pack_bytes(M, D, F, esize);
     return b;
 }
@@ -570,7 +619,7 @@ AR_EXPORT ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_
     AR_TRY(check_glu_sizes(M, D, F));
     *bytes = M <= kFewRows || D == 0 || F == 0
                  ? 0
-                 : part_bytes(cut_of(M, F, D, 1, es, true), M, F, 2) + pack_bytes(M, D, F, es);
+                 : part_bytes(cut_of(M, F, D, 1, es, true), M, F, 1, true) + pack_bytes(M, D, F, es);
     if (backward) *bytes = std::max(*bytes, back_space(M, D, F, es).end);
     return AR_OK;
 }
@@ -612,7 +661,7 @@ AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_
             sw{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride, D};
         if (M > kFewRows && packs(M, D, F, es) && !(direct(sx, true) && direct(sw, true)))
             pack<T>(M, D, F, &sx, &sw,
-                    static_cast<char*>(workspace) + part_bytes(cut_of(M, F, D, 1, es, true), M, F, 2), st);
+                    static_cast<char*>(workspace) + part_bytes(cut_of(M, F, D, 1, es, true), M, F, 1, true), st);
         run_forward<T>(a, M, D, F, sx, sw, static_cast<T*>(h), workspace, st);
         return launch_status("gated feed-forward");
     };

@@ -27,8 +27,9 @@
 // end with the row: what it holds lies `shift` further on, in the accumulators
 // too, and the store reads it from there.
 //
-// Few tiles.  A product may be split along k (`splits`), each part's sums going
-// to memory in fp32; a second kernel adds them in order.
+// Tiles that do not fill the card.  The last tiles, or all of them, may be split
+// along k (`splits`), each part's sums going to memory in fp32; a second kernel
+// adds them in order.
 #pragma once
 
 #include "replica.hpp"
@@ -59,9 +60,15 @@ struct ProductShape {
     int64_t K;           // of one segment
     int segments;        // 1 or 2
     int64_t row_tiles, col_tiles;
-    int splits;          // parts along k
-    float* part;         // their sums (splits > 1), [split][output][rows][pitch]
-    int64_t pitch;
+    int64_t tiles, whole;  // of all outputs; the first `whole` of them are not split
+    int splits;            // parts along k of the others
+    float* part;           // their sums, [tile][split][rows of a tile][its columns]
+};
+
+// A block's work: a tile, or part `split` of its `splits`.
+struct Unit {
+    int64_t tile;
+    int split, splits;
 };
 
 __device__ __forceinline__ int swz(int r) { return ((r >> 1) ^ ((r & 1) << 2)) & 7; }
@@ -250,16 +257,22 @@ __device__ __forceinline__ void multiply(const u32x4 l, const u32x4 r, f32x16& a
     }
 }
 
-// The tile of the block: blocks go to the 8 XCDs in turn, so XCD x takes a
+// The block's work: blocks go to the 8 XCDs in turn, so XCD x takes a
 // contiguous eighth of the tiles, in strips of `kStrip` tile rows that are
 // walked along the columns: what its 32 CUs work on at a time shares panels
-// in its L2.
+// in its L2.  The parts of the tiles that are split follow, an eighth each too.
 constexpr int kStrip = 4;
-__device__ __forceinline__ bool tile_of(const ProductShape& p, int64_t tiles, int64_t block,
-                                        int64_t* tile) {
-    const int64_t share = (tiles + 7) / 8;
-    *tile = (block & 7) * share + (block >> 3);
-    return (block >> 3) < share && *tile < tiles;
+__device__ __forceinline__ bool unit_of(const ProductShape& p, int64_t block, Unit* u) {
+    const int64_t x = block & 7, i = block >> 3, share = (p.whole + 7) / 8;
+    if (i < share) {
+        *u = Unit{x * share + i, 0, 1};
+        return u->tile < p.whole;
+    }
+    const int64_t rest = p.tiles - p.whole, parts = rest * p.splits, eighth = (parts + 7) / 8;
+    const int64_t n = x * eighth + i - share;
+    if (i - share >= eighth || n >= parts) return false;
+    *u = Unit{p.whole + n % rest, int(n / rest), p.splits};
+    return true;
 }
 // Where the tile lies in its product.
 __device__ __forceinline__ void place_of(const ProductShape& p, int64_t t, int64_t* r, int64_t* c) {
@@ -268,7 +281,9 @@ __device__ __forceinline__ void place_of(const ProductShape& p, int64_t t, int64
     *r = strip * kStrip + in % h;
     *c = in / h;
 }
-inline int64_t tile_blocks(int64_t tiles) { return ceil_div(tiles, 8) * 8; }
+inline int64_t unit_blocks(const ProductShape& p) {
+    return 8 * (ceil_div(p.whole, 8) + ceil_div((p.tiles - p.whole) * p.splits, 8));
+}
 
 // This wavefront's copies have landed in LDS and its own LDS stores are done;
 // after the barrier that follows, so have all the block's.
@@ -289,7 +304,7 @@ struct Tile {
     static constexpr int LDS = 2 * HALF;
 
     static __device__ __forceinline__ void run(const ProductShape& p, const Side<T>& R,
-                                               const Side<T>& L, int64_t r0, int64_t c0, int split,
+                                               const Side<T>& L, int64_t r0, int64_t c0, const Unit& u,
                                                AR_LDS char* lds, f32x16 (&acc)[SR][SC]) {
         const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
         const RP rp(R, r0, RKC ? p.rows : R.extent);
@@ -299,8 +314,8 @@ struct Tile {
         constexpr int KS = StepOf<T>::K;
         const int per = int((p.K + KS - 1) / KS), all = per * p.segments;
         // this part's steps
-        const int from = int(int64_t(all) * split / p.splits);
-        const int steps = int(int64_t(all) * (split + 1) / p.splits) - from;
+        const int from = int(int64_t(all) * u.split / u.splits);
+        const int steps = int(int64_t(all) * (u.split + 1) / u.splits) - from;
         if (steps == 0) return;
         u32x4 rv[DIRECT ? 1 : RP::LOADS], lv[DIRECT ? 1 : LP::LOADS];
         // The step whose copies come next: its segment and number there, and where

@@ -217,6 +217,16 @@ def test_glu_many_tiles(M, D, F, dtype, layout):
     test_glu(M, D, F, dtype, "silu", layout)
 
 
+@pytest.mark.parametrize("layout", ("rows", "wide"))
+@pytest.mark.parametrize("dtype,M,D,F", [
+    ("f32", 777, 1003, 2731), ("f32", 700, 520, 1000), ("f32", 785, 1299, 323),
+    ("bf16", 645, 1319, 2731), ("bf16", 1273, 1177, 1621), ("bf16", 1290, 1500, 5380)])
+def test_glu_uneven_tiles(dtype, M, D, F, layout):
+    """Some tiles more than whole rounds of the card: whole ones first, and the
+    others split."""
+    test_glu(M, D, F, dtype, "silu", layout)
+
+
 @pytest.mark.parametrize("M,D,F", [(65, 130, 129), (200, 4000, 70)])
 def test_glu_compact_factors(M, D, F):
     """Factors saved in bf16, half of the memory: within the bound, which
