@@ -253,11 +253,15 @@ __device__ __forceinline__ bool read_entries(const DistillArgs& a, int64_t t, co
     return __syncthreads_or(any) != 0;
 }
 
-// The entries' p, by differences to their largest; the row's loss, without its
-// factors.  By the whole block, or, if `alone`, by its first wavefront.
+// The entries' p, by differences to their largest; the row's loss, with
+// scale = weight * temperature.  The difference of the logits is taken in their
+// own units and each term scaled before the sum: a student's logit of the type's
+// lowest value, which is beyond fp32 in units of log2, leaves the loss finite.
+// By the whole block, or, if `alone`, by its first wavefront.
 template <int B>
 __device__ __forceinline__ float finish_entries(const DistillArgs& a, const Entries& e,
-                                                const Row& row, Shared<B>& sh, bool alone) {
+                                                const Row& row, float scale, Shared<B>& sh,
+                                                bool alone) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int64_t step = alone ? 64 : B;
     auto all = [&](float v, bool max) {
@@ -278,13 +282,15 @@ __device__ __forceinline__ float finish_entries(const DistillArgs& a, const Entr
         if (e.id[k] >= 0) sum += pow2((e.p[k] - top) * a.c);
     sum = all(sum, false);
     const float ls = __builtin_amdgcn_logf(sum);
+    // temperature (ln S - ln sum): what log p - log q has beside the logits
+    const float sums = (__builtin_amdgcn_logf(row.S) - ls) * 0.6931471805599453f * a.temperature;
     for (int64_t k = threadIdx.x; k < a.K; k += step) {
         if (e.id[k] < 0) continue;
-        const float lp = (e.p[k] - top) * a.c - ls, p = pow2(lp);
+        const float s = e.p[k] - top, p = pow2(s * a.c - ls);
         e.p[k] = p;
-        if (p != 0.0f) loss += p * (lp - row.log2q(e.z[k]));
+        if (p != 0.0f) loss += scale * (p * (s - (e.z[k] - row.m) + sums));
     }
-    return all(loss, false) * 0.6931471805599453f;
+    return all(loss, false);
 }
 
 // The gradient at the entries in [lo, hi): every entry with an id stores the
@@ -394,8 +400,8 @@ __global__ __launch_bounds__(B, 4) void kept_kernel(DistillArgs a, const T* logi
         }
         if (live) {
             if (!alone || w == 0) {
-                const float loss = finish_entries<B>(a, e, row, sh, alone);
-                if (tid == 0) a.loss[t] = scale * a.temperature * loss;
+                const float loss = finish_entries<B>(a, e, row, scale, sh, alone);
+                if (tid == 0) a.loss[t] = loss;
                 if (!alone) __syncthreads();
                 for (int64_t k = tid; g && k < a.K; k += alone ? 64 : B) {
                     const int32_t id = e.id[k];
@@ -482,10 +488,10 @@ __global__ __launch_bounds__(B) void split_kernel(DistillArgs a, const T* logits
         if (g) part.store_zero(g + lo);
         return;
     }
-    const float loss = finish_entries<B>(a, e, row, sh, false);
-    if (threadIdx.x == 0 && j == 0) a.loss[t] = weight * a.temperature * a.temperature * loss;
-    if (!g) return;
     const float scale = weight * a.temperature;
+    const float loss = finish_entries<B>(a, e, row, scale, sh, false);
+    if (threadIdx.x == 0 && j == 0) a.loss[t] = loss;
+    if (!g) return;
     store_gradient(part, row, scale, z, g + lo, static_cast<const T*>(nullptr));
     __syncthreads();  // the entries' elements are written once more, after these
     store_entries<T, B>(a, e, row, scale, lo, hi, g);

@@ -416,6 +416,33 @@ def test_distill_masks(dtype, V, copies):
                 ref.stored(grad[12][rest], dtype) + 1e-5 * grad[12][rest])
 
 
+@pytest.mark.parametrize("V,copies", [(2051, 1), (2051, 13), (20011, 1), (20011, 13), (70001, 13)])
+@pytest.mark.parametrize("tau", (0.5, 1.0, 2.0))
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_distill_entries_at_the_masks_value(V, copies, tau, dtype):
+    """The student's logit at entries of the teacher is the type's lowest value:
+    the loss is that far off, and finite in fp32."""
+    T, K = 16, 6
+    low = torch.finfo(ref.TORCH[dtype]).min
+    z = rnd(1, T, V, dtype=dtype, scale=3.0)
+    ids, tea = teacher_of(2, T, V, K)
+    for t in range(T):
+        z[t, ids[t, :1 + t % (K - 1)]] = low        # one to all but one
+    w = torch.full((T,), 0.25)
+    (loss, el), (grad, eg) = ref.distill(z, tea, ids, tau, w, dtype)
+    assert bool((loss > 1e28).all()) and bool((loss < 3.4e38).all())
+    # (the reference's bound leaves numbers of this size out: K terms, each off
+    # by its probability's error, 6 units a unit of its logarithm, that is above
+    # -45, and some roundings)
+    el = loss * (K + 64 + 6 * 45) * ref.U
+    args = [x.cuda().repeat(copies, 1) for x in (z, tea, ids)]
+    got, g = ops.distill(*args, temperature=tau, weights=w.cuda().repeat(copies),
+                         grad=torch.empty(copies * T, V, dtype=z.dtype, device="cuda"))
+    ref.compare("loss", got, loss.repeat(copies), el.repeat(copies))
+    for i in (0, copies - 1):
+        ref.compare("gradient", g[i * T:(i + 1) * T], grad, eg)
+
+
 @pytest.mark.parametrize("K", (0, 1000, 4096))
 def test_distill_numbers_of_entries(K):
     T, V = 3, 5003
