@@ -539,8 +539,12 @@ ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_t F, int32
  * student logit of -inf at an entry with p > 0 gives loss +inf and a finite
  * gradient.  teacher_dtype may differ from dtype; loss and weights are fp32 vectors.  grad may be NULL
  * (the loss alone), or logits itself with the same stride (in place).
- * K <= AR_DISTILL_MAX_K (AR_ERR_UNSUPPORTED above); temperature finite and > 0. */
+ * K <= AR_DISTILL_MAX_K (AR_ERR_UNSUPPORTED above); temperature finite and > 0
+ * (AR_ERR_INVALID_ARG), and where its square and its inverse are in fp32's range
+ * (AR_ERR_UNSUPPORTED outside the two bounds). */
 #define AR_DISTILL_MAX_K 4096
+#define AR_DISTILL_MIN_TEMPERATURE 1e-37f
+#define AR_DISTILL_MAX_TEMPERATURE 1e19f
 ar_status ar_distill_workspace(int64_t T, int64_t V, int64_t K, int64_t* bytes);
 ar_status ar_distill(int32_t dtype, int64_t T, int64_t V, int64_t K, const void* logits,
                      int64_t logits_stride, int32_t teacher_dtype, const void* teacher,

@@ -383,6 +383,7 @@ AR_ACT_SILU, AR_ACT_GELU = 0, 1
 ACTS = {"silu": AR_ACT_SILU, "gelu": AR_ACT_GELU}
 AR_EMBED_RUN = 32
 AR_DISTILL_MAX_K = 4096
+AR_DISTILL_MIN_TEMPERATURE, AR_DISTILL_MAX_TEMPERATURE = 1e-37, 1e19
 AR_GLU_MAX_EXTENT = 4194304
 
 

@@ -611,6 +611,9 @@ AR_EXPORT ar_status ar_distill(int32_t dtype, int64_t T, int64_t V, int64_t K, c
     AR_TRY(ar_distill_workspace(T, V, K, &need));
     if (!(temperature > 0.0f) || std::isinf(temperature))
         return fail(AR_ERR_INVALID_ARG, "temperature must be finite and > 0");
+    if (temperature < AR_DISTILL_MIN_TEMPERATURE || temperature > AR_DISTILL_MAX_TEMPERATURE)
+        return fail(AR_ERR_UNSUPPORTED,
+                    "temperature is outside AR_DISTILL_MIN_TEMPERATURE .. AR_DISTILL_MAX_TEMPERATURE");
     const MatArg ml{"logits", logits, T, V, logits_stride, es},
         mt{"teacher", teacher, T, K, teacher_stride, ts}, mi{"ids", ids, T, K, ids_stride, 8},
         mw{"weights", weights, 1, weights ? T : 0, T, 4}, mo{"loss", loss, 1, T, T, 4},

@@ -443,6 +443,22 @@ def test_distill_entries_at_the_masks_value(V, copies, tau, dtype):
         ref.compare("gradient", g[i * T:(i + 1) * T], grad, eg)
 
 
+@pytest.mark.parametrize("tau", (arplan.AR_DISTILL_MIN_TEMPERATURE, 1e-20, 1e-3, 1e6,
+                                 arplan.AR_DISTILL_MAX_TEMPERATURE))
+@pytest.mark.parametrize("V,copies", [(2051, 1), (20011, 1), (20011, 64)])
+def test_distill_temperatures(V, copies, tau):
+    """The ends of the range: one logit takes all, and all the same."""
+    T, K = 3, 6
+    z, w = rnd(1, T, V, scale=3.0), torch.full((T,), 1e-2)
+    ids, tea = teacher_of(2, T, V, K)
+    (loss, el), (grad, eg) = ref.distill(z, tea, ids, tau, w, "f32")
+    got, g = ops.distill(*(x.cuda().repeat(copies, 1) for x in (z, tea, ids)), temperature=tau,
+                         weights=w.cuda().repeat(copies),
+                         grad=torch.empty(copies * T, V, device="cuda"))
+    ref.compare("loss", got, loss.repeat(copies), el.repeat(copies))
+    ref.compare("gradient", g[-T:], grad, eg)
+
+
 @pytest.mark.parametrize("K", (0, 1000, 4096))
 def test_distill_numbers_of_entries(K):
     T, V = 3, 5003

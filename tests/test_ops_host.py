@@ -122,6 +122,12 @@ def test_refusals_of_one_call():
     refuses(arplan.ar_distill, DISTILL, INVALID, grad=DISTILL["logits"], grad_stride=101)
 
 
+def test_temperatures_beyond_the_range_are_refused():
+    for t in (1e-45, 4e-39, 0.9 * arplan.AR_DISTILL_MIN_TEMPERATURE,
+              1.1 * arplan.AR_DISTILL_MAX_TEMPERATURE, 2e19, 3e38):
+        refuses(arplan.ar_distill, DISTILL, UNSUPPORTED, temperature=t)
+
+
 def test_empty_calls_need_no_pointers():
     arplan.ar_embed_lookup("f32", 0, 8, 0, None, 8, None, 1.0, None, 8)
     arplan.ar_embed_grad("f32", 0, 8, 5, at(0), 8, at(1), 1.0, 0, None, 8, None, 0)
