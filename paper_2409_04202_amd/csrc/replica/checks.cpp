@@ -1,4 +1,7 @@
 // Argument checks of the replica operators.
+#include <exception>
+#include <new>
+
 #include "replica.hpp"
 
 namespace arp {
@@ -69,6 +72,20 @@ ar_status launch_status(const char* what) {
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess) return AR_OK;
     return fail(AR_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+ar_status thrown() noexcept {
+    try {
+        try {
+            throw;
+        } catch (const std::bad_alloc&) {
+            return fail(AR_ERR_OOM, "host allocation failed");
+        } catch (const std::exception& e) {
+            return fail(AR_ERR_INTERNAL, e.what());
+        }
+    } catch (...) {
+        return AR_ERR_OOM;  // nor is there memory for the text
+    }
 }
 
 }  // namespace arp

@@ -586,7 +586,7 @@ ar_status run_distill(DistillArgs a, const void* logits, const void* teacher, vo
 
 using namespace arp;
 
-AR_EXPORT ar_status ar_distill_workspace(int64_t T, int64_t V, int64_t K, int64_t* bytes) {
+AR_EXPORT ar_status ar_distill_workspace(int64_t T, int64_t V, int64_t K, int64_t* bytes) try {
     clear_error();
     if (!bytes) return fail(AR_ERR_INVALID_ARG, "bytes is NULL");
     AR_TRY(check_extent("T", T));
@@ -595,6 +595,8 @@ AR_EXPORT ar_status ar_distill_workspace(int64_t T, int64_t V, int64_t K, int64_
     if (K > AR_DISTILL_MAX_K) return fail(AR_ERR_UNSUPPORTED, "K exceeds AR_DISTILL_MAX_K");
     *bytes = std::max(space_of(form_of(T, V, 4), K).end, space_of(form_of(T, V, 2), K).end);
     return AR_OK;
+} catch (...) {
+    return thrown();
 }
 
 AR_EXPORT ar_status ar_distill(int32_t dtype, int64_t T, int64_t V, int64_t K, const void* logits,
@@ -602,7 +604,7 @@ AR_EXPORT ar_status ar_distill(int32_t dtype, int64_t T, int64_t V, int64_t K, c
                                int64_t teacher_stride, const int64_t* ids, int64_t ids_stride,
                                float temperature, const float* weights, float* loss, void* grad,
                                int64_t grad_stride, void* workspace, int64_t workspace_bytes,
-                               void* stream) {
+                               void* stream) try {
     clear_error();
     int32_t es = 0, ts = 0;
     AR_TRY(check_dtype("dtype", dtype, &es));
@@ -646,4 +648,6 @@ AR_EXPORT ar_status ar_distill(int32_t dtype, int64_t T, int64_t V, int64_t K, c
                                        : run_distill<float, uint16_t>(a, logits, teacher, grad, ws, st);
     return teacher_dtype == AR_F32 ? run_distill<uint16_t, float>(a, logits, teacher, grad, ws, st)
                                    : run_distill<uint16_t, uint16_t>(a, logits, teacher, grad, ws, st);
+} catch (...) {
+    return thrown();
 }

@@ -696,7 +696,7 @@ using namespace arp;
 
 AR_EXPORT ar_status ar_embed_lookup(int32_t dtype, int64_t V, int64_t D, int64_t T,
                                     const void* table, int64_t table_stride, const int64_t* ids,
-                                    float scale, void* out, int64_t out_stride, void* stream) {
+                                    float scale, void* out, int64_t out_stride, void* stream) try {
     clear_error();
     int32_t es = 0;
     AR_TRY(check_dtype("dtype", dtype, &es));
@@ -715,9 +715,11 @@ AR_EXPORT ar_status ar_embed_lookup(int32_t dtype, int64_t V, int64_t D, int64_t
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return dtype == AR_F32 ? run_lookup<float>(V, D, T, table, table_stride, ids, scale, out, out_stride, st)
                            : run_lookup<uint16_t>(V, D, T, table, table_stride, ids, scale, out, out_stride, st);
+} catch (...) {
+    return thrown();
 }
 
-AR_EXPORT ar_status ar_embed_grad_workspace(int64_t V, int64_t D, int64_t T, int64_t* bytes) {
+AR_EXPORT ar_status ar_embed_grad_workspace(int64_t V, int64_t D, int64_t T, int64_t* bytes) try {
     clear_error();
     if (!bytes) return fail(AR_ERR_INVALID_ARG, "bytes is NULL");
     AR_TRY(check_extent("V", V));
@@ -725,12 +727,14 @@ AR_EXPORT ar_status ar_embed_grad_workspace(int64_t V, int64_t D, int64_t T, int
     AR_TRY(check_extent("T", T));
     *bytes = V == 0 || D == 0 || T == 0 ? 0 : grad_space(D, T).end;
     return AR_OK;
+} catch (...) {
+    return thrown();
 }
 
 AR_EXPORT ar_status ar_embed_grad(int32_t dtype, int64_t V, int64_t D, int64_t T, const void* dout,
                                   int64_t dout_stride, const int64_t* ids, float scale,
                                   int32_t accumulate, void* dtable, int64_t dtable_stride,
-                                  void* workspace, int64_t workspace_bytes, void* stream) {
+                                  void* workspace, int64_t workspace_bytes, void* stream) try {
     clear_error();
     int32_t es = 0;
     AR_TRY(check_dtype("dtype", dtype, &es));
@@ -753,4 +757,6 @@ AR_EXPORT ar_status ar_embed_grad(int32_t dtype, int64_t V, int64_t D, int64_t T
     char* ws = static_cast<char*>(workspace);
     return dtype == AR_F32 ? run_grad<float>(V, D, T, dout, dout_stride, ids, scale, accumulate, dtable, dtable_stride, ws, st)
                            : run_grad<uint16_t>(V, D, T, dout, dout_stride, ids, scale, accumulate, dtable, dtable_stride, ws, st);
+} catch (...) {
+    return thrown();
 }

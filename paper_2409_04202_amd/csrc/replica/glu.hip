@@ -612,7 +612,7 @@ static ar_status check_glu_sizes(int64_t M, int64_t D, int64_t F) {
 }
 
 AR_EXPORT ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_t F,
-                                     int32_t backward, int64_t* bytes) {
+                                     int32_t backward, int64_t* bytes) try {
     clear_error();
     if (!bytes) return fail(AR_ERR_INVALID_ARG, "bytes is NULL");
     int32_t es = 0;
@@ -623,13 +623,15 @@ AR_EXPORT ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_
                  : part_bytes(cut_of(M, F, D, 1, es, true), M, F, 1, true) + pack_bytes(M, D, F, es);
     if (backward) *bytes = std::max(*bytes, back_space(M, D, F, es).end);
     return AR_OK;
+} catch (...) {
+    return thrown();
 }
 
 AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_t D, int64_t F,
                                    const void* x, int64_t x_stride, const void* wg, const void* wu,
                                    int64_t w_stride, void* h, int64_t h_stride, void* saved_gate,
                                    void* saved_up, int64_t saved_stride, int32_t saved_dtype,
-                                   void* workspace, int64_t workspace_bytes, void* stream) {
+                                   void* workspace, int64_t workspace_bytes, void* stream) try {
     clear_error();
     int32_t es = 0, ss = 0;
     int64_t need = 0;
@@ -667,6 +669,8 @@ AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_
         return launch_status("gated feed-forward");
     };
     return dtype == AR_F32 ? go(float(0)) : go(uint16_t(0));
+} catch (...) {
+    return thrown();
 }
 
 AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t F, const void* dh,
@@ -676,7 +680,7 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
                                     int64_t saved_stride, int32_t saved_dtype,
                                     int32_t accumulate, void* dx,
                                     int64_t dx_stride, void* dwg, void* dwu, int64_t dw_stride,
-                                    void* workspace, int64_t workspace_bytes, void* stream) {
+                                    void* workspace, int64_t workspace_bytes, void* stream) try {
     clear_error();
     int32_t es = 0, ss = 0;
     int64_t need = 0;
@@ -740,4 +744,6 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
         return launch_status("gated feed-forward gradients");
     };
     return dtype == AR_F32 ? go(float(0)) : go(uint16_t(0));
+} catch (...) {
+    return thrown();
 }

@@ -33,6 +33,10 @@ ar_status check_extent(const char* what, int64_t v);
 ar_status check_workspace(const void* ws, int64_t have, int64_t need);
 ar_status launch_status(const char* what);
 
+// The status of what a C entry has caught.  The entries' bodies are function try
+// blocks: the text of an error takes memory, and may throw.
+ar_status thrown() noexcept;
+
 inline int64_t round_up(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
