@@ -32,7 +32,7 @@ int main() {
     const int64_t big = int64_t(1) << 40;
     int bad = 0;
     bad += check("ar_embed_lookup", [&] {
-        return ar_embed_lookup(AR_F32, 10, 8, 4, nullptr, 8, ids, 1.0f, p, 8, nullptr);
+        return ar_embed_lookup(AR_F32, 10, 8, 4, p, 1, ids, 1.0f, p, 8, nullptr);
     });
     bad += check("ar_embed_grad_workspace",
                  [&] { return ar_embed_grad_workspace(big, 8, 4, &bytes); });
