@@ -50,10 +50,11 @@ ar_status check_apart(const MatArg& a, const MatArg& b) {
     if (ea <= pb || eb <= pa) return AR_OK;
     // Columns of one wider matrix: with a common row stride the rows lie side
     // by side where the second begins behind the first's width and ends
-    // before its next row.
-    if (sa == sb) {
-        const uint64_t d = pb >= pa ? (pb - pa) % sa : (sa - (pa - pb) % sa) % sa;
-        if (d >= wa && d + wb <= sa) return AR_OK;
+    // before its next row.  One row has any stride.
+    if (sa == sb || a.rows == 1 || b.rows == 1) {
+        const uint64_t s = a.rows == 1 ? sb : sa;
+        const uint64_t d = pb >= pa ? (pb - pa) % s : (s - (pa - pb) % s) % s;
+        if (d >= wa && d + wb <= s) return AR_OK;
     }
     return fail(AR_ERR_INVALID_ARG, std::string(a.name) + " overlaps " + b.name);
 }

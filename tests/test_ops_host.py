@@ -86,6 +86,19 @@ def test_overlaps_are_refused(f, args, outs):
                 refuses(f, args, INVALID, **{o: args[k] + 4})
 
 
+def test_one_row_beside_the_columns_of_a_matrix():
+    """A table of one row within the output's rows, in columns that the output
+    leaves out, is no overlap: the call is refused for its size, which is checked
+    after that."""
+    T, D = (1 << 31) - 1, 1024
+    args = dict(LOOKUP, V=1, T=T, D=D, table=at(0, 4 * (5 * 4096 + D)), table_stride=D,
+                ids=at(1 << 20), out=at(0), out_stride=4096)
+    refuses(arplan.ar_embed_lookup, args, UNSUPPORTED)
+    refuses(arplan.ar_embed_lookup, args, UNSUPPORTED, table=at(0, 4 * (5 * 4096 + 3 * D)))
+    refuses(arplan.ar_embed_lookup, args, INVALID, table=at(0, 4 * (5 * 4096 + D - 1)))
+    refuses(arplan.ar_embed_lookup, args, INVALID, table=at(0, 4 * (5 * 4096 + 3 * D + 1)))
+
+
 def test_workspaces():
     need = arplan.ar_embed_grad_workspace(10, 8, 4)
     assert need > 0
