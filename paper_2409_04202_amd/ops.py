@@ -19,9 +19,15 @@ function of ``arplan`` names) is allocated where it is not given.
 
 Wrong shapes, types or devices raise ValueError; what the library refuses
 raises ``arplan.ArError``.
+
+Autograd does not see these calls: the gradients are calls of their own.  With
+gradients enabled a tensor that requires one raises ValueError (call under
+``torch.no_grad()``, or with detached tensors), and what a call writes into a
+given tensor counts as a change of it, as of any torch call in place.
 """
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import arplan
 
@@ -55,12 +61,19 @@ def _ids(name, ids, like):
 
 class _on:
     """The stream a call runs on, as a handle: its allocations are made there,
-    and the tensors it is given are marked as used there."""
+    and the tensors it is given are marked as used there, those in ``written`` as
+    changed."""
 
-    __slots__ = ("like", "stream", "tensors", "entered")
+    __slots__ = ("like", "stream", "tensors", "written", "entered")
 
-    def __init__(self, like, stream, tensors):
+    def __init__(self, like, stream, tensors, written=()):
+        if torch.is_grad_enabled():
+            for t in tensors:
+                if t is not None and t.requires_grad:
+                    raise ValueError("a tensor requires a gradient, and none is recorded here: "
+                                     "call under torch.no_grad() or with detached tensors")
         self.like, self.stream, self.tensors, self.entered = like, stream, tensors, ()
+        self.written = written
 
     def __enter__(self):
         if self.stream is None:
@@ -76,6 +89,9 @@ class _on:
     def __exit__(self, *exc):
         for e in reversed(self.entered):
             e.__exit__(*exc)
+        for t in self.written:
+            if t is not None:
+                increment_version(t)
         if self.stream is not None:
             for t in self.tensors:
                 if t is not None:
@@ -103,7 +119,7 @@ def embed_lookup(table, ids, scale=1.0, out=None, stream=None):
     _ids("ids", ids, table)
     V, D = table.shape
     T = ids.numel()
-    with _on(table, stream, (table, ids, out)) as s:
+    with _on(table, stream, (table, ids, out), (out,)) as s:
         flat = ids if ids.is_contiguous() else ids.contiguous()
         if out is None:
             res = torch.empty(ids.shape + (D,), dtype=table.dtype, device=table.device)
@@ -124,7 +140,7 @@ def embed_grad(dout, ids, dtable, scale=1.0, accumulate=False, workspace=None, s
     V = dtable.shape[0]
     if dtable.shape[1] != D or ids.numel() != T:
         raise ValueError("dtable has to be as wide as dout, and ids one a row of dout")
-    with _on(dout, stream, (dout, ids, dtable, workspace)) as s:
+    with _on(dout, stream, (dout, ids, dtable, workspace), (dtable,)) as s:
         flat = ids if ids.is_contiguous() else ids.contiguous()
         w, n, keep = _space(workspace, arplan.ar_embed_grad_workspace(V, D, T), dout)
         arplan.ar_embed_grad(_DT[dout.dtype], V, D, T, dout, sd, flat, scale, accumulate, dtable,
@@ -149,7 +165,7 @@ def glu_forward(x, wg, wu, act="silu", save=False, out=None, workspace=None, str
         raise ValueError("wg and wu: one row stride expected")
     if act not in arplan.ACTS:
         raise ValueError("act: one of %s expected" % ", ".join(sorted(arplan.ACTS)))
-    with _on(x, stream, (x, wg, wu, out, workspace)) as s:
+    with _on(x, stream, (x, wg, wu, out, workspace), (out,)) as s:
         h = torch.empty(M, F, dtype=x.dtype, device=x.device) if out is None else out
         sh = _matrix("out", h, (M, F), x)
         kind = torch.float32 if save in (True, False, None) else save
@@ -189,7 +205,7 @@ def glu_backward(dh, x, wg, wu, saved, dx=None, dwg=None, dwu=None, accumulate=F
         raise ValueError("dwg and dwu are given together")
     if accumulate and dwg is None:
         raise ValueError("accumulate: dwg and dwu have to be given")
-    with _on(dh, stream, (dh, x, wg, wu, saved, dx, dwg, dwu, workspace)) as s:
+    with _on(dh, stream, (dh, x, wg, wu, saved, dx, dwg, dwu, workspace), (dx, dwg, dwu)) as s:
         if dx is None:
             dx = torch.empty(M, D, dtype=dh.dtype, device=dh.device)
         if dwg is None:
@@ -228,7 +244,7 @@ def distill(logits, teacher, ids, temperature=1.0, weights=None, grad=None, work
                                 or weights.device != logits.device or not weights.is_contiguous()):
         raise ValueError("weights: a contiguous float32 vector, one a row, expected")
     sg = _matrix("grad", grad, (T, V), logits) if grad is not None else 0
-    with _on(logits, stream, (logits, teacher, ids, weights, grad, workspace)) as s:
+    with _on(logits, stream, (logits, teacher, ids, weights, grad, workspace), (grad,)) as s:
         loss = torch.empty(T, dtype=torch.float32, device=logits.device)
         w, n, keep = _space(workspace, arplan.ar_distill_workspace(T, V, K), logits)
         arplan.ar_distill(_DT[logits.dtype], T, V, K, logits, sl, _DT[teacher.dtype], teacher, st,

@@ -549,6 +549,50 @@ def test_ops_repeat_bit_for_bit_and_on_another_stream():
             assert torch.equal(a, b)
 
 
+def _tensors():
+    """(function, arguments, the names of what it writes) of every operator."""
+    M, D, F, V, K = 4, 8, 16, 32, 3
+    e = lambda *s: rnd(1, *s).cuda()  # noqa: E731
+    ids = torch.zeros(M, dtype=torch.int64, device="cuda")
+    return [
+        (ops.embed_lookup, dict(table=e(V, D), ids=ids, out=e(M, D)), ("out",)),
+        (ops.embed_grad, dict(dout=e(M, D), ids=ids, dtable=e(V, D)), ("dtable",)),
+        (ops.glu_forward, dict(x=e(M, D), wg=e(F, D), wu=e(F, D), out=e(M, F)), ("out",)),
+        (ops.glu_backward, dict(dh=e(M, F), x=e(M, D), wg=e(F, D), wu=e(F, D), saved=e(2, M, F),
+                                dx=e(M, D), dwg=e(F, D), dwu=e(F, D)), ("dx", "dwg", "dwu")),
+        (ops.distill, dict(logits=e(M, V), teacher=e(M, K), ids=ids[:, None].repeat(1, K),
+                           weights=e(M, 1)[:, 0].contiguous(), grad=e(M, V)), ("grad",))]
+
+
+def test_tensors_that_require_a_gradient_are_refused():
+    for f, args, _ in _tensors():
+        for name, t in args.items():
+            if not t.is_floating_point():
+                continue
+            t.requires_grad_()
+            with pytest.raises(ValueError, match="gradient"):
+                f(**args)
+            with torch.no_grad():
+                f(**args)
+            t.requires_grad_(False)
+
+
+def test_written_tensors_count_as_changed():
+    for f, args, written in _tensors():
+        before = {name: t._version for name, t in args.items()}
+        f(**args)
+        for name, t in args.items():
+            assert (t._version > before[name]) == (name in written), (f.__name__, name)
+    # an in-place gradient over logits that autograd has saved
+    w = torch.ones(4, 32, device="cuda", requires_grad=True)
+    logits = rnd(1, 4, 32).cuda()
+    y = (w * logits).sum()
+    ops.distill(logits, rnd(2, 4, 3).cuda(), torch.zeros(4, 3, dtype=torch.int64, device="cuda"),
+                grad=logits)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
 def test_ops_in_a_graph():
     go, table = _pass()
     side = torch.cuda.Stream()
