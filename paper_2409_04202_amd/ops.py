@@ -81,6 +81,8 @@ class _on:
                 self.entered = (torch.cuda.device(self.like.device),)
                 self.entered[0].__enter__()
             return torch.cuda.current_stream().cuda_stream
+        if self.stream.device != self.like.device:
+            raise ValueError("stream: one of the operands' device expected")
         self.entered = (torch.cuda.device(self.like.device), torch.cuda.stream(self.stream))
         for e in self.entered:
             e.__enter__()

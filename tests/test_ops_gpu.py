@@ -577,6 +577,14 @@ def test_tensors_that_require_a_gradient_are_refused():
             t.requires_grad_(False)
 
 
+def test_a_stream_of_another_device_is_refused():
+    class Other:
+        device, cuda_stream = torch.device("cuda", torch.cuda.device_count()), 0
+    for f, args, _ in _tensors():
+        with pytest.raises(ValueError, match="stream"):
+            f(stream=Other(), **args)
+
+
 def test_written_tensors_count_as_changed():
     for f, args, written in _tensors():
         before = {name: t._version for name, t in args.items()}
