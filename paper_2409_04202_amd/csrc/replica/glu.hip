@@ -529,11 +529,9 @@ void run_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Si
                            dim3(256), 0, st, p, a, h, c.tile, c.tile / 2);
 }
 
-// bf16 rows that do not lie at 16 bytes cannot be copied straight to LDS: x and
-// the weights are laid out once more, in rows of whole vectors, where the widths
-// say so and the products are long enough to pay for it (6000 x 2051 x 5465:
-// forward 382 -> 347 us, backward 1346 -> 698; 1531 rows of it: forward 122 -> 126,
-// backward 705 -> 299).
+// bf16 rows that do not lie at 16 bytes, by their width, stride or address, cannot
+// be copied straight to LDS: x and the weights are laid out once more, in rows of
+// whole vectors, where enough rows of x read the weights to pay for it.
 template <class T>
 __global__ __launch_bounds__(256) void pack_kernel(int64_t rows, int64_t cols, const T* from,
                                                    int64_t stride, T* to, int64_t pitch) {
@@ -546,11 +544,20 @@ __global__ __launch_bounds__(256) void pack_kernel(int64_t rows, int64_t cols, c
     }
 }
 
-bool packs(int64_t M, int64_t D, int64_t F, int esize) {
-    return esize == 2 && D % 8 && double(M) * double(D) * double(F) > 5e8;
+// The forward's panels lie along their rows, the backward's across them, where
+// rows that all start at another place within 16 bytes are the slowest.  M x D x F,
+// us as they lie and laid out anew.  Forward, 2048 x 1003 x 4096 71 and 77, 2048 x
+// 2048 x 5464 161 and 139, 512 x 4099 x 16384 195 and 276, 4096 x 4099 x 16384 1334 and
+// 1241, 4096 x 4096 x 16384 1541 and 1042.  Backward, 128 x 4099 x 16384 316 and
+// 365, 256 x 4099 x 16384 454 and 416, 1536 x 2051 x 5465 717 and 302; of whole vectors 512
+// x 4096 x 16384 436 and 470, 768 x 1024 x 4096 107 and 98, 4096 x 2048 x 5464 551 and
+// 475.
+bool packs(int64_t M, int64_t D, int64_t F, int esize, bool backward) {
+    const int64_t rows = !backward ? 2048 : D % 8 ? 256 : 768;
+    return esize == 2 && M >= rows && double(M) * double(D) * double(F) > 5e8;
 }
-int64_t pack_bytes(int64_t M, int64_t D, int64_t F, int esize) {
-    return packs(M, D, F, esize) ? round_up((M + 2 * F) * round_up(D, 8) * esize, 256) : 0;
+int64_t pack_bytes(int64_t M, int64_t D, int64_t F, int esize, bool backward) {
+    return packs(M, D, F, esize, backward) ? round_up((M + 2 * F) * round_up(D, 8) * esize, 256) : 0;
 }
 // Replaces x and w by their copies in `space`.
 template <class T>
@@ -585,7 +592,7 @@ BackSpace back_space(int64_t M, int64_t D, int64_t F, int esize) {
     b.dx = round_up(2 * M * factor_stride(F) * esize, 256);
     b.dw = b.dx + part_bytes(cut_of(M, D, 2 * F, 1, esize, false), M, D, 1, false);
     b.packed = b.dw + part_bytes(cut_of(F, D, M, 2, esize, false), F, D, 2, false);
-    b.end = b.packed + pack_bytes(M, D, F, esize);
+    b.end = b.packed + pack_bytes(M, D, F, esize, true);
     return b;
 }
 
@@ -620,7 +627,8 @@ AR_EXPORT ar_status ar_glu_workspace(int32_t dtype, int64_t M, int64_t D, int64_
     AR_TRY(check_glu_sizes(M, D, F));
     *bytes = M <= kFewRows || D == 0 || F == 0
                  ? 0
-                 : part_bytes(cut_of(M, F, D, 1, es, true), M, F, 1, true) + pack_bytes(M, D, F, es);
+                 : part_bytes(cut_of(M, F, D, 1, es, true), M, F, 1, true) +
+                       pack_bytes(M, D, F, es, false);
     if (backward) *bytes = std::max(*bytes, back_space(M, D, F, es).end);
     return AR_OK;
 } catch (...) {
@@ -662,8 +670,8 @@ AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_
         using T = decltype(zero);
         Side<T> sx{{static_cast<const T*>(x), static_cast<const T*>(x)}, x_stride, D},
             sw{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride, D};
-        if (M > kFewRows && packs(M, D, F, es) && !(direct(sx, true) && direct(sw, true)))
-            pack<T>(M, D, F, &sx, &sw,
+        if (packs(M, D, F, es, false))
+            pack<T>(M, D, F, direct(sx, true) ? nullptr : &sx, direct(sw, true) ? nullptr : &sw,
                     static_cast<char*>(workspace) + part_bytes(cut_of(M, F, D, 1, es, true), M, F, 1, true), st);
         run_forward<T>(a, M, D, F, sx, sw, static_cast<T*>(h), workspace, st);
         return launch_status("gated feed-forward");
@@ -727,7 +735,7 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
         char* const ws = static_cast<char*>(workspace);
         Side<T> sx{{static_cast<const T*>(x), static_cast<const T*>(x)}, x_stride, D},
             sw{{static_cast<const T*>(wg), static_cast<const T*>(wu)}, w_stride, D};
-        if (packs(M, D, F, es))
+        if (packs(M, D, F, es, true))
             pack<T>(M, D, F, dwg && !direct(sx, false) ? &sx : nullptr,
                     dx && !direct(sw, false) ? &sw : nullptr, ws + space.packed, st);
         const Side<T> sg{{dg, du}, fs, fs};

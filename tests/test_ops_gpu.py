@@ -227,6 +227,32 @@ def test_glu_uneven_tiles(dtype, M, D, F, layout):
     test_glu(M, D, F, dtype, "silu", layout)
 
 
+@pytest.mark.parametrize("which", ("x", "weights", "both"))
+@pytest.mark.parametrize("M,D,F", [(800, 1024, 776), (2050, 520, 776)])
+def test_glu_views_of_a_flat_vector(M, D, F, which):
+    """Whole vectors wide, but at an odd place of a flat vector: the same bits as
+    at 16 bytes, and the definition's values."""
+    x, wg = rnd(1, M, D, dtype="bf16"), rnd(2, F, D, dtype="bf16", scale=D ** -0.5)
+    wu, dh = rnd(3, F, D, dtype="bf16", scale=D ** -0.5), rnd(4, M, F, dtype="bf16")
+    want = ref.glu(x, wg, wu, "silu", dh, "bf16")
+
+    def odd(t):
+        v = torch.full((t.numel() + 6,), float("nan"), dtype=t.dtype, device="cuda")
+        v[3:3 + t.numel()] = t.flatten().cuda()
+        return v[3:3 + t.numel()].view(t.shape)
+    gx, gg, gu, gd = (t.cuda() for t in (x, wg, wu, dh))
+    ox = gx if which == "weights" else odd(x)
+    og, ou = (gg, gu) if which == "x" else (odd(wg), odd(wu))
+    h, saved = ops.glu_forward(gx, gg, gu, save=True)
+    even = (h, saved) + ops.glu_backward(gd, gx, gg, gu, saved)
+    h, saved = ops.glu_forward(ox, og, ou, save=True)
+    got = (h, saved) + ops.glu_backward(gd, ox, og, ou, saved)
+    for a, b in zip(got, even):
+        assert torch.equal(a, b)
+    for name, g, w in zip(("h", "dx", "dwg", "dwu"), (got[0],) + got[2:], want):
+        ref.compare(name, g, *w)
+
+
 @pytest.mark.parametrize("M,D,F", [(65, 130, 129), (200, 4000, 70)])
 def test_glu_compact_factors(M, D, F):
     """Factors saved in bf16, half of the memory: within the bound, which

@@ -121,6 +121,15 @@ def test_workspaces():
         assert b.value == -7        # written on success only
 
 
+@pytest.mark.parametrize("M,D,F", [(2048, 1024, 2048), (4000, 2051, 5465)])
+def test_workspace_for_rows_laid_out_anew(M, D, F):
+    """Whether rows lie at 16 bytes is known by their addresses and strides, not by
+    their width: a long bf16 product's workspace has room for x and the weights."""
+    rows = (M + 2 * F) * (-(-D // 8) * 8) * 2
+    assert arplan.ar_glu_workspace("bf16", M, D, F, False) >= rows
+    assert arplan.ar_glu_workspace("bf16", M, D, F, True) >= rows + 2 * M * F * 2
+
+
 def test_refusals_of_one_call():
     refuses(arplan.ar_glu_forward, FORWARD, INVALID, act=2)
     refuses(arplan.ar_glu_forward, FORWARD, INVALID, saved_up=None)
