@@ -81,7 +81,7 @@ __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, F
         auto pass = [&](auto* out, int64_t stride, auto f) {
             S::fill(part, f);
             wave_sync();
-            S::store(part, out, stride, r0, p.rows, c0, p.cols, false, 0, 0, 0, 0);
+            S::store(part, out, stride, r0, p.rows, c0, p.cols, false, 0, 0);
             wave_sync();
         };
         if (unit.splits > 1) {  // g on the left, u on the right
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, F
             auto sums = [&](int j) {
                 S::fill(part, [&](int, int e) { return acc[i][j][e]; });
                 wave_sync();
-                S::store(part, to, BC, tr, BR, tc + j * (BC / 2), BC, false, 0, 0, 0, 0);
+                S::store(part, to, BC, tr, BR, tc + j * (BC / 2), BC, false, 0, 0);
                 wave_sync();
             };
             sums(0);
@@ -329,8 +329,7 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductShape p, P
     P::run(p, second ? a.r[1] : a.r[0], a.l, rt * BR, ct * BC, unit, (AR_LDS char*)lds, acc);
     const int wave = int(threadIdx.x) >> 6, wr = wave / WC, wc = wave % WC;
     AR_LDS float* const part = (AR_LDS float*)((AR_LDS char*)lds + wave * S::BYTES);
-    const int rshift = DIRECT && !RKC ? int((VEC - a.r[0].extent % VEC) % VEC) : 0,
-              cshift = DIRECT ? int((VEC - a.l.extent % VEC) % VEC) : 0;
+    const int shift = DIRECT ? int((VEC - a.l.extent % VEC) % VEC) : 0;
 #pragma unroll
     for (int i = 0; i < P::SR; ++i) {
         S::fill(part, [&](int j, int e) { return acc[i][j][e]; });
@@ -341,10 +340,10 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductShape p, P
             S::store(part, p.part + part_at(p, unit.tile, unit.split, BR, BC), BC, tr,
                      p.rows - rt * BR < BR ? p.rows - rt * BR : BR, tc,
                      p.cols - ct * BC < BC ? p.cols - ct * BC : BC, false, VEC,
-                     rt + 1 == p.row_tiles ? rshift : 0, VEC, ct + 1 == p.col_tiles ? cshift : 0);
+                     ct + 1 == p.col_tiles ? shift : 0);
         else
             S::store(part, second ? a.out[1] : a.out[0], a.stride, r0, p.rows, c0, p.cols,
-                     a.accumulate, VEC, rshift, VEC, cshift);
+                     a.accumulate, VEC, shift);
         wave_sync();
     }
 }

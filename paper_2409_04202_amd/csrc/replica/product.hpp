@@ -25,7 +25,8 @@
 // what lies there, NaN included, has no effect.  Where copies go straight to
 // LDS, the last chunk of a K-major row that has fewer elements is moved back to
 // end with the row: what it holds lies `shift` further on, in the accumulators
-// too, and the store reads it from there.
+// too, and the store reads it from there.  (Column operands only: the rows of a
+// K-major row operand, the factors in the workspace, are whole chunks.)
 //
 // Tiles that do not fill the card.  The last tiles, or all of them, may be split
 // along k (`splits`), each part's sums going to memory in fp32; a second kernel
@@ -463,13 +464,12 @@ struct Store {
                 *(AR_LDS f4*)(part + (lane & 31) * PITCH + j * 32 + 8 * q + 4 * (lane >> 5)) = v;
             }
     }
-    // rows r0 .. of `out`, columns c0 .. of the SC * 32; the last rows (columns)
-    // of an incomplete chunk of rshift (cshift) fewer lie so much further on
+    // rows r0 .. of `out`, columns c0 .. of the SC * 32; the last columns of an
+    // incomplete chunk of `shift` fewer lie so much further on
     template <class T>
     static __device__ __forceinline__ void store(const AR_LDS float* part, T* out, int64_t stride,
                                                  int64_t r0, int64_t rows, int64_t c0, int64_t cols,
-                                                 bool accumulate, int rchunk, int rshift,
-                                                 int cchunk, int cshift) {
+                                                 bool accumulate, int chunk, int shift) {
         constexpr int VEC = Num<T>::VEC, PER = SC * 32 / VEC, ROWS = 64 / PER;
         const int lane = int(threadIdx.x) & 63;
 #pragma unroll
@@ -478,12 +478,11 @@ struct Store {
             const int64_t left = cols - c0 - c;
             if (r0 + r >= rows || left <= 0) continue;
             T* const at = out + (r0 + r) * stride + c0 + c;
-            const AR_LDS float* const row =
-                part + (rshift && rows - (r0 + r) <= rchunk - rshift ? r + rshift : r) * PITCH;
+            const AR_LDS float* const row = part + r * PITCH;
             float v[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                v[e] = row[c + e + (cshift && left - e <= cchunk - cshift ? cshift : 0)];
+                v[e] = row[c + e + (shift && left - e <= chunk - shift ? shift : 0)];
             const int n = int(left < VEC ? left : VEC);
             if (accumulate) {
                 float old[VEC];
