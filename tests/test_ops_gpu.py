@@ -174,6 +174,63 @@ def test_glu(M, D, F, dtype, act, layout):
         c()
 
 
+GLU_EXACT = [
+    (1, 1, 1), (8, 2051, 37), (9, 72, 64), (20, 3000, 70), (70, 130, 2500), (1500, 65, 130),
+    (130, 2, 67), (5000, 65, 9), (2309, 5800, 40), (50, 3849, 3081), (203, 133, 301),
+    (645, 1319, 2731), (777, 1003, 2731), (1290, 1500, 5380), (1531, 264, 520), (2050, 504, 520),
+    (600, 1003, 1000)]
+
+
+def whole(seed, *shape, far=2):
+    """Whole numbers up to ``far`` in magnitude."""
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(-far, far + 1, shape, generator=g).double()
+
+
+@pytest.mark.parametrize("layout", ("rows", "wide"))
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,D,F", GLU_EXACT)
+def test_glu_products_are_exact(M, D, F, dtype, layout):
+    """On small whole numbers every product and sum is exact in fp32 (the largest
+    sum, of 2 F terms up to 8, stays below 2^24), the factors in bf16 too: each
+    result is the exact one rounded once, and a term lost, or added twice, at
+    any place of a sum shows."""
+    dt = ref.TORCH[dtype]
+    x, wg, wu, dh = whole(1, M, D), whole(2, F, D), whole(3, F, D), whole(4, M, F)
+    sg, su = whole(5, M, F), whole(6, M, F)
+    dg, du = dh * sg, dh * su
+    gpu = lambda t: laid(t.to(dt), layout)  # noqa: E731
+    gx, gg, gu, gd = (gpu(t) for t in (x, wg, wu, dh))
+    for kind in {torch.float32, dt}:
+        saved = torch.stack((sg, su)).to(kind).cuda()
+        (ox, c0), (og, c1), (ou, c2) = (room(r, D, dtype, layout) for r in (M, F, F))
+        og.copy_(whole(7, F, D))
+        ou.copy_(whole(8, F, D))
+        for add in (True, False):   # (first onto whole numbers)
+            ops.glu_backward(gd, gx, gg, gu, saved, dx=ox, dwg=og, dwu=ou, accumulate=add)
+            assert torch.equal(ox.cpu(), (dg @ wg + du @ wu).to(dt))
+            for i, (o, d) in enumerate(((og, dg), (ou, du))):
+                want = d.t() @ x + (whole(7 + i, F, D) if add else 0)
+                assert torch.equal(o.cpu(), want.to(dt)), (i, add)
+        for c in (c0, c1, c2):
+            c()
+    # the forward: a(g) is g for gates this large, and the other projection 1
+    x[:, 0] = 1
+    far, one = wg.clone(), torch.zeros(F, D).double()
+    far[:, 0], one[:, 0] = 4096, 1
+    x[:, 1:] = x[:, 1:].clamp(-1, 1)
+    out, check = room(M, F, dtype, layout)
+    ops.glu_forward(gpu(x), gpu(far), gpu(one), out=out)
+    g = x @ far.t()
+    assert bool((g > 64).all())
+    assert torch.equal(out.cpu(), g.to(dt))
+    gate = one * 64
+    out.fill_(7.0)
+    ops.glu_forward(gpu(x), gpu(gate), gpu(wu), out=out)
+    assert torch.equal(out.cpu(), (64 * (x @ wu.t())).to(dt))
+    check()
+
+
 @pytest.mark.parametrize("layout", ("rows", "wide"))
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("M,D,F", [(20, 3000, 70), (70, 130, 2500), (1500, 65, 130), (130, 2, 67),
