@@ -174,6 +174,17 @@ def test_glu(M, D, F, dtype, act, layout):
         c()
 
 
+@pytest.mark.parametrize("layout", ("rows", "wide"))
+@pytest.mark.parametrize("act", ("silu", "gelu"))
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,F", [(1, 5), (7, 33), (513, 100), (2500, 67), (4104, 130)])
+@pytest.mark.parametrize("M", (2, 3, 4, 5, 6, 7, 8, 9))
+def test_glu_few_rows(M, D, F, dtype, act, layout):
+    """Every number of rows that takes the weights in whole rows, and one more:
+    lanes with nothing, one vector and several, an odd last feature."""
+    test_glu(M, D, F, dtype, act, layout)
+
+
 GLU_EXACT = [
     (1, 1, 1), (8, 2051, 37), (9, 72, 64), (20, 3000, 70), (70, 130, 2500), (1500, 65, 130),
     (130, 2, 67), (5000, 65, 9), (2309, 5800, 40), (50, 3849, 3081), (203, 133, 301),
