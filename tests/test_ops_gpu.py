@@ -386,6 +386,33 @@ def test_glu_extremes(M, act, dtype):
         assert torch.equal(h2[keep], h[keep]) and bool(h2[3].isnan().all())
 
 
+@pytest.mark.parametrize("M", (5, 40))
+@pytest.mark.parametrize("act", ("silu", "gelu"))
+def test_glu_activations_in_their_tails(M, act):
+    """fp32, gates from -12 to 12 that are exact, against 64 bits and relative to
+    the value: an argument off by a unit moves the tail of the normal
+    distribution by g^2 units, and the functions are off by some tens of units of
+    their own.  The slope, which has a zero, relative to its two terms."""
+    F = 4801
+    g = torch.linspace(-12, 12, F).double().float()
+    x, wg, wu = torch.zeros(M, 3), torch.zeros(F, 3), torch.zeros(F, 3)
+    x[:, 1], wg[:, 1], wu[:, 1] = 1, g, 1
+    h, saved = ops.glu_forward(x.cuda(), wg.cuda(), wu.cuda(), act=act, save=True)
+    g = g.double()
+    value, slope = ref.activate(act, g)
+    if act == "silu":
+        s = torch.sigmoid(g)
+        terms = s * (1 + (g * torch.sigmoid(-g)).abs())
+        slope = s * (1 + g * torch.sigmoid(-g))
+    else:
+        pdf = torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+        terms = 0.5 * torch.special.erfc(-g / math.sqrt(2.0)) + g.abs() * pdf
+    rel = (64 + 4 * g * g) * ref.U
+    for name, got, want, size in (("h", h, value, value.abs()), ("a", saved[1], value, value.abs()),
+                                  ("a'", saved[0], slope, terms)):
+        ref.compare(name, got, want[None, :].expand(M, F), (rel * size)[None, :].expand(M, F))
+
+
 def test_glu_gradients_are_derivatives():
     """Against central differences of <h, dh> in 64 bits."""
     M, D, F = 5, 4, 3
