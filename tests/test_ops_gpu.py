@@ -564,6 +564,59 @@ def test_distill_entries_at_the_masks_value(V, copies, tau, dtype):
         ref.compare("gradient", g[i * T:(i + 1) * T], grad, eg)
 
 
+@pytest.mark.parametrize("K", (6, 64, 65, 1500, 4096))
+@pytest.mark.parametrize("dtype,V,T", [
+    ("bf16", 2051, 9001), ("f32", 2051, 9001), ("bf16", 12001, 5000), ("f32", 6001, 5000),
+    ("bf16", 20011, 2600), ("f32", 10007, 2600), ("bf16", 50021, 1300), ("f32", 20011, 1300),
+    ("bf16", 100003, 650), ("f32", 50021, 650), ("bf16", 131072, 300), ("f32", 65536, 300)])
+def test_distill_rows_in_turn(dtype, V, T, K):
+    """More rows than blocks, so that each takes several in turn, at every size of
+    a block: eleven rows of every kind over and over, whose successor within a
+    block is another kind.  Every copy of a row has its bits."""
+    inf, nan, low = float("inf"), float("nan"), torch.finfo(ref.TORCH[dtype]).min
+    P = 11
+    z = rnd(1, P, V, dtype=dtype, scale=3.0)
+    ids, tea = teacher_of(2, P, V, K, repeat=K > V // 2)
+    w = torch.rand(P, generator=torch.Generator().manual_seed(3)) + 0.1
+    w[1], z[1] = 0, nan                             # weight 0, whatever it holds
+    ids[2], z[2, 3] = -1, nan                       # no entry
+    z[3] = -inf                                     # no logit
+    z[4] = low                                      # the mask's value throughout
+    z[6, V // 2] = inf
+    z[7, 10:] = -inf                                # few logits left
+    z[8, :V // 2] = -300                            # the maximum far from the first vectors
+    z[9, :V // 2] = -30
+    ids[10, K // 2:] = ids[10, 0]                   # one id many times
+    tea = tea.to(ref.TORCH[dtype])
+    (loss, el), (grad, eg) = ref.distill(z, tea, ids, 1.5, w, dtype)
+    # a base that lies 30 below the maximum: differences of 30 log2(e) / 1.5 and
+    # as large a logarithm of the sum, each off by a few units, against the 64
+    # that the bound has for a row
+    el[9], eg[9] = 4 * el[9], 4 * eg[9]
+    n = -(-T // P)
+    args = [x.cuda().repeat(n, 1)[:T].contiguous() for x in (z, tea, ids)]
+    weights = w.cuda().repeat(n)[:T].contiguous()
+    kind = torch.int32 if dtype == "f32" else torch.int16
+
+    def copies_agree(loss, g):
+        b = g.view(kind)
+        for i in range(P, T, P):
+            m = min(P, T - i)
+            assert torch.equal(b[i:i + m], b[:m])
+            assert torch.equal(loss[i:i + m].view(torch.int32), loss[:m].view(torch.int32))
+    got, g = ops.distill(*args, temperature=1.5, weights=weights,
+                         grad=torch.full((T, V), 7.0, dtype=z.dtype, device="cuda"))
+    copies_agree(got, g)
+    ref.compare("loss", got[:P], loss, el)
+    for t in range(P):
+        ref.compare("gradient of row %d" % t, g[t], grad[t], eg[t])
+    only = ops.distill(*args, temperature=1.5, weights=weights)
+    assert torch.equal(only.view(torch.int32), got.view(torch.int32))
+    again, _ = ops.distill(*args, temperature=1.5, weights=weights, grad=args[0])
+    assert torch.equal(args[0].view(kind), g.view(kind))
+    assert torch.equal(again.view(torch.int32), got.view(torch.int32))
+
+
 @pytest.mark.parametrize("tau", (arplan.AR_DISTILL_MIN_TEMPERATURE, 1e-20, 1e-3, 1e6,
                                  arplan.AR_DISTILL_MAX_TEMPERATURE))
 @pytest.mark.parametrize("V,copies", [(2051, 1), (20011, 1), (20011, 64)])
