@@ -16,14 +16,14 @@
 //  * kept: a block takes rows in turn and holds each in registers between the
 //    sum and the gradient, so that it is read once; as it stores the gradient
 //    it loads the next row into the registers that become free.  4096 rows of
-//    131072 bf16 and their gradient: 470 us, 4.3 TB/s (a plain copy of them
-//    gets 4.8), the vector units 45 % busy; 1021 rows of 32003 fp32, the loss
-//    alone: 29 us, 4.6 TB/s with the call;
+//    131072 bf16 and their gradient: 467 us (473 the median of a trace), 4.3 of the
+//    6.2 TB/s of a large copy, the vector units 45 % busy; 1021 rows of 32003 fp32,
+//    the loss alone: 29 us, 4.5 TB/s;
 //  * split: rows longer than a block holds, and rows too few to fill the card.
 //    Each row is cut into parts of a block; one launch leaves the parts' sums,
 //    a second one reads the parts again and writes the gradient.  4096 rows of
 //    140000 bf16: 646 us, 5.3 TB/s of three passes; 8 rows of 131072, the loss
-//    alone: 7 us.
+//    alone: 4 us each.
 #include <algorithm>
 #include <cmath>
 
@@ -33,7 +33,8 @@ namespace arp {
 namespace {
 
 // Vectors of a row that a thread keeps: 64 registers, which leaves a CU its 16
-// wavefronts.
+// wavefronts.  (With 1024 threads three values that hold for all rows are spilled,
+// written once and read once a row.)
 constexpr int kKeep = 16;
 
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -14,10 +14,10 @@
 // that is most of the bytes); the runs; the rows of more than one run.
 // 16384 tokens over a table of 131072 x 4096 bf16, frequencies falling as
 // 1 / rank: 259 us, 4.7 TB/s of the bytes that have to pass; the sort and the
-// zeros 168-184 (6.2 TB/s), the runs 74-80, which also wait for the zeros on
-// their way from the caches to memory, the long rows 6.  5003 tokens, 32003 x
-// 1001 fp32: 55 us, of which the sort (two passes) takes 27, longer than the zeros,
-// the runs 12, the long rows 4.
+// zeros 177 (6.1 TB/s), the runs 76, which also wait for the zeros on their way
+// from the caches to memory, the long rows 7 (medians of a trace).  5003 tokens,
+// 32003 x 1001 fp32: 55 us; the sort, in two passes and longer than the zeros, 33,
+// the runs 19, the long rows 5.
 #include <algorithm>
 #include <type_traits>
 

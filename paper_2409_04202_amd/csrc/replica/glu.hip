@@ -21,7 +21,9 @@ __device__ __forceinline__ float inverse(float x) {
 }
 
 // a(g) and a'(g).  For bf16 the hardware's exponential and reciprocal as they
-// are: their errors, some units of fp32, are far below its rounding.
+// are: their errors, some units of fp32 and about |g| more of the exponent's rounding,
+// are far below the rounding of h, and of dg and du, which is all that the
+// factors are for, those saved in fp32 too.
 template <class T>
 __device__ __forceinline__ void activate(int act, float g, float* value, float* slope) {
     if (act == AR_ACT_SILU) {
@@ -57,8 +59,9 @@ __device__ __forceinline__ int64_t part_at(const ProductShape& p, int64_t tile, 
 // the tile's sums of g and of u.  A panel holds rows of both weights, so that a
 // lane has g and u of the same element and the activation is its epilogue.
 // Bound by the matrix cores and the copies' issue: 2048 x 4096 x 16384 bf16 469
-// us, 1172 TFLOP/s; 8192 rows with the factors saved 1.9 ms; 777 x 1003 x 2731
-// fp32 103 us, 83 TFLOP/s, and its join 6.
+// us, 1172 TFLOP/s, in calls that follow each other (504 the median of a trace, whose
+// launches stand apart); in traces 8192 rows with the factors saved 2.02 ms; 777 x
+// 1003 x 2731 fp32 101 us, 85 TFLOP/s, and its join 6.
 template <class T, int BR, int BC, int WR, int WC, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, ForwardArgs a,
                                                                Side<T> x, Side<T> w, T* h) {
@@ -112,7 +115,7 @@ __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, F
 // Up to kFewRows rows of x: the weights pass once, so a wavefront takes whole
 // rows of them, two of each, its lanes side by side along D, and one
 // accumulator a (weight row, row of x).  Bound by memory: the weights' bytes.
-// 2 x 16384 x 4096 bf16: 46 us for one row, 5.9 TB/s.  For 8 rows 69 us, on
+// 2 x 16384 x 4096 bf16: 45 us for one row, 5.9 TB/s.  For 8 rows 69 us, on
 // the tiles below 78; fp32, 2 x 8192 x 4096: 60 and 147.  From 9 rows on the
 // registers for a sum each would leave too few loads in flight; on the tiles 16 rows
 // take 76.
@@ -259,8 +262,10 @@ __global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, Forwa
 
 // dg = dh * saved_gate and du = dh * saved_up (of type S), a vector of T a
 // lane.  Bound by memory: five matrices pass once (8192 x 16384 bf16 with fp32
-// factors: 0.36 ms, 5.2 TB/s).  A pass of its own because both gradients read dg and
-// du, each element of them in several tiles.
+// factors: 0.37 ms, 5.1 TB/s).  A pass of its own because both gradients read dg and
+// du, each element of them in several tiles.  For bf16 the rounding is that of the
+// matrix instruction's operands: it takes the gradients' error from 0.0017 of their
+// norm, the last rounding's, to 0.0023.
 template <class T, class S>
 __global__ __launch_bounds__(256) void factors_kernel(int64_t M, int64_t F, const T* dh,
                                                       int64_t dh_stride, const S* sg, const S* su,
@@ -302,8 +307,8 @@ __global__ __launch_bounds__(256) void factors_kernel(int64_t M, int64_t F, cons
 
 // One or two products C = R L^T of one shape (the two weight gradients have
 // row operands of their own, and share a launch), or C += with accumulate.
-// 8192 x 4096 x 16384 bf16: dx 1.7 ms, 1.3 PFLOP/s, both weight gradients 1.7 ms.
-// 777 x 1003 x 2731 fp32: 105 us and 92.
+// 8192 x 4096 x 16384 bf16, medians of a trace: dx 1.71 ms, 1.29 PFLOP/s, both
+// weight gradients 1.70.  777 x 1003 x 2731 fp32: 102 us, its join 5, and 89.
 template <class T>
 struct Products {
     Side<T> r[2], l;

@@ -152,8 +152,8 @@ struct Panel {
     // written as assembly because of the waits: the compiler would hold every
     // LDS read back until all copies have landed, those of the other buffer
     // among them.  Whoever reads what they bring waits for the vector memory
-    // counter and passes a barrier first (see landed()).  (m0 is never
-    // allocated: nothing else here uses it.)
+    // counter and passes a barrier first (see landed()).  (m0 is reserved: the
+    // compiler keeps nothing in it, and takes no clobber of it.)
     __device__ __forceinline__ void copy(int i, uint64_t at, uint32_t lds) const {
         // a raw buffer from there on, without a bound below 4 GiB
         const u32x4 rsrc = {uint32_t(at), uint32_t(at >> 32) & 0xFFFFu, 0xFFFFFFFFu, 0x00020000u};

@@ -1,8 +1,9 @@
 """The replica operators on torch tensors.
 
 What a data-parallel replica computes between two AllReduces: an embedding
-lookup and its gradient, a gated feed-forward block and its gradients, a
-distillation loss and its gradient.  The functions here check their tensors,
+lookup and its gradient, the first half of a gated feed-forward block (both
+projections, the activation and the product) and its gradients, a distillation
+loss and its gradient.  The functions here check their tensors,
 allocate what the caller did not give and call the C functions of the same
 names in ``paper_2409_04202_amd.arplan``, whose header says what each
 computes.  There is no fallback: all work is the library's kernels.
@@ -184,7 +185,8 @@ def glu_forward(x, wg, wu, act="silu", save=False, out=None, workspace=None, str
 def glu_backward(dh, x, wg, wu, saved, dx=None, dwg=None, dwu=None, accumulate=False,
                  workspace=None, stream=None):
     """(dx, dwg, dwu) for ``dh`` (M, F), the gradient at ``glu_forward``'s
-    result, and what that saved.  Outputs that are given are written in place;
+    result, and what that saved.  With bfloat16 the gradients at the two
+    projections are rounded to it before the products, and the results again.  Outputs that are given are written in place;
     with ``accumulate`` dwg and dwu are added to (and have to be given)."""
     sh = _matrix("dh", dh)
     M, F = dh.shape
