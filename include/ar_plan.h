@@ -441,8 +441,10 @@ ar_status ar_genmodel_select_tiered(int32_t n, int64_t N, int32_t dtype, const d
 
 /* What a data-parallel replica computes between two AllReduces, from tokens
  * to the gradients that an ar_plan sums: an embedding lookup and its
- * gradient, a gated feed-forward block and its gradients, and a distillation
- * loss with its gradient.  Common to all of them:
+ * gradient, attention's relative position bias and its gradient, a gated
+ * feed-forward block and its gradients, activations kept in 8 bits, the
+ * routing of tokens to experts with a balance loss and its gradient, and a
+ * distillation loss with its gradient.  Common to all of them:
  *   - dtype is AR_F32 or AR_BF16 (AR_ERR_UNSUPPORTED for AR_I32) and is that
  *     of every matrix.  Sums, softmax statistics and products accumulate in
  *     fp32; a bf16 result is rounded once (round to nearest even) unless the
@@ -497,7 +499,9 @@ ar_status ar_embed_grad(int32_t dtype, int64_t V, int64_t D, int64_t T, const vo
  * rule needs: saved_gate = a'(g) u and saved_up = a(g) (M x F, a common
  * stride; both NULL for a forward pass alone), in saved_dtype: AR_F32, or
  * dtype, rounded once, which takes half of the memory for bf16 and adds a
- * rounding to every gradient. */
+ * rounding to every gradient, or AR_BLOCK8: rows as ar_checkpoint_store makes
+ * them of the fp32 factors, bit for bit (saved_stride in bytes then, pointers
+ * and stride multiples of 16). */
 typedef enum ar_act { AR_ACT_SILU = 0, AR_ACT_GELU = 1 } ar_act;
 #define AR_GLU_MAX_EXTENT 4194304 /* M, D and F (AR_ERR_UNSUPPORTED above) */
 ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_t D, int64_t F,
@@ -518,6 +522,26 @@ ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t F, const 
                           const void* saved_up, int64_t saved_stride, int32_t saved_dtype,
                           int32_t accumulate, void* dx, int64_t dx_stride, void* dwg, void* dwu, int64_t dw_stride,
                           void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Activations kept in 8 bits from a forward to a backward pass: x is M x N, in
+ * `kept` a row is ar_checkpoint_row(N) bytes, its stride in bytes.  Runs of
+ * AR_BLOCK8_RUN elements of a row (from element 0 on; the last may be shorter)
+ * share a power of two 2^e, and an element is held as the whole number
+ * x 2^-e rounded to nearest, ties to even.  e is the least in [-126, 121] for
+ * which no number of the run leaves [-127, 127] (one beyond at 2^121 is held
+ * there), so an element is off by 2^(e-1) at most.  A run with a NaN or an
+ * infinity comes back as NaN, all of it.  What is kept reads as the same values in
+ * fp32 and bf16, exactly.
+ *   A row holds the numbers in whole runs (int8, zeros behind the row), then a
+ * byte a run, e + 127, or 255 for NaN; the bytes behind those are not written.
+ * `kept` and its stride are multiples of 16 (AR_ERR_INVALID_ARG). */
+#define AR_BLOCK8 8 /* a saved_dtype: rows of 8 bits */
+#define AR_BLOCK8_RUN 32
+ar_status ar_checkpoint_row(int64_t N, int64_t* bytes);
+ar_status ar_checkpoint_store(int32_t dtype, int64_t M, int64_t N, const void* x, int64_t x_stride,
+                              void* kept, int64_t kept_stride, void* stream);
+ar_status ar_checkpoint_load(int32_t dtype, int64_t M, int64_t N, const void* kept,
+                             int64_t kept_stride, void* x, int64_t x_stride, void* stream);
 
 /* The larger of the two calls' workspaces (backward == 0: the forward
  * call's alone). */
@@ -551,6 +575,90 @@ ar_status ar_distill(int32_t dtype, int64_t T, int64_t V, int64_t K, const void*
                      int64_t teacher_stride, const int64_t* ids, int64_t ids_stride,
                      float temperature, const float* weights, float* loss, void* grad,
                      int64_t grad_stride, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Attention's relative position bias, from a table of `buckets` x H:
+ *   out[h, i, j] = table[bucket(offset + i - j), h],  i < Q, j < K,
+ * for queries at positions offset, offset + 1, ... and keys at 0, 1, ...  A
+ * side has S buckets: with causal != 0 all of them, for the keys up to the
+ * query's position, and later keys have the bias -inf; with causal == 0 half
+ * of them (`buckets` is even), and keys behind the query take the upper half.
+ * At distance n >= 0 the bucket of a side is n for n < X = S / 2 (rounded
+ * down), and from there on, in logarithmic steps that end at max_distance,
+ *   min(S - 1, X + floor((S - X) log(n / X) / log(max_distance / X))),
+ * taken exactly: n is in bucket X + m or above if n^(S-X) >= X^(S-X-m)
+ * max_distance^m.  A value is the table's, unchanged.  An element of out is at
+ * h head_stride + i row_stride + j; either the rows lie within the heads or
+ * the heads within the rows (AR_ERR_INVALID_ARG where they overlap).
+ *   2 <= S, buckets <= AR_POSITION_MAX_BUCKETS (AR_ERR_UNSUPPORTED above),
+ * X < max_distance, |offset| <= 2^62.  Whether `out` and the table overlap goes
+ * by all of the memory from out's first to its last element. */
+#define AR_POSITION_MAX_BUCKETS 256
+ar_status ar_position_bias(int32_t dtype, int32_t buckets, int32_t max_distance, int32_t causal,
+                           int64_t H, int64_t Q, int64_t K, int64_t offset, const void* table,
+                           int64_t table_stride, void* out, int64_t head_stride, int64_t row_stride,
+                           void* stream);
+
+/* The gradient of ar_position_bias' table for a gradient at the bias of each
+ * of B sequences,
+ *   dtable[b, h] = sum of dbias[n, h, i, j] over n < B and i, j of bucket b,
+ * all of it (buckets that no i, j has become zero), or dtable += that with
+ * accumulate != 0; sums in fp32 in an order that the sizes alone decide.  With
+ * causal != 0 what dbias holds at later keys has no effect, NaN included.
+ * Strides of dbias may be any that are not negative, zero (a gradient that is
+ * the same for several) among them, and the memory between its first and its
+ * last element is read, without an effect of what lies between its rows. */
+ar_status ar_position_bias_grad_workspace(int32_t dtype, int32_t buckets, int64_t B, int64_t H,
+                                          int64_t Q, int64_t K, int64_t* bytes);
+ar_status ar_position_bias_grad(int32_t dtype, int32_t buckets, int32_t max_distance, int32_t causal,
+                                int64_t B, int64_t H, int64_t Q, int64_t K, int64_t offset,
+                                const void* dbias, int64_t batch_stride, int64_t head_stride,
+                                int64_t row_stride, int32_t accumulate, void* dtable,
+                                int64_t table_stride, void* workspace, int64_t workspace_bytes,
+                                void* stream);
+
+/* Routing: for each row t of logits (T x E) the k experts of its largest
+ * logits, in falling order, of equal ones the lower expert first (-0 and 0
+ * are equal), and their gates.  With p = softmax of the row,
+ *   ids[t, j]   = the expert, or -1,
+ *   gates[t, j] = p at it, or with normalize != 0 that over their sum,
+ *   counts[e]   = how often expert e is among ids,
+ *   counts[E]   = how many rows are routed,
+ *   mass[e]     = sum of p_te over the rows that are.
+ * ids and gates are T x k with adjacent rows; counts has E + 1 elements, so that
+ * an AR_I32 plan over them gives all replicas' counts and rows.  A row is not
+ * routed where `live` (T bytes; NULL: all 1) is 0 or all its logits are -inf: ids
+ * are -1, gates 0.  An expert whose logit is -inf is absent, never chosen; where
+ * fewer than k are left, the last ids are -1 with gates 0.  A NaN or +inf makes
+ * its row's gates and all of mass NaN; a NaN ranks above every number.
+ * E <= AR_ROUTE_MAX_EXPERTS, k <= AR_ROUTE_MAX_K (AR_ERR_UNSUPPORTED above),
+ * 1 <= k <= E (AR_ERR_INVALID_ARG). */
+#define AR_ROUTE_MAX_EXPERTS 1024
+#define AR_ROUTE_MAX_K 32
+ar_status ar_route_workspace(int64_t T, int64_t E, int64_t k, int64_t* bytes);
+ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, const void* logits,
+                   int64_t logits_stride, const uint8_t* live, int32_t normalize, int64_t* ids,
+                   float* gates, int32_t* counts, float* mass, void* workspace,
+                   int64_t workspace_bytes, void* stream);
+
+/* The balance loss of a routing, with N = counts[E],
+ *   loss = coefficient E / (k N^2) * sum over e of counts[e] mass[e]
+ * (0 for N <= 0), one fp32 number, and with grad (T x E; NULL: the loss alone)
+ * the gradient at the logits of the loss, for counts that do not change, and of
+ * the gates, for dgates = dL/dgates (T x k, adjacent rows; NULL: none):
+ *   c_e = coefficient E counts[e] / (k N^2),  G_te = sum of dgates[t, j] with ids[t, j] = e,
+ *   grad[t, e] = p_te (a_te - sum of p_ti a_ti),  a_te = c_e + G_te, or, with normalize != 0,
+ *   grad[t, e] = p_te (c_e - sum of p_ti c_i) + sum over j with ids[t, j] = e of
+ *                gates_tj (dgates_tj - sum of gates_ti dgates_ti).
+ * logits, ids, k and normalize are ar_route's; counts and N may be all replicas'
+ * (summed by a plan): then the replicas' losses, each with its own mass, add up to
+ * the whole batch's, and so do their gradients.  Rows with ids[t, 0] < 0 have a
+ * gradient of zero, other ids outside [0, E) none of their gate's.  grad may be logits
+ * itself with the same stride (in place).  coefficient is finite
+ * (AR_ERR_INVALID_ARG). */
+ar_status ar_balance(int32_t dtype, int64_t T, int64_t E, int64_t k, const void* logits,
+                     int64_t logits_stride, const int64_t* ids, const int32_t* counts,
+                     const float* mass, float coefficient, int32_t normalize, const float* dgates,
+                     float* loss, void* grad, int64_t grad_stride, void* stream);
 
 /* --------------------------------------------------------------- timing */
 

@@ -110,6 +110,21 @@ _sig = {
     "ar_distill_workspace": [c_int64, c_int64, c_int64, POINTER(c_int64)],
     "ar_distill": [c_int32, c_int64, c_int64, c_int64, _P, c_int64, c_int32, _P, c_int64, _P,
                    c_int64, c_float, _P, _P, _P, c_int64, _P, c_int64, _P],
+    "ar_checkpoint_row": [c_int64, POINTER(c_int64)],
+    "ar_checkpoint_store": [c_int32, c_int64, c_int64, _P, c_int64, _P, c_int64, _P],
+    "ar_checkpoint_load": [c_int32, c_int64, c_int64, _P, c_int64, _P, c_int64, _P],
+    "ar_position_bias": [c_int32, c_int32, c_int32, c_int32, c_int64, c_int64, c_int64, c_int64, _P,
+                         c_int64, _P, c_int64, c_int64, _P],
+    "ar_position_bias_grad_workspace": [c_int32, c_int32, c_int64, c_int64, c_int64, c_int64,
+                                        POINTER(c_int64)],
+    "ar_position_bias_grad": [c_int32, c_int32, c_int32, c_int32, c_int64, c_int64, c_int64, c_int64,
+                              c_int64, _P, c_int64, c_int64, c_int64, c_int32, _P, c_int64, _P,
+                              c_int64, _P],
+    "ar_route_workspace": [c_int64, c_int64, c_int64, POINTER(c_int64)],
+    "ar_route": [c_int32, c_int64, c_int64, c_int64, _P, c_int64, _P, c_int32, _P, _P, _P, _P, _P,
+                 c_int64, _P],
+    "ar_balance": [c_int32, c_int64, c_int64, c_int64, _P, c_int64, _P, _P, _P, c_float, c_int32, _P,
+                   _P, _P, c_int64, _P],
     "ar_timer_create": [c_int64, POINTER(_P)],
     "ar_timer_reset": [_P],
     "ar_timer_read": [_P, c_int64, POINTER(c_int64), POINTER(c_int32),
@@ -385,6 +400,9 @@ AR_EMBED_RUN = 32
 AR_DISTILL_MAX_K = 4096
 AR_DISTILL_MIN_TEMPERATURE, AR_DISTILL_MAX_TEMPERATURE = 1e-37, 1e19
 AR_GLU_MAX_EXTENT = 4194304
+AR_BLOCK8, AR_BLOCK8_RUN = 8, 32
+AR_POSITION_MAX_BUCKETS = 256
+AR_ROUTE_MAX_EXPERTS, AR_ROUTE_MAX_K = 1024, 32
 
 
 def ar_embed_lookup(dtype, V, D, T, table, table_stride, ids, scale, out, out_stride, stream=None):
@@ -450,6 +468,67 @@ def ar_distill(dtype, T, V, K, logits, logits_stride, teacher_dtype, teacher, te
                            _dtype(teacher_dtype), _ptr(teacher), teacher_stride, _ptr(ids),
                            ids_stride, temperature, _ptr(weights), _ptr(loss), _ptr(grad),
                            grad_stride, _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ar_checkpoint_row(N):
+    """A row's bytes."""
+    b = c_int64()
+    _check(_lib.ar_checkpoint_row(N, ctypes.byref(b)))
+    return b.value
+
+
+def ar_checkpoint_store(dtype, M, N, x, x_stride, kept, kept_stride, stream=None):
+    _check(_lib.ar_checkpoint_store(_dtype(dtype), M, N, _ptr(x), x_stride, _ptr(kept), kept_stride,
+                                    _stream(stream)))
+
+
+def ar_checkpoint_load(dtype, M, N, kept, kept_stride, x, x_stride, stream=None):
+    _check(_lib.ar_checkpoint_load(_dtype(dtype), M, N, _ptr(kept), kept_stride, _ptr(x), x_stride,
+                                   _stream(stream)))
+
+
+def ar_position_bias(dtype, buckets, max_distance, causal, H, Q, K, offset, table, table_stride, out,
+                     head_stride, row_stride, stream=None):
+    _check(_lib.ar_position_bias(_dtype(dtype), buckets, max_distance, int(causal), H, Q, K, offset,
+                                 _ptr(table), table_stride, _ptr(out), head_stride, row_stride,
+                                 _stream(stream)))
+
+
+def ar_position_bias_grad_workspace(dtype, buckets, B, H, Q, K):
+    """The workspace's bytes."""
+    b = c_int64()
+    _check(_lib.ar_position_bias_grad_workspace(_dtype(dtype), buckets, B, H, Q, K, ctypes.byref(b)))
+    return b.value
+
+
+def ar_position_bias_grad(dtype, buckets, max_distance, causal, B, H, Q, K, offset, dbias,
+                          batch_stride, head_stride, row_stride, accumulate, dtable, table_stride,
+                          workspace, workspace_bytes, stream=None):
+    _check(_lib.ar_position_bias_grad(_dtype(dtype), buckets, max_distance, int(causal), B, H, Q, K,
+                                      offset, _ptr(dbias), batch_stride, head_stride, row_stride,
+                                      int(accumulate), _ptr(dtable), table_stride, _ptr(workspace),
+                                      workspace_bytes, _stream(stream)))
+
+
+def ar_route_workspace(T, E, k):
+    """The workspace's bytes."""
+    b = c_int64()
+    _check(_lib.ar_route_workspace(T, E, k, ctypes.byref(b)))
+    return b.value
+
+
+def ar_route(dtype, T, E, k, logits, logits_stride, live, normalize, ids, gates, counts, mass,
+             workspace, workspace_bytes, stream=None):
+    _check(_lib.ar_route(_dtype(dtype), T, E, k, _ptr(logits), logits_stride, _ptr(live),
+                         int(normalize), _ptr(ids), _ptr(gates), _ptr(counts), _ptr(mass),
+                         _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ar_balance(dtype, T, E, k, logits, logits_stride, ids, counts, mass, coefficient, normalize,
+               dgates, loss, grad, grad_stride, stream=None):
+    _check(_lib.ar_balance(_dtype(dtype), T, E, k, _ptr(logits), logits_stride, _ptr(ids),
+                           _ptr(counts), _ptr(mass), coefficient, int(normalize), _ptr(dgates),
+                           _ptr(loss), _ptr(grad), grad_stride, _stream(stream)))
 
 
 # ---------------------------------------------------------------- timing

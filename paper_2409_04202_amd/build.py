@@ -4,7 +4,8 @@ Run ``python -m paper_2409_04202_amd.build`` (or ``__graft_entry__.build()``).
 The plan library and the C ABI (plan.cpp, capi.cpp) are compiled with the
 host compiler; the executor (exec.hip, and its host-side planning in
 rewrite.cpp, schedule.cpp, programs.cpp and onepass.cpp, which share its HIP types) and the
-replica operators (``replica/``: embed.hip, distill.hip, glu.hip, their checks) with
+replica operators (``replica/``: embed.hip, bias.hip, glu.hip, checkpoint.hip, route.hip,
+distill.hip, their checks) with
 ``hipcc --offload-arch=gfx950``; hipcc links the shared library.  The
 objects are compiled in parallel and always from scratch.
 
@@ -34,7 +35,8 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 HOST_SRCS = ["plan.cpp", "capi.cpp", "genmodel.cpp"]
 HIP_SRCS = ["exec.hip", "rewrite.cpp", "schedule.cpp", "programs.cpp", "onepass.cpp",
-            "replica/checks.cpp", "replica/embed.hip", "replica/distill.hip", "replica/glu.hip"]
+            "replica/checks.cpp", "replica/embed.hip", "replica/bias.hip", "replica/glu.hip",
+            "replica/checkpoint.hip", "replica/route.hip", "replica/distill.hip"]
 CHECK_SRCS = ["debug.cpp"]          # compiled as HIP, linked into the check library only
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall",

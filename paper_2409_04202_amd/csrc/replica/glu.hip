@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "block8.hpp"
 #include "product.hpp"
 
 namespace arp {
@@ -44,10 +45,40 @@ __device__ __forceinline__ void activate(int act, float g, float* value, float* 
 struct ForwardArgs {
     int64_t h_stride, saved_stride;
     int act;
-    // the saved factors, or NULL: in fp32, or in the matrices' type
+    // the saved factors, or NULL: in fp32, in the matrices' type, or in 8 bits
     void *sg, *su;
-    bool saved_f32;
+    bool saved_f32, saved_8;
 };
+
+// A square's 32 x 32 values to rows of 8 bits: a row's 32 are a run, two lanes hold
+// it, and columns behind the matrix' last are zeros.
+__device__ __forceinline__ void store_runs(const AR_LDS float* part, uint8_t* out, int64_t stride,
+                                           int64_t r0, int64_t rows, int64_t c0, int64_t cols) {
+    const int lane = int(threadIdx.x) & 63, c = (lane & 1) * 16;
+    if (c0 >= cols) return;
+#pragma unroll
+    for (int b = 0; b < 32; b += 32) {
+        const int r = b + (lane >> 1);
+        const AR_LDS float* const row = part + r * Store<1>::PITCH + c;
+        float v[16];
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            v[e] = c0 + c + e < cols ? row[e] : 0.0f;
+            top = max(top, magnitude(v[e]));
+        }
+        top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0xB1, 0xF, 0xF, true)));
+        const uint32_t byte = run_byte(top);
+        const float inverse = run_inverse(byte);
+        if (r0 + r >= rows) continue;
+        uint8_t* const to = out + (r0 + r) * stride;
+        u32x4 codes;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) codes[i] = four_numbers(v + 4 * i, inverse);
+        *(AR_GLOBAL u32x4*)(to + c0 + c) = codes;
+        if (c == 0) to[runs_of(cols) * kRun + c0 / kRun] = uint8_t(byte);
+    }
+}
 
 // Where the sums of a part of a tile (rows x cols) are.
 __device__ __forceinline__ int64_t part_at(const ProductShape& p, int64_t tile, int split, int rows,
@@ -107,8 +138,20 @@ __global__ __launch_bounds__(64 * WR * WC) void forward_kernel(ProductShape p, F
             pass(sg, a.saved_stride, [&](int, int e) { return slope[e] * acc[i][1][e]; });
             pass(su, a.saved_stride, [&](int, int e) { return value[e]; });
         };
-        if (a.sg && a.saved_f32) save(static_cast<float*>(a.sg), static_cast<float*>(a.su));
-        else if (a.sg) save(static_cast<T*>(a.sg), static_cast<T*>(a.su));
+        auto runs = [&](void* out, auto f) {
+            S::fill(part, f);
+            wave_sync();
+            store_runs(part, static_cast<uint8_t*>(out), a.saved_stride, r0, p.rows, c0, p.cols);
+            wave_sync();
+        };
+        if (a.sg && a.saved_8) {
+            runs(a.sg, [&](int, int e) { return slope[e] * acc[i][1][e]; });
+            runs(a.su, [&](int, int e) { return value[e]; });
+        } else if (a.sg && a.saved_f32) {
+            save(static_cast<float*>(a.sg), static_cast<float*>(a.su));
+        } else if (a.sg) {
+            save(static_cast<T*>(a.sg), static_cast<T*>(a.su));
+        }
     }
 }
 
@@ -216,6 +259,24 @@ __device__ __forceinline__ void store_four(T* p, const float* v, int64_t n) {
     }
 }
 
+// Four values of a row of 8 bits at columns c on, a multiple of four: the eight lanes
+// that hold a run are in a row.
+__device__ __forceinline__ void store_run_part(uint8_t* row, const float* v, int64_t c, int64_t cols) {
+    float x[4];
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = c + e < cols ? v[e] : 0.0f;
+        top = max(top, magnitude(x[e]));
+    }
+    top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0xB1, 0xF, 0xF, true)));
+    top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0x4E, 0xF, 0xF, true)));
+    top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0x141, 0xF, 0xF, true)));
+    const uint32_t byte = run_byte(top);
+    *(AR_GLOBAL uint32_t*)(row + c) = four_numbers(x, run_inverse(byte));
+    if (c % kRun == 0) row[runs_of(cols) * kRun + c / kRun] = uint8_t(byte);
+}
+
 // The sums of the tiles that are split along k, added in order, to the output:
 // `rows` of a tile and `cols` of the output in it are powers of two.
 template <class T>
@@ -228,7 +289,8 @@ __global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, Forwa
         int64_t rt, ct;
         place_of(p, tile, &rt, &ct);
         const int64_t r = rt * rows + tr, c = ct * cols + tc;
-        if (r >= p.rows || c >= p.cols) continue;
+        // (a run's eight lanes stay together: they are all of this row)
+        if (r >= p.rows || (c & -kRun) >= p.cols) continue;
         float g[4] = {}, u[4] = {};
         for (int s = 0; s < p.splits; ++s) {
             const float* const from = p.part + part_at(p, tile, s, rows, 2 * cols) + tr * (2 * cols) + tc;
@@ -249,7 +311,13 @@ __global__ __launch_bounds__(256) void forward_join_kernel(ProductShape p, Forwa
             g[e] = value[e] * u[e];
         }
         const int64_t left = p.cols - c, at = r * a.saved_stride + c;
+        if (a.sg && a.saved_8) {
+            store_run_part(static_cast<uint8_t*>(a.sg) + r * a.saved_stride, slope, c, p.cols);
+            store_run_part(static_cast<uint8_t*>(a.su) + r * a.saved_stride, value, c, p.cols);
+        }
+        if (left <= 0) continue;
         store_four(h + r * a.h_stride + c, g, left);
+        if (a.saved_8) continue;
         if (a.sg && a.saved_f32) {
             store_four(static_cast<float*>(a.sg) + at, slope, left);
             store_four(static_cast<float*>(a.su) + at, value, left);
@@ -302,6 +370,45 @@ __global__ __launch_bounds__(256) void factors_kernel(int64_t M, int64_t F, cons
         // (their rows are whole vectors: the last one's rest is zero)
         store_vec(dg + r * stride + c, Num<T>::pack(g));
         store_vec(du + r * stride + c, Num<T>::pack(u));
+    }
+}
+
+// The same from factors in 8 bits, 16 elements a lane, half of a run.
+template <class T>
+__global__ __launch_bounds__(256) void factors_8_kernel(int64_t M, int64_t F, const T* dh,
+                                                        int64_t dh_stride, const uint8_t* sg,
+                                                        const uint8_t* su, int64_t saved_stride, T* dg,
+                                                        T* du, int64_t stride) {
+    constexpr int VEC = Num<T>::VEC, N = 16;
+    const int64_t per = (F + N - 1) / N, step = int64_t(gridDim.x) * 256;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < M * per; i += step) {
+        const int64_t r = i / per, c = i % per * N;
+        const T* const pd = dh + r * dh_stride + c;
+        const uint8_t *pg = sg + r * saved_stride, *pu = su + r * saved_stride;
+        const int64_t scale = runs_of(F) * kRun + c / kRun;
+        const u32x4 cg = *(const AR_GLOBAL u32x4*)(pg + c), cu = *(const AR_GLOBAL u32x4*)(pu + c);
+        const float s = run_scale(pg[scale]), t = run_scale(pu[scale]);
+        float g[N], u[N];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            four_values(cg[e], s, g + 4 * e);
+            four_values(cu[e], t, u + 4 * e);
+        }
+#pragma unroll
+        for (int v = 0; v < N; v += VEC) {
+            const int64_t left = F - c - v;
+            if (left <= 0) break;
+            float d[VEC];
+            Num<T>::unpack(left >= VEC ? load_vec(pd + v) : load_part(pd + v, int(left)), d);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                // (a run of NaN ends with the row)
+                g[v + e] = e < left ? g[v + e] * d[e] : 0.0f;
+                u[v + e] = e < left ? u[v + e] * d[e] : 0.0f;
+            }
+            store_vec(dg + r * stride + c + v, Num<T>::pack(g + v));
+            store_vec(du + r * stride + c + v, Num<T>::pack(u + v));
+        }
     }
 }
 
@@ -510,7 +617,7 @@ void launch_forward(const ProductShape& p, const ForwardArgs& a, const Side<T>& 
 template <class T>
 void run_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Side<T>& x,
                  const Side<T>& w, T* h, void* part, hipStream_t st) {
-    if (M <= kFewRows) {
+    if (M <= kFewRows && !a.saved_8) {
         const dim3 grid(unsigned(ceil_div(F, 8))), block(256);
         auto go = [&](auto rows) {
             hipLaunchKernelGGL((few_rows_kernel<T, decltype(rows)::value>), grid, block, 0, st, M, D,
@@ -522,7 +629,9 @@ void run_forward(const ForwardArgs& a, int64_t M, int64_t D, int64_t F, const Si
         else go(std::integral_constant<int, 8>{});
         return;
     }
-    const Cut c = cut_of(M, F, D, 1, int(sizeof(T)), true);
+    // (few rows with factors in 8 bits, whose runs no wavefront above has: on tiles that
+    // need no workspace, as the rows do)
+    const Cut c = M <= kFewRows ? Cut{64, 1, 0} : cut_of(M, F, D, 1, int(sizeof(T)), true);
     const ProductShape p = shape(M, F, D, 1, c, c.tile / 2, 1, part);
     const bool fast = direct(x, true) && direct(w, true);
     if (c.tile == 256) launch_forward<T, 256, 2, 4>(p, a, x, w, h, fast, st);
@@ -606,10 +715,24 @@ BackSpace back_space(int64_t M, int64_t D, int64_t F, int esize) {
 using namespace arp;
 
 static ar_status check_saved_dtype(int32_t dtype, int32_t saved, int32_t* esize) {
+    if (saved == AR_BLOCK8) {
+        *esize = 1;
+        return AR_OK;
+    }
     AR_TRY(check_dtype("saved_dtype", saved, esize));
     if (saved != dtype && saved != AR_F32)
         return fail(AR_ERR_UNSUPPORTED, "saved_dtype is dtype or AR_F32");
     return AR_OK;
+}
+
+// Elements of a saved row, or its bytes in 8 bits.
+static int64_t saved_width(int64_t F, int32_t saved) {
+    return saved == AR_BLOCK8 ? block8_row(F) : F;
+}
+static ar_status check_saved_rows(const MatArg& gate, const MatArg& up, int32_t saved, int64_t F) {
+    if (saved != AR_BLOCK8) return AR_OK;
+    AR_TRY(check_block8(gate.name, gate.ptr, gate.rows, F, gate.stride));
+    return check_block8(up.name, up.ptr, up.rows, F, up.stride);
 }
 
 static ar_status check_glu_sizes(int64_t M, int64_t D, int64_t F) {
@@ -657,10 +780,11 @@ AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_
     const int64_t sr = saved_gate ? M : 0;
     const MatArg mx{"x", x, M, D, x_stride, es}, mg{"wg", wg, F, D, w_stride, es},
         mu{"wu", wu, F, D, w_stride, es}, mh{"h", h, M, F, h_stride, es},
-        sg{"saved_gate", saved_gate, sr, F, saved_stride, ss},
-        su{"saved_up", saved_up, sr, F, saved_stride, ss},
+        sg{"saved_gate", saved_gate, sr, saved_width(F, saved_dtype), saved_stride, ss},
+        su{"saved_up", saved_up, sr, saved_width(F, saved_dtype), saved_stride, ss},
         mw{"the workspace", workspace, 1, need, need, 1};
     for (const MatArg& m : {mx, mg, mu, mh, sg, su}) AR_TRY(check_matrix(m));
+    AR_TRY(check_saved_rows(sg, su, saved_dtype, F));
     AR_TRY(check_workspace(workspace, workspace_bytes, need));
     for (const MatArg& o : {mh, sg, su, mw})
         for (const MatArg& i : {mx, mg, mu}) AR_TRY(check_apart(o, i));
@@ -668,7 +792,8 @@ AR_EXPORT ar_status ar_glu_forward(int32_t dtype, int32_t act, int64_t M, int64_
     for (const MatArg& o : {su, mw}) AR_TRY(check_apart(o, sg));
     AR_TRY(check_apart(mw, su));
     if (M == 0 || F == 0) return AR_OK;
-    const ForwardArgs a{h_stride, saved_stride, act, saved_gate, saved_up, saved_dtype == AR_F32};
+    const ForwardArgs a{h_stride, saved_stride, act, saved_gate, saved_up, saved_dtype == AR_F32,
+                        saved_dtype == AR_BLOCK8};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     auto go = [&](auto zero) {
         using T = decltype(zero);
@@ -703,12 +828,13 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
         return fail(AR_ERR_INVALID_ARG, "dwg and dwu are given together");
     const MatArg mh{"dh", dh, M, F, dh_stride, es}, mx{"x", x, dwg ? M : 0, D, x_stride, es},
         mg{"wg", wg, dx ? F : 0, D, w_stride, es}, mu{"wu", wu, dx ? F : 0, D, w_stride, es},
-        sg{"saved_gate", saved_gate, M, F, saved_stride, ss},
-        su{"saved_up", saved_up, M, F, saved_stride, ss},
+        sg{"saved_gate", saved_gate, M, saved_width(F, saved_dtype), saved_stride, ss},
+        su{"saved_up", saved_up, M, saved_width(F, saved_dtype), saved_stride, ss},
         ox{"dx", dx, dx ? M : 0, D, dx_stride, es},
         og{"dwg", dwg, dwg ? F : 0, D, dw_stride, es}, ou{"dwu", dwu, dwg ? F : 0, D, dw_stride, es},
         mw{"the workspace", workspace, 1, need, need, 1};
     for (const MatArg& m : {mh, mx, mg, mu, sg, su, ox, og, ou}) AR_TRY(check_matrix(m));
+    AR_TRY(check_saved_rows(sg, su, saved_dtype, F));
     AR_TRY(check_workspace(workspace, workspace_bytes, need));
     for (const MatArg& o : {ox, og, ou, mw})
         for (const MatArg& i : {mh, mx, mg, mu, sg, su}) AR_TRY(check_apart(o, i));
@@ -732,7 +858,13 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
                                saved_stride, dg, du, fs);
         };
         if (M > 0 && F > 0) {
-            if (saved_dtype == AR_F32) factors(float(0));
+            if (saved_dtype == AR_BLOCK8)
+                hipLaunchKernelGGL((factors_8_kernel<T>),
+                                   dim3(unsigned(std::min<int64_t>(ceil_div(M * ceil_div(F, 16), 256), 1 << 16))),
+                                   dim3(256), 0, st, M, F, static_cast<const T*>(dh), dh_stride,
+                                   static_cast<const uint8_t*>(saved_gate),
+                                   static_cast<const uint8_t*>(saved_up), saved_stride, dg, du, fs);
+            else if (saved_dtype == AR_F32) factors(float(0));
             else factors(T(0));
         }
         const BackSpace space = back_space(M, D, F, es);

@@ -1,9 +1,11 @@
 """The replica operators on torch tensors.
 
 What a data-parallel replica computes between two AllReduces: an embedding
-lookup and its gradient, the first half of a gated feed-forward block (both
-projections, the activation and the product) and its gradients, a distillation
-loss and its gradient.  The functions here check their tensors,
+lookup and its gradient, attention's relative position bias and its gradient,
+the first half of a gated feed-forward block (both projections, the activation
+and the product) and its gradients, activations kept in 8 bits, the routing of
+tokens to experts with a balance loss and its gradient, a distillation loss
+and its gradient.  The functions here check their tensors,
 allocate what the caller did not give and call the C functions of the same
 names in ``paper_2409_04202_amd.arplan``, whose header says what each
 computes.  There is no fallback: all work is the library's kernels.
@@ -33,6 +35,8 @@ from torch.autograd.graph import increment_version
 from . import arplan
 
 _DT = {torch.float32: arplan.AR_F32, torch.bfloat16: arplan.AR_BF16}
+_MOST = (1 << 31) - 1
+_SAVED = {**_DT, torch.uint8: arplan.AR_BLOCK8}
 
 
 def _matrix(name, x, shape=None, like=None):
@@ -53,6 +57,22 @@ def _matrix(name, x, shape=None, like=None):
     if cols > 1 and x.stride(1) != 1:
         raise ValueError("%s: the elements of a row have to be adjacent" % name)
     return x.stride(0) if rows > 1 else max(cols, 1)
+
+
+def _strides(name, x, shape, like):
+    """The strides of all but the last dimension, after the checks."""
+    if not isinstance(x, torch.Tensor) or tuple(x.shape) != tuple(shape):
+        raise ValueError("%s: shape %s expected" % (name, tuple(shape)))
+    if x.dtype != like.dtype or x.device != like.device:
+        raise ValueError("%s: type and device differ from the first operand's" % name)
+    if x.shape[-1] > 1 and x.stride(-1) != 1:
+        raise ValueError("%s: the elements of a row have to be adjacent" % name)
+    return x.stride()[:-1]
+
+
+def _whole(name, v, low, high):
+    if not isinstance(v, int) or not low <= v <= high:
+        raise ValueError("%s: a whole number from %d to %d expected" % (name, low, high))
 
 
 def _ids(name, ids, like):
@@ -151,12 +171,63 @@ def embed_grad(dout, ids, dtable, scale=1.0, accumulate=False, workspace=None, s
     return dtable
 
 
+# --------------------------------------------------------- position bias
+
+def position_bias(table, queries, keys, max_distance=128, offset=0, causal=False, out=None,
+                  stream=None):
+    """Attention's relative position bias (H, queries, keys) from ``table``
+    (buckets, H), for queries at positions ``offset`` on and keys at 0 on; with
+    ``causal`` all buckets are the past's and later keys have -inf.  ``out``
+    may have any strides of heads and rows, a slice of a wider tensor's among
+    them."""
+    st = _matrix("table", table)
+    buckets, H = table.shape
+    for name, v in (("queries", queries), ("keys", keys)):
+        _whole(name, v, 0, _MOST)
+    _whole("max_distance", max_distance, 1, _MOST)
+    _whole("offset", offset, -1 << 62, 1 << 62)
+    with _on(table, stream, (table, out), (out,)) as s:
+        res = out
+        if out is None:
+            res = torch.empty(H, queries, keys, dtype=table.dtype, device=table.device)
+        sh, sr = _strides("out", res, (H, queries, keys), table)
+        arplan.ar_position_bias(_DT[table.dtype], buckets, max_distance, causal, H, queries, keys,
+                                offset, table, st, res, sh, sr, s)
+    return res
+
+
+def position_bias_grad(dbias, dtable, max_distance=128, offset=0, causal=False, accumulate=False,
+                       workspace=None, stream=None):
+    """The gradient of ``position_bias``'s table for ``dbias`` (B, H, queries,
+    keys) or (H, queries, keys), summed over the batch and stored into
+    ``dtable`` (buckets, H), all of it, or added to it; returns ``dtable``."""
+    st = _matrix("dtable", dtable)
+    if isinstance(dbias, torch.Tensor) and dbias.dim() == 3:
+        dbias = dbias[None]
+    if not isinstance(dbias, torch.Tensor) or dbias.dim() != 4:
+        raise ValueError("dbias: a (batch, heads, queries, keys) tensor expected")
+    _whole("max_distance", max_distance, 1, _MOST)
+    _whole("offset", offset, -1 << 62, 1 << 62)
+    B, H, Q, K = dbias.shape
+    buckets = dtable.shape[0]
+    if dtable.shape[1] != H:
+        raise ValueError("dtable: a column for each of dbias's heads expected")
+    sb, sh, sr = _strides("dbias", dbias, (B, H, Q, K), dtable)
+    with _on(dbias, stream, (dbias, dtable, workspace), (dtable,)) as s:
+        need = arplan.ar_position_bias_grad_workspace(_DT[dbias.dtype], buckets, B, H, Q, K)
+        w, n, keep = _space(workspace, need, dbias)
+        arplan.ar_position_bias_grad(_DT[dbias.dtype], buckets, max_distance, causal, B, H, Q, K,
+                                     offset, dbias, sb, sh, sr, accumulate, dtable, st, w, n, s)
+    return dtable
+
+
 # ---------------------------------------------------- gated feed-forward
 
 def glu_forward(x, wg, wu, act="silu", save=False, out=None, workspace=None, stream=None):
     """``act(x wg^T) * (x wu^T)`` for x (M, D) and wg, wu (F, D): (M, F).  With
     ``save`` returns it and what ``glu_backward`` needs, a (2, M, F) tensor:
-    ``True`` in float32, a dtype (float32 or x's) in that."""
+    ``True`` in float32, a dtype (float32 or x's) in that; ``torch.uint8`` in 8
+    bits, a (2, M, row) tensor of rows as ``checkpoint_store`` makes them."""
     sx = _matrix("x", x)
     M, D = x.shape
     sw = _matrix("wg", wg, None, x)
@@ -172,13 +243,14 @@ def glu_forward(x, wg, wu, act="silu", save=False, out=None, workspace=None, str
         h = torch.empty(M, F, dtype=x.dtype, device=x.device) if out is None else out
         sh = _matrix("out", h, (M, F), x)
         kind = torch.float32 if save in (True, False, None) else save
-        if kind not in (torch.float32, x.dtype):
-            raise ValueError("save: True, float32 or x's type expected")
-        saved = torch.empty(2, M, F, dtype=kind, device=x.device) if save else None
+        if kind not in (torch.float32, x.dtype, torch.uint8):
+            raise ValueError("save: True, float32, x's type or uint8 expected")
+        width = arplan.ar_checkpoint_row(F) if kind == torch.uint8 else F
+        saved = torch.empty(2, M, width, dtype=kind, device=x.device) if save else None
         a, b = (saved[0], saved[1]) if save else (None, None)
         w, n, keep = _space(workspace, arplan.ar_glu_workspace(_DT[x.dtype], M, D, F, False), x)
         arplan.ar_glu_forward(_DT[x.dtype], act, M, D, F, x, sx, wg, wu, sw, h, sh, a, b,
-                              max(F, 1), w, n, s, saved_dtype=_DT[kind])
+                              max(width, 1), w, n, s, saved_dtype=_SAVED[kind])
     return (h, saved) if save else h
 
 
@@ -200,11 +272,15 @@ def glu_backward(dh, x, wg, wu, saved, dx=None, dwg=None, dwu=None, accumulate=F
     if (not isinstance(saved, torch.Tensor) or saved.dim() != 3 or saved.shape[0] != 2):
         raise ValueError("saved: what glu_forward saved expected")
     sg, su = saved[0], saved[1]
-    if saved.dtype not in (torch.float32, dh.dtype) or saved.device != dh.device:
-        raise ValueError("saved: float32 or dh's type on dh's device expected")
-    ss = _matrix("saved", sg, (M, F))
-    if _matrix("saved", su, (M, F)) != ss:
-        raise ValueError("saved: one row stride expected")
+    if saved.dtype not in (torch.float32, dh.dtype, torch.uint8) or saved.device != dh.device:
+        raise ValueError("saved: float32, dh's type or uint8 on dh's device expected")
+    if saved.dtype == torch.uint8:
+        ss = _kept("saved", sg, M, F)
+        _kept("saved", su, M, F)
+    else:
+        ss = _matrix("saved", sg, (M, F))
+        if _matrix("saved", su, (M, F)) != ss:
+            raise ValueError("saved: one row stride expected")
     if (dwg is None) != (dwu is None):
         raise ValueError("dwg and dwu are given together")
     if accumulate and dwg is None:
@@ -221,8 +297,130 @@ def glu_backward(dh, x, wg, wu, saved, dx=None, dwg=None, dwu=None, accumulate=F
         w, n, keep = _space(workspace, arplan.ar_glu_workspace(_DT[dh.dtype], M, D, F, True), dh)
         arplan.ar_glu_backward(_DT[dh.dtype], M, D, F, dh, sh, x, sx, wg, wu, sw, sg, su, ss,
                                accumulate, dx, sdx, dwg, dwu, sdw, w, n, s,
-                               saved_dtype=_DT[saved.dtype])
+                               saved_dtype=_SAVED[saved.dtype])
     return dx, dwg, dwu
+
+
+# ------------------------------------------------- activations in 8 bits
+
+def _kept(name, x, rows, width):
+    """The row stride of rows in 8 bits."""
+    if (not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype != torch.uint8 or not x.is_cuda):
+        raise ValueError("%s: a two-dimensional uint8 tensor on a GPU expected" % name)
+    if rows is not None and x.shape[0] != rows:
+        raise ValueError("%s: %d rows expected, got %d" % (name, rows, x.shape[0]))
+    need = arplan.ar_checkpoint_row(width)
+    if x.shape[1] < need or (need > 1 and x.stride(1) != 1):
+        raise ValueError("%s: rows of %d adjacent bytes expected" % (name, need))
+    return x.stride(0) if x.shape[0] > 1 else need
+
+
+def checkpoint_store(x, out=None, stream=None):
+    """``x`` (M, N) in 8 bits for a later pass: a uint8 (M, row) tensor, ``row``
+    being ``arplan.ar_checkpoint_row(N)``, or ``out``, which may be wider.  32
+    elements of a row share a power of two; each is off by half a unit of that at
+    most, 2^-7 of the largest of the 32."""
+    sx = _matrix("x", x)
+    M, N = x.shape
+    with _on(x, stream, (x, out), (out,)) as s:
+        res = out
+        if out is None:
+            res = torch.empty(M, arplan.ar_checkpoint_row(N), dtype=torch.uint8, device=x.device)
+        sk = _kept("out", res, M, N)
+        if res.device != x.device:
+            raise ValueError("out: on x's device expected")
+        arplan.ar_checkpoint_store(_DT[x.dtype], M, N, x, sx, res, sk, s)
+    return res
+
+
+def checkpoint_load(kept, width, dtype=None, out=None, stream=None):
+    """The (M, ``width``) values that ``kept`` holds, exactly, as ``dtype``
+    (float32 or bfloat16) or into ``out``."""
+    sk = _kept("kept", kept, None, width)
+    M = kept.shape[0]
+    if out is None and dtype not in _DT:
+        raise ValueError("dtype: float32 or bfloat16 expected")
+    with _on(kept, stream, (kept, out), (out,)) as s:
+        res = torch.empty(M, width, dtype=dtype, device=kept.device) if out is None else out
+        sx = _matrix("out", res, (M, width))
+        if res.device != kept.device or (dtype is not None and res.dtype != dtype):
+            raise ValueError("out: of dtype and on kept's device expected")
+        arplan.ar_checkpoint_load(_DT[res.dtype], M, width, kept, sk, res, sx, s)
+    return res
+
+
+# --------------------------------------------------------------- routing
+
+def _vector(name, x, n, dtype, like):
+    if (not isinstance(x, torch.Tensor) or x.shape != (n,) or x.dtype != dtype
+            or x.device != like.device or not x.is_contiguous()):
+        raise ValueError("%s: a contiguous %s vector of %d on the operands' device expected"
+                         % (name, str(dtype)[6:], n))
+
+
+def _choices(name, x, shape, dtype, like):
+    if (not isinstance(x, torch.Tensor) or tuple(x.shape) != tuple(shape) or x.dtype != dtype
+            or x.device != like.device or not x.is_contiguous()):
+        raise ValueError("%s: a contiguous %s tensor of shape %s on the operands' device expected"
+                         % (name, str(dtype)[6:], tuple(shape)))
+
+
+def route(logits, k, live=None, normalize=False, counts=None, mass=None, workspace=None,
+          stream=None):
+    """The ``k`` experts of each row of ``logits`` (T, E): (ids, gates, counts,
+    mass) with int64 ids (T, k), -1 where there is none, float32 gates (T, k) (the
+    softmax there; with ``normalize`` over their sum), int32 counts (E + 1,) (how
+    often each expert was chosen, and how many rows were routed) and float32 mass
+    (E,) (the probabilities' sums).  Rows whose ``live`` (bool (T,)) is false are
+    padding.  ``counts`` and ``mass`` may be given, such as a slice of the vector
+    that an int32 plan sums."""
+    sl = _matrix("logits", logits)
+    T, E = logits.shape
+    if live is not None:
+        _vector("live", live, T, torch.bool, logits)
+    with _on(logits, stream, (logits, live, counts, mass, workspace), (counts, mass)) as s:
+        dev = logits.device
+        w, n, keep = _space(workspace, arplan.ar_route_workspace(T, E, k), logits)
+        if counts is None:
+            counts = torch.empty(E + 1, dtype=torch.int32, device=dev)
+        if mass is None:
+            mass = torch.empty(E, dtype=torch.float32, device=dev)
+        _vector("counts", counts, E + 1, torch.int32, logits)
+        _vector("mass", mass, E, torch.float32, logits)
+        ids = torch.empty(T, k, dtype=torch.int64, device=dev)
+        gates = torch.empty(T, k, dtype=torch.float32, device=dev)
+        arplan.ar_route(_DT[logits.dtype], T, E, k, logits, sl, live, normalize, ids, gates, counts,
+                        mass, w, n, s)
+    return ids, gates, counts, mass
+
+
+def balance(logits, ids, counts, mass, coefficient=0.01, normalize=False, dgates=None, grad=None,
+            stream=None):
+    """The balance loss of a routing, a float32 scalar: ``coefficient`` times E
+    times the sum over experts of the share of choices times the mean probability.
+    With ``grad`` (T, E; ``logits`` itself for a gradient in place) returns the loss
+    and ``grad``, holding its gradient and that of the gates for ``dgates`` (float32
+    (T, k)).  ``counts`` may be all replicas' (summed by a plan): the replicas'
+    losses and gradients then add up to the whole batch's."""
+    sl = _matrix("logits", logits)
+    T, E = logits.shape
+    _ids("ids", ids, logits)
+    if ids.dim() != 2 or ids.shape[0] != T:
+        raise ValueError("ids: a row for each of logits' expected")
+    k = ids.shape[1]
+    _choices("ids", ids, (T, k), torch.int64, logits)
+    _vector("counts", counts, E + 1, torch.int32, logits)
+    _vector("mass", mass, E, torch.float32, logits)
+    if dgates is not None:
+        _choices("dgates", dgates, (T, k), torch.float32, logits)
+        if grad is None:
+            raise ValueError("dgates: grad has to be given")
+    sg = _matrix("grad", grad, (T, E), logits) if grad is not None else 0
+    with _on(logits, stream, (logits, ids, counts, mass, dgates, grad), (grad,)) as s:
+        loss = torch.empty((), dtype=torch.float32, device=logits.device)
+        arplan.ar_balance(_DT[logits.dtype], T, E, k, logits, sl, ids, counts, mass, coefficient,
+                          normalize, dgates, loss, grad, sg, s)
+    return (loss, grad) if grad is not None else loss
 
 
 # ----------------------------------------------------------- distillation
