@@ -12,46 +12,71 @@
 namespace arp {
 namespace {
 
-constexpr int kBlock = 256;
-constexpr int kMaxParts = 512;  // blocks whose sums are joined
+constexpr int kRouteBlock = 1024, kBalanceBlock = 256;
+constexpr int kMaxParts = 512;  // blocks whose sums are joined: two a CU, all its wavefronts
 
 // exp(x) for x <= 0, to a few units in the last place: 2^(x log2 e) with what the
-// product was rounded by put back.
+// product was rounded by put back.  (Zero below -200; a NaN counts as that: the rows
+// that have one get it back from their sum of zero.)
 __device__ __forceinline__ float exp_below(float x) {
-    const float t = x * 1.44269504f, lost = fmaf(x, 1.44269504f, -t) + x * 1.92596299e-8f;
+    x = fmaxf(x, -200.0f);
+    const float t = x * 1.44269504f, lost = fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269504f, -t));
     const float e = __builtin_amdgcn_exp2f(t);
-    return t > -120.0f ? fmaf(e, lost * 0.69314718f, e) : e;
+    return fmaf(e, lost * 0.69314718f, e);
 }
+// The larger number, or a NaN where there is one.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// Another lane's value: lanes change places in pairs 2^STEP apart, or mirrored
-// within the next larger group, which a reduction does not tell apart.
-template <int STEP>
-__device__ __forceinline__ uint32_t other(uint32_t v) {
-    if constexpr (STEP == 0) return uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0xB1, 0xF, 0xF, true));
-    else if constexpr (STEP == 1) return uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x4E, 0xF, 0xF, true));
-    else if constexpr (STEP == 2) return uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x141, 0xF, 0xF, true));
-    else if constexpr (STEP == 3) return uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x140, 0xF, 0xF, true));
-    else return uint32_t(__shfl_xor(int(v), 1 << STEP));
-}
-template <int LOG, int STEP = 0, class V, class F>
-__device__ __forceinline__ V group_reduce(V v, F&& f) {
-    if constexpr (STEP < LOG) {
-        if constexpr (sizeof(V) == 4) {
-            v = f(v, __builtin_bit_cast(V, other<STEP>(__builtin_bit_cast(uint32_t, v))));
-        } else {
-            const uint32_t lo = other<STEP>(uint32_t(v)), hi = other<STEP>(uint32_t(v >> 32));
-            v = f(v, V(hi) << 32 | lo);
-        }
-        return group_reduce<LOG, STEP + 1>(v, f);
+// v combined with another lane's: lanes change places in pairs 2^STEP apart, or
+// mirrored within the next larger group, which a reduction does not tell apart.
+// (RING: rotated by 4 and by 8 lanes of 16 instead, for sums over all groups, whose
+// lanes are not alike.)
+template <int STEP, bool RING, class F>
+__device__ __forceinline__ uint32_t with_other(uint32_t v, F&& f) {
+    if constexpr (STEP < 4) {
+        constexpr int CTRL = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? (RING ? 0x124 : 0x141)
+                                                                             : (RING ? 0x128 : 0x140);
+        return f(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), CTRL, 0xF, 0xF, true)));
+    } else if constexpr (STEP == 4) {  // rows of 16 lanes: {0, 0, 2, 2} and {1, 1, 3, 3}
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return f(r[0], r[1]);
     } else {
-        return v;
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return f(r[0], r[1]);
     }
 }
+// Over a group's 2^TO lanes, or with FROM over the same lane of all groups; every lane
+// has the result.
+template <int TO, int FROM = 0, bool RING = false, class F>
+__device__ __forceinline__ uint32_t group_reduce(uint32_t v, F&& f) {
+    if constexpr (FROM < TO) return group_reduce<TO, FROM + 1, RING>(with_other<FROM, RING>(v, f), f);
+    else return v;
+}
+struct AddBits {
+    __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }
+};
 template <int LOG> __device__ __forceinline__ float group_sum(float v) {
-    return group_reduce<LOG>(v, [](float a, float b) { return a + b; });
+    return __uint_as_float(group_reduce<LOG>(__float_as_uint(v), AddBits{}));
+}
+template <int LOG> __device__ __forceinline__ float groups_sum(float v) {
+    return __uint_as_float(group_reduce<6, LOG, true>(__float_as_uint(v), AddBits{}));
 }
 template <int LOG> __device__ __forceinline__ float group_max(float v) {
-    return group_reduce<LOG>(v, [](float a, float b) { return fmaxf(a, b); });
+    return __uint_as_float(group_reduce<LOG>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(larger(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
+template <int LOG> __device__ __forceinline__ uint32_t group_most(uint32_t v) {
+    return group_reduce<LOG>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+// The largest of ranks; one of 64 bits by its upper and then its lower half.
+template <int LOG> __device__ __forceinline__ uint32_t group_best(uint32_t v) { return group_most<LOG>(v); }
+template <int LOG> __device__ __forceinline__ uint64_t group_best(uint64_t v) {
+    const uint32_t hi = group_most<LOG>(uint32_t(v >> 32));
+    const uint32_t lo = group_most<LOG>(uint32_t(v >> 32) == hi ? uint32_t(v) : 0u);
+    return uint64_t(hi) << 32 | lo;
 }
 
 // A logit and its place as one number: larger for a larger logit, and of equal
@@ -102,29 +127,47 @@ __device__ __forceinline__ void load_logits(const T* row, int first, int E, floa
     }
 }
 
-// The row's probabilities; false where no logit is above -inf.
+// The row's probabilities and the inverse of their sum, from its largest logit: all NaN
+// where that is a NaN or an infinity.
 template <int LOG, int P>
-__device__ __forceinline__ bool softmax(const float* z, float* p, float* top, float* inverse) {
-    float m = z[0];
-#pragma unroll
-    for (int i = 1; i < P; ++i) m = fmaxf(m, z[i]);
-    m = group_max<LOG>(m);
-    // (a NaN is no maximum: a row of NaN and -inf has a NaN for its sum)
-    float s = 0.0f, any = m;
+__device__ __forceinline__ float softmax(const float* z, float top, float* p) {
+    float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        p[i] = exp_below(z[i] - m);
+        p[i] = exp_below(z[i] - top);
         s += p[i];
-        if (z[i] != z[i]) any = 0.0f;
     }
-    s = group_sum<LOG>(s);
-    any = group_max<LOG>(any);
-    const float r = 1.0f / s;
+    const float inverse = 1.0f / group_sum<LOG>(s);
 #pragma unroll
-    for (int i = 0; i < P; ++i) p[i] *= r;
-    *top = m;
-    *inverse = r;
-    return any != -INFINITY;
+    for (int i = 0; i < P; ++i) p[i] *= inverse;
+    return inverse;
+}
+
+// Compares and exchanges until the larger are in front: merges of sorted halves, odd and
+// even places apart.
+template <int P, class V>
+__device__ __forceinline__ void sort_falling(V& key) {
+#pragma unroll
+    for (int size = 1; size < P; size *= 2)
+#pragma unroll
+        for (int step = size; step > 0; step /= 2)
+#pragma unroll
+            for (int j = step % size; j + step < P; j += 2 * step)
+#pragma unroll
+                for (int i = 0; i < step; ++i)
+                    if (j + i + step < P && (j + i) / (2 * size) == (j + i + step) / (2 * size)) {
+                        const auto a = key[j + i], b = key[j + i + step];
+                        key[j + i] = a > b ? a : b;
+                        key[j + i + step] = a > b ? b : a;
+                    }
+}
+
+// The elements behind the first, and a zero.
+template <int P, class V>
+__device__ __forceinline__ V moved_up(V v) {
+    const V zero = 0;
+    if constexpr (P == 8) return __builtin_shufflevector(v, zero, 1, 2, 3, 4, 5, 6, 7, 8);
+    else return __builtin_shufflevector(v, zero, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 16);
 }
 
 struct RouteArgs {
@@ -142,84 +185,90 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// Bound by the choice's reductions, then by memory.
+// A lane's logits are sorted once; each choice is then a reduction over the lanes'
+// first ones, and the lane that it came from moves on to its next.  Lane j keeps choice
+// j, so gates, counts and stores are made for all of them at once.  Bound by the
+// reductions' instructions.
 template <class T, int LOG, int P>
-__global__ __launch_bounds__(kBlock) void route_kernel(const T* logits, RouteArgs a) {
+__global__ __launch_bounds__(kRouteBlock) void route_kernel(const T* logits, RouteArgs a) {
     using R = Rank<T>;
     using K = typename R::K;
-    constexpr int LANES = 1 << LOG, GROUPS = 64 / LANES, WAVES = kBlock / 64;
+    typedef K V __attribute__((ext_vector_type(P)));
+    constexpr int LANES = 1 << LOG, GROUPS = 64 / LANES, WAVES = kRouteBlock / 64;
     constexpr int WIDE = LANES * P;                     // experts at most
     constexpr int PICKS = WIDE < AR_ROUTE_MAX_K ? WIDE : AR_ROUTE_MAX_K;
+    constexpr int SLOTS = (PICKS + LANES - 1) / LANES;  // choices a lane keeps
     __shared__ int32_t hist[WIDE + 1];
-    __shared__ float sums[WAVES * GROUPS][WIDE];
-    __shared__ int32_t place[WAVES][GROUPS * PICKS];
-    __shared__ float gate[WAVES][GROUPS * PICKS];
+    __shared__ float sums[WAVES][WIDE];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> LOG;
     const int sub = lane & (LANES - 1), first = sub * P;
-    for (int i = threadIdx.x; i <= WIDE; i += kBlock) hist[i] = 0;
+    for (int i = threadIdx.x; i <= WIDE; i += kRouteBlock) hist[i] = 0;
     __syncthreads();
     float mass[P] = {};
     const int64_t step = int64_t(gridDim.x) * WAVES * GROUPS;
     for (int64_t r0 = (int64_t(blockIdx.x) * WAVES + wave) * GROUPS; r0 < a.T; r0 += step) {
         const int64_t r = r0 + group;
-        const bool live = r < a.T && (!a.live || a.live[r]);
-        float z[P], p[P], top, inverse;
-        if (live) {
-            load_logits<T, P>(logits + r * a.stride, first, a.E, z);
-        } else {
+        const bool in = r < a.T;
+        float z[P], p[P];
+        load_logits<T, P>(logits + r * a.stride, in ? first : a.E, a.E, z);
+        const bool live = in && (!a.live || a.live[r]);
+        // (a vector, not an array: a choice between its elements is one of registers)
+        V key;
+        K mine[SLOTS];
 #pragma unroll
-            for (int i = 0; i < P; ++i) z[i] = -INFINITY;
+        for (int i = 0; i < P; ++i) key[i] = live ? R::of(z[i], uint32_t(first + i)) : K(0);
+        sort_falling<P>(key);
+        K best = group_best<LOG>(key[0]);
+        const bool any = best != 0;
+        const float top = R::logit(best), inverse = softmax<LOG, P>(z, top, p);
+#pragma unroll
+        for (int i = 0; i < P; ++i) mass[i] += any ? p[i] : 0.0f;
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            mine[s] = 0;
+            for (int j = 0; j < LANES && s * LANES + j < a.k; ++j) {
+                mine[s] = sub == j ? best : mine[s];
+                key = key[0] == best ? moved_up<P>(key) : key;
+                best = group_best<LOG>(key[0]);
+            }
         }
-        const bool any = softmax<LOG, P>(z, p, &top, &inverse) && live;
-        K key[P];
+        float gate[SLOTS], total = 0.0f;
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            mass[i] += any ? p[i] : 0.0f;
-            key[i] = R::of(z[i], uint32_t(first + i));
+        for (int s = 0; s < SLOTS; ++s) {
+            gate[s] = mine[s] ? exp_below(R::logit(mine[s]) - top) * inverse : 0.0f;
+            total += gate[s];
         }
-        float total = 0.0f;
-        for (int j = 0; j < a.k; ++j) {
-            K best = key[0];
+        float scale = 1.0f;
+        if (a.normalize) {
+            total = group_sum<LOG>(total);
+            scale = any ? 1.0f / total : 0.0f;
+        }
 #pragma unroll
-            for (int i = 1; i < P; ++i) best = key[i] > best ? key[i] : best;
-            best = group_reduce<LOG>(best, [](K x, K y) { return x > y ? x : y; });
-            const bool here = best != 0;
-            const float g = here ? exp_below(R::logit(best) - top) * inverse : 0.0f;
-            total += g;
-#pragma unroll
-            for (int i = 0; i < P; ++i) key[i] = key[i] == best ? K(0) : key[i];
-            if (sub == 0) {
-                const int e = here ? int(R::place(best)) : -1;
-                place[wave][group * a.k + j] = e;
-                gate[wave][group * a.k + j] = g;
-                if (here) atomicAdd(&hist[e], 1);
+        for (int s = 0; s < SLOTS; ++s) {
+            const int j = s * LANES + sub;
+            if (j < a.k && in) {
+                const int e = mine[s] ? int(R::place(mine[s])) : -1;
+                a.ids[r * a.k + j] = e;
+                a.gates[r * a.k + j] = gate[s] * scale;
+                if (mine[s]) atomicAdd(&hist[e], 1);
             }
         }
         if (sub == 0 && any) atomicAdd(&hist[a.E], 1);
-        if (a.normalize) {
-            wave_sync();
-            for (int j = sub; j < a.k; j += LANES)
-                if (any) gate[wave][group * a.k + j] /= total;
-        }
-        wave_sync();
-        // the wavefront's rows are adjacent: so are their choices
-        const int64_t rows = a.T - r0 < GROUPS ? a.T - r0 : GROUPS;
-        for (int i = lane; i < int(rows) * a.k; i += 64) {
-            a.ids[r0 * a.k + i] = place[wave][i];
-            a.gates[r0 * a.k + i] = gate[wave][i];
-        }
-        wave_sync();
     }
 #pragma unroll
-    for (int i = 0; i < P; ++i) sums[wave * GROUPS + group][first + i] = mass[i];
+    for (int i = 0; i < P; ++i) {
+        const float m = groups_sum<LOG>(mass[i]);       // the wavefront's rows
+        if (group == 0) sums[wave][first + i] = m;
+    }
     __syncthreads();
     int32_t* const counts = a.counts + int64_t(blockIdx.x) * (a.E + 1);
     float* const masses = a.mass + int64_t(blockIdx.x) * a.E;
-    for (int e = threadIdx.x; e <= a.E; e += kBlock) {
+    for (int e = threadIdx.x; e <= a.E; e += kRouteBlock) {
         counts[e] = hist[e];
         if (e == a.E) break;
         float s = 0.0f;
-        for (int i = 0; i < WAVES * GROUPS; ++i) s += sums[i][e];
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) s += sums[i][e];
         masses[e] = s;
     }
 }
@@ -234,11 +283,19 @@ __global__ __launch_bounds__(1024) void route_join_kernel(int parts, int E, cons
     const int e = int(blockIdx.x) * 16 + (threadIdx.x & 15), at = threadIdx.x >> 4;
     int32_t n = 0;
     float s = 0.0f;
-    if (e <= E)
-        for (int i = at; i < parts; i += 64) {
-            n += counts[int64_t(i) * (E + 1) + e];
-            if (e < E) s += mass[int64_t(i) * E + e];
-        }
+    int32_t x[kMaxParts / 64];
+    float y[kMaxParts / 64];
+#pragma unroll
+    for (int i = 0; i < kMaxParts / 64; ++i) {
+        const int64_t part = at + 64 * i;
+        x[i] = part < parts && e <= E ? counts[part * (E + 1) + e] : 0;
+        y[i] = part < parts && e < E ? mass[part * E + e] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < kMaxParts / 64; ++i) {
+        n += x[i];
+        s += y[i];
+    }
     c[at][threadIdx.x & 15] = n;
     m[at][threadIdx.x & 15] = s;
     for (int half = 32; half; half >>= 1) {
@@ -263,12 +320,6 @@ struct BalanceArgs {
     float* loss;
 };
 
-// The loss' slope at an expert's probability: coefficient E counts_e / (k N^2).
-__device__ __forceinline__ float slope_of(const BalanceArgs& a, int e) {
-    const float n = float(a.counts[a.E]);
-    return n > 0.0f ? a.coefficient * float(a.E) / float(a.k) * (float(a.counts[e]) / n) / n : 0.0f;
-}
-
 // The loss, by one wavefront, in 64 bits.
 __device__ __forceinline__ void loss_of(const BalanceArgs& a) {
     double s = 0.0;
@@ -280,64 +331,107 @@ __device__ __forceinline__ void loss_of(const BalanceArgs& a) {
 }
 __global__ __launch_bounds__(64) void loss_kernel(BalanceArgs a) { loss_of(a); }
 
-// The gradient, and in the last block the loss.
+// The gradient, and in the last block the loss.  What is chosen reaches the lanes that
+// hold its logits through LDS: a place a logit, with the choice's number (0: none) and
+// its gate's gradient.
 template <class T, int LOG, int P>
-__global__ __launch_bounds__(kBlock) void balance_kernel(const T* logits, T* grad, BalanceArgs a) {
+__global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits, T* grad, BalanceArgs a) {
     constexpr int VEC = Num<T>::VEC;
-    constexpr int LANES = 1 << LOG, GROUPS = 64 / LANES, WAVES = kBlock / 64;
+    constexpr int LANES = 1 << LOG, GROUPS = 64 / LANES, WAVES = kBalanceBlock / 64, WIDE = LANES * P;
+    constexpr int PICKS = WIDE < AR_ROUTE_MAX_K ? WIDE : AR_ROUTE_MAX_K;
+    constexpr int SLOTS = (PICKS + LANES - 1) / LANES;
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    __shared__ __attribute__((aligned(16))) int chosen[WAVES][64 * P];
+    __shared__ __attribute__((aligned(16))) float wanted[WAVES][64 * P];
     if (blockIdx.x == gridDim.x - 1) {
         if (threadIdx.x < 64) loss_of(a);
         return;
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> LOG;
-    const int first = (lane & (LANES - 1)) * P;
+    const int sub = lane & (LANES - 1), first = sub * P;
+    // the slopes of the loss: coefficient E counts_e / (k N^2)
+    const float n = float(a.counts[a.E]);
+    const float unit = n > 0.0f ? a.coefficient * float(a.E) / float(a.k) / n / n : 0.0f;
     float slope[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i) slope[i] = first + i < a.E ? slope_of(a, first + i) : 0.0f;
+    for (int i = 0; i < P; ++i) slope[i] = first + i < a.E ? float(a.counts[first + i]) * unit : 0.0f;
     const int64_t step = int64_t(gridDim.x - 1) * WAVES * GROUPS;
     for (int64_t r0 = (int64_t(blockIdx.x) * WAVES + wave) * GROUPS; r0 < a.T; r0 += step) {
         const int64_t r = r0 + group;
-        const int64_t* const ids = a.ids + r * a.k;
-        const bool live = r < a.T && ids[0] >= 0;
-        float z[P], p[P], top, inverse;
-        if (live) {
-            load_logits<T, P>(logits + r * a.stride, first, a.E, z);
-        } else {
+        const bool in = r < a.T;
+        float z[P], p[P];
+        load_logits<T, P>(logits + r * a.stride, in ? first : a.E, a.E, z);
+        int64_t id[SLOTS];
+        float g[SLOTS];
 #pragma unroll
-            for (int i = 0; i < P; ++i) z[i] = -INFINITY;
+        for (int s = 0; s < SLOTS; ++s) {
+            const int j = s * LANES + sub;
+            const bool here = in && j < a.k;
+            id[s] = here ? a.ids[r * a.k + j] : -1;
+            g[s] = here && a.dgates ? a.dgates[r * a.k + j] : 0.0f;
         }
-        const bool any = softmax<LOG, P>(z, p, &top, &inverse) && live;
-        // at[i]: the slope at p_i; with normalized gates apart, what is chosen: how often, and
-        // the sum of its gates' gradients
-        float at[P], times[P], wants[P];
-        float sum = 0.0f;
+        const bool live = in && a.ids[r * a.k] >= 0;
+        float top = z[0];
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            at[i] = slope[i];
-            times[i] = wants[i] = 0.0f;
-        }
-        if (a.dgates && live) {
-            const float* const dg = a.dgates + r * a.k;
-            for (int j = 0; j < a.k; ++j) {
-                const int64_t rel = ids[j] - first;
-                const float g = dg[j];
+        for (int i = 1; i < P; ++i) top = larger(top, z[i]);
+        top = group_max<LOG>(top);
+        const bool any = live && top != -INFINITY;
+        softmax<LOG, P>(z, top, p);
+        // wants: the sum of the gates' gradients, of those chosen `times` times
+        float times[P], wants[P];
 #pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    wants[i] += rel == i ? g : 0.0f;
-                    times[i] += rel == i ? 1.0f : 0.0f;
+        for (int i = 0; i < P; ++i) times[i] = wants[i] = 0.0f;
+        if (a.dgates) {
+            int* const number = chosen[wave] + group * WIDE;
+            float* const want = wanted[wave] + group * WIDE;
+            wave_sync();
+#pragma unroll
+            for (int i = 0; i < P; i += 4) *(AR_LDS i32x4*)((AR_LDS int*)number + first + i) = i32x4{0, 0, 0, 0};
+            wave_sync();
+            bool twice = false;
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s)
+                if (id[s] >= 0 && id[s] < a.E) {
+                    number[id[s]] = s * LANES + sub + 1;
+                    want[id[s]] = g[s];
+                }
+            wave_sync();
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s)
+                if (id[s] >= 0 && id[s] < a.E) twice |= number[id[s]] != s * LANES + sub + 1;
+            if (!__builtin_amdgcn_ballot_w64(twice)) {
+#pragma unroll
+                for (int i = 0; i < P; i += 4) {
+                    const i32x4 m = *(AR_LDS i32x4*)((AR_LDS int*)number + first + i);
+                    const f32x4 w = *(AR_LDS f32x4*)((AR_LDS float*)want + first + i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        times[i + e] = m[e] ? 1.0f : 0.0f;
+                        wants[i + e] = m[e] ? w[e] : 0.0f;
+                    }
+                }
+            } else if (in) {  // an expert more than once in a row: every choice at every lane
+                for (int j = 0; j < a.k; ++j) {
+                    const int64_t rel = a.ids[r * a.k + j] - first;
+                    const float w = a.dgates[r * a.k + j];
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        wants[i] += rel == i && first + i < a.E ? w : 0.0f;
+                        times[i] += rel == i && first + i < a.E ? 1.0f : 0.0f;
+                    }
                 }
             }
-            if (!a.normalize) {
-#pragma unroll
-                for (int i = 0; i < P; ++i) at[i] += wants[i];
-            }
         }
+        float d[P], sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < P; ++i) sum += p[i] * at[i];
+        for (int i = 0; i < P; ++i) {
+            d[i] = slope[i] + (a.normalize ? 0.0f : wants[i]);
+            sum += p[i] * d[i];
+        }
         sum = group_sum<LOG>(sum);
-        float d[P];
 #pragma unroll
-        for (int i = 0; i < P; ++i) d[i] = p[i] * (at[i] - sum);
+        for (int i = 0; i < P; ++i) d[i] = p[i] * (d[i] - sum);
         if (a.normalize && a.dgates) {
             float total = 0.0f, dot = 0.0f;
 #pragma unroll
@@ -345,13 +439,13 @@ __global__ __launch_bounds__(kBlock) void balance_kernel(const T* logits, T* gra
                 total += times[i] != 0.0f ? p[i] * times[i] : 0.0f;
                 dot += times[i] != 0.0f ? p[i] * wants[i] : 0.0f;
             }
-            total = group_sum<LOG>(total);
-            dot = group_sum<LOG>(dot) / total;
+            const float share = 1.0f / group_sum<LOG>(total);
+            dot = group_sum<LOG>(dot) * share;
 #pragma unroll
             for (int i = 0; i < P; ++i)
-                d[i] += times[i] != 0.0f ? p[i] / total * (wants[i] - times[i] * dot) : 0.0f;
+                d[i] += times[i] != 0.0f ? p[i] * share * (wants[i] - times[i] * dot) : 0.0f;
         }
-        if (r >= a.T) continue;
+        if (!in) continue;
         T* const to = grad + r * a.grad_stride;
 #pragma unroll
         for (int i = 0; i < P; ++i) d[i] = any ? d[i] : 0.0f;
@@ -383,10 +477,10 @@ int group_log(int64_t E) {
     return log;
 }
 
-// Blocks of a routing: as many as the rows fill, each with `4 passes` at least.
+// Blocks of a routing, as many as the rows fill.
 int64_t parts_of(int64_t T, int64_t E) {
-    const int64_t rows = (kBlock / 64) * (64 >> group_log(E));
-    return std::max<int64_t>(1, std::min<int64_t>(kMaxParts, ceil_div(T, 4 * rows)));
+    const int64_t rows = (kRouteBlock / 64) * (64 >> group_log(E));
+    return std::max<int64_t>(1, std::min<int64_t>(kMaxParts, ceil_div(T, rows)));
 }
 int64_t part_bytes(int64_t T, int64_t E) {
     const int64_t parts = parts_of(T, E);
@@ -450,7 +544,7 @@ AR_EXPORT ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, con
         using U = decltype(zero);
         by_width(int(E), [&](auto log, auto p) {
             hipLaunchKernelGGL((route_kernel<U, decltype(log)::value, decltype(p)::value>),
-                               dim3(unsigned(parts)), dim3(kBlock), 0, st,
+                               dim3(unsigned(parts)), dim3(kRouteBlock), 0, st,
                                static_cast<const U*>(logits), a);
         });
         if (parts > 1)
@@ -493,9 +587,10 @@ AR_EXPORT ar_status ar_balance(int32_t dtype, int64_t T, int64_t E, int64_t k, c
     auto go = [&](auto zero) {
         using U = decltype(zero);
         by_width(int(E), [&](auto log, auto p) {
-            const int64_t blocks = ceil_div(T, (kBlock / 64) * (64 >> decltype(log)::value));
+            const int64_t blocks = ceil_div(T, (kBalanceBlock / 64) * (64 >> decltype(log)::value));
             hipLaunchKernelGGL((balance_kernel<U, decltype(log)::value, decltype(p)::value>),
-                               dim3(unsigned(std::min<int64_t>(blocks, 2048)) + 1), dim3(kBlock), 0, st,
+                               dim3(unsigned(std::min<int64_t>(blocks, 2048)) + 1), dim3(kBalanceBlock),
+                               0, st,
                                static_cast<const U*>(logits), static_cast<U*>(grad), a);
         });
         return launch_status("balance loss");

@@ -80,6 +80,11 @@ def _ids(name, ids, like):
         raise ValueError("%s: an int64 tensor on the operands' device expected" % name)
 
 
+# The device's current stream as a handle, without the object around it, whose making
+# takes longer than a short call's launch (4 us of 13).
+_current_stream = torch._C._cuda_getCurrentRawStream
+
+
 class _on:
     """The stream a call runs on, as a handle: its allocations are made there,
     and the tensors it is given are marked as used there, those in ``written`` as
@@ -101,7 +106,7 @@ class _on:
             if self.like.device.index != torch.cuda.current_device():
                 self.entered = (torch.cuda.device(self.like.device),)
                 self.entered[0].__enter__()
-            return torch.cuda.current_stream().cuda_stream
+            return _current_stream(self.like.device.index)
         if self.stream.device != self.like.device:
             raise ValueError("stream: one of the operands' device expected")
         self.entered = (torch.cuda.device(self.like.device), torch.cuda.stream(self.stream))
@@ -187,10 +192,12 @@ def position_bias(table, queries, keys, max_distance=128, offset=0, causal=False
     _whole("max_distance", max_distance, 1, _MOST)
     _whole("offset", offset, -1 << 62, 1 << 62)
     with _on(table, stream, (table, out), (out,)) as s:
-        res = out
         if out is None:
             res = torch.empty(H, queries, keys, dtype=table.dtype, device=table.device)
-        sh, sr = _strides("out", res, (H, queries, keys), table)
+            sh, sr = queries * keys, keys
+        else:
+            res = out
+            sh, sr = _strides("out", out, (H, queries, keys), table)
         arplan.ar_position_bias(_DT[table.dtype], buckets, max_distance, causal, H, queries, keys,
                                 offset, table, st, res, sh, sr, s)
     return res
@@ -325,10 +332,12 @@ def checkpoint_store(x, out=None, stream=None):
     with _on(x, stream, (x, out), (out,)) as s:
         res = out
         if out is None:
-            res = torch.empty(M, arplan.ar_checkpoint_row(N), dtype=torch.uint8, device=x.device)
-        sk = _kept("out", res, M, N)
-        if res.device != x.device:
-            raise ValueError("out: on x's device expected")
+            sk = arplan.ar_checkpoint_row(N)
+            res = torch.empty(M, sk, dtype=torch.uint8, device=x.device)
+        else:
+            sk = _kept("out", out, M, N)
+            if out.device != x.device:
+                raise ValueError("out: on x's device expected")
         arplan.ar_checkpoint_store(_DT[x.dtype], M, N, x, sx, res, sk, s)
     return res
 
@@ -341,10 +350,12 @@ def checkpoint_load(kept, width, dtype=None, out=None, stream=None):
     if out is None and dtype not in _DT:
         raise ValueError("dtype: float32 or bfloat16 expected")
     with _on(kept, stream, (kept, out), (out,)) as s:
-        res = torch.empty(M, width, dtype=dtype, device=kept.device) if out is None else out
-        sx = _matrix("out", res, (M, width))
-        if res.device != kept.device or (dtype is not None and res.dtype != dtype):
-            raise ValueError("out: of dtype and on kept's device expected")
+        if out is None:
+            res, sx = torch.empty(M, width, dtype=dtype, device=kept.device), max(width, 1)
+        else:
+            res, sx = out, _matrix("out", out, (M, width))
+            if out.device != kept.device or (dtype is not None and out.dtype != dtype):
+                raise ValueError("out: of dtype and on kept's device expected")
         arplan.ar_checkpoint_load(_DT[res.dtype], M, width, kept, sk, res, sx, s)
     return res
 
@@ -383,10 +394,12 @@ def route(logits, k, live=None, normalize=False, counts=None, mass=None, workspa
         w, n, keep = _space(workspace, arplan.ar_route_workspace(T, E, k), logits)
         if counts is None:
             counts = torch.empty(E + 1, dtype=torch.int32, device=dev)
+        else:
+            _vector("counts", counts, E + 1, torch.int32, logits)
         if mass is None:
             mass = torch.empty(E, dtype=torch.float32, device=dev)
-        _vector("counts", counts, E + 1, torch.int32, logits)
-        _vector("mass", mass, E, torch.float32, logits)
+        else:
+            _vector("mass", mass, E, torch.float32, logits)
         ids = torch.empty(T, k, dtype=torch.int64, device=dev)
         gates = torch.empty(T, k, dtype=torch.float32, device=dev)
         arplan.ar_route(_DT[logits.dtype], T, E, k, logits, sl, live, normalize, ids, gates, counts,
