@@ -1,15 +1,13 @@
 // Attention's relative position bias by buckets of distance, and its table's gradient.
 //
 // The bias depends on j - i alone: along a diagonal of a head's Q x K matrix it is one
-// number, and all of a diagonal's gradients go to one bucket.  So a lane owns a vector
-// of adjacent diagonals and walks down the rows: the bias is looked up once and stored
-// row after row, one element further on in each; the gradients are added in registers,
-// and only the diagonals' sums are sorted into buckets.  An element costs its way
-// through memory and, in the gradient, one addition.  Rows start at any element, and so
-// do the vectors.
+// number, and all of a diagonal's gradients go to one bucket.  So buckets are looked up
+// a diagonal, not an element: a patch of the bias is stored from its diagonals' values
+// in LDS, and a patch of gradients is first summed along its diagonals, in registers, and
+// those sums are sorted into buckets.  An element costs its way through memory and, in
+// the gradient, one addition.
 //
-// Diagonals are counted g = j - i + Q - 1 >= 0; the distance is n = c - g with
-// c = offset + Q - 1.
+// The distance on diagonal d = j - i is n = offset - d.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -22,6 +20,12 @@ namespace {
 
 constexpr int kBlock = 256, kWaves = kBlock / 64;
 
+// Orders a wavefront's accesses to LDS of which one lane's is another's.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // The distances at which the buckets of a side begin: bucket b of `side` from at[b] on.
 struct Borders {
     int32_t side;
@@ -30,66 +34,122 @@ struct Borders {
 };
 
 struct BiasShape {
-    int64_t H, Q, K, c;
-    int64_t rows, row_tiles, chunks;  // rows of a tile; chunks of diagonals a tile has
+    int64_t H, Q, K, offset;
+    int64_t rows, row_tiles, chunks;  // rows of a tile, and chunks of columns
 };
 
-// The bucket of distance n; behind the query in buckets of their own, or (causal) none.
-__device__ __forceinline__ int bucket_of(const Borders& s, int64_t n) {
-    if (s.causal && n < 0) return -1;
-    const int64_t d = n < 0 ? -n : n;
-    int lo = 0, hi = s.side;  // at[lo] <= d < at[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s.at[mid] <= d) lo = mid;
-        else hi = mid;
-    }
-    return n < 0 ? s.side + lo : lo;
-}
-
-// The place of a block: head, rows [i0, i1) and its first diagonal.
+// The place of a block: head, rows [i0, i1) and its first column.
 struct Patch {
-    int64_t h, i0, i1, g0;
+    int64_t h, i0, i1, j0;
 };
+// A quotient, in 32 bits where they hold both.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? int64_t(uint32_t(a) / uint32_t(b)) : a / b;
+}
 __device__ __forceinline__ Patch patch_of(const BiasShape& s, int64_t n, int width) {
-    const int64_t chunk = n % s.chunks, tile = n / s.chunks % s.row_tiles;
+    const int64_t over = quotient(n, s.chunks), chunk = n - over * s.chunks;
     Patch p;
-    p.h = n / s.chunks / s.row_tiles;
+    p.h = quotient(over, s.row_tiles);
+    const int64_t tile = over - p.h * s.row_tiles;
     p.i0 = tile * s.rows;
     p.i1 = p.i0 + s.rows < s.Q ? p.i0 + s.rows : s.Q;
-    p.g0 = s.Q - p.i1 + chunk * width;
+    p.j0 = chunk * width;
     return p;
 }
 
-// Bound by memory: the matrix is written once.
+// The bucket of distance n from the borders `at`; behind the query in buckets of their
+// own, or (causal) none.
+__device__ __forceinline__ int bucket_of(const int32_t* at, int side, bool causal, int64_t n) {
+    if (causal && n < 0) return -1;
+    const int64_t d = n < 0 ? -n : n;
+    int lo = 0, hi = side;  // at[lo] <= d < at[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (at[mid] <= d) lo = mid;
+        else hi = mid;
+    }
+    return n < 0 ? side + lo : lo;
+}
+
+// The bias: a wavefront stores kBiasRows rows of 64 vectors, the block's wavefronts lie
+// side by side as far as the rows are long.
+constexpr int kBiasRows = 16;
+// (Few rows: a block a chunk of 64 vectors, for there the lookups are what takes time.)
+int bias_side(int64_t Q, int64_t K, int width) {
+    return Q < kBiasRows ? 1 : K > 2 * width ? 4 : K > width ? 2 : 1;
+}
+
+// A lane's vectors of VEC rows from the 2 VEC diagonals' values that hold them all: row
+// r's begins VEC - r further on.
+__device__ __forceinline__ void vectors_of(const u32x4 a, const u32x4 b, float, u32x4* v) {
+    v[0] = b;
+    v[1] = u32x4{a[3], b[0], b[1], b[2]};
+    v[2] = u32x4{a[2], a[3], b[0], b[1]};
+    v[3] = u32x4{a[1], a[2], a[3], b[0]};
+}
+__device__ __forceinline__ void vectors_of(const u32x4 a, const u32x4 b, uint16_t, u32x4* v) {
+    const uint32_t even[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    uint32_t odd[7];
+#pragma unroll
+    for (int k = 0; k < 7; ++k) odd[k] = __builtin_amdgcn_alignbyte(even[k + 1], even[k], 2);
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int x = 8 - r + 2 * e;
+            v[r][e] = x % 2 ? odd[x / 2] : even[x / 2];
+        }
+}
+
+// The values of a patch's diagonals lie in LDS; a lane reads those of VEC rows at once,
+// and their vectors are parts of them.  Bound by memory: the matrix is written once.
 template <class T>
 __global__ __launch_bounds__(kBlock) void bias_kernel(BiasShape s, Borders borders, const T* table,
-                                                      int64_t table_stride, T* out, int64_t head_stride,
-                                                      int64_t row_stride, int64_t patches) {
+                                                      int64_t table_stride, int buckets, T* out,
+                                                      int64_t head_stride, int64_t row_stride,
+                                                      int64_t patches, int side) {
     constexpr int VEC = Num<T>::VEC, WIDTH = 64 * VEC;
-    __shared__ __attribute__((aligned(16))) T value[WIDTH];
+    __shared__ __attribute__((aligned(16))) T value[kWaves * WIDTH + kWaves * kBiasRows];
+    __shared__ int32_t at[AR_POSITION_MAX_BUCKETS];
+    __shared__ T column[AR_POSITION_MAX_BUCKETS];
     const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6);
+    const int across = wave % side, down = wave / side;
     for (int64_t n = blockIdx.x; n < patches; n += gridDim.x) {
-        const Patch p = patch_of(s, n, WIDTH);
-        for (int x = threadIdx.x; x < WIDTH; x += kBlock) {
-            const int b = bucket_of(borders, s.c - (p.g0 + x));
-            value[x] = b < 0 ? Num<T>::down(-INFINITY) : table[b * table_stride + p.h];
+        const Patch p = patch_of(s, n, side * WIDTH);
+        const int rows = int(p.i1 - p.i0);
+        const int ceiling = (rows + VEC - 1) / VEC * VEC;
+        if (int(threadIdx.x) < buckets) {
+            at[threadIdx.x] = borders.at[threadIdx.x];
+            column[threadIdx.x] = table[threadIdx.x * table_stride + p.h];
         }
         __syncthreads();
-        const u32x4 v = *(const AR_LDS u32x4*)((AR_LDS T*)value + lane * VEC);
-        const int64_t per = (s.rows + kWaves - 1) / kWaves, i0 = p.i0 + wave * per;
-        const int64_t i1 = i0 + per < p.i1 ? i0 + per : p.i1;
-        int64_t j = p.g0 + lane * VEC + i0 - (s.Q - 1);
-        T* to = out + p.h * head_stride + i0 * row_stride + j;
-        for (int64_t i = i0; i < i1; ++i, ++j, to += row_stride + 1) {
-            if (j >= 0 && j + VEC <= s.K) {
-                store_vec(to, v);
-            } else if (j > -VEC && j < s.K) {
-                float f[VEC];
-                Num<T>::unpack(v, f);
+        // diagonal j0 - i0 - ceiling + x at x
+        for (int x = threadIdx.x; x < side * WIDTH + ceiling; x += kBlock) {
+            const int b = bucket_of(at, borders.side, borders.causal, s.offset - (p.j0 - p.i0 - ceiling + x));
+            value[x] = b < 0 ? Num<T>::down(-INFINITY) : column[b];
+        }
+        __syncthreads();
+        const int x = (across * 64 + lane) * VEC;
+        const int64_t j = p.j0 + x;
+        const int end = (down + 1) * kBiasRows < rows ? (down + 1) * kBiasRows : rows;
+        for (int i = down * kBiasRows; i < end; i += VEC) {
+            const AR_LDS u32x4* const from = (const AR_LDS u32x4*)((const AR_LDS T*)value + x + ceiling - i - VEC);
+            u32x4 v[VEC];
+            const u32x4 a = from[0], b = from[1];
+            vectors_of(a, b, T(0), v);
+            T* const to = out + p.h * head_stride + (p.i0 + i) * row_stride + j;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (j + e >= 0 && j + e < s.K) ((AR_GLOBAL T*)to)[e] = Num<T>::down(f[e]);
+            for (int r = 0; r < VEC; ++r) {
+                if (i + r >= end) break;
+                if (j + VEC <= s.K) {
+                    store_vec(to + r * row_stride, v[r]);
+                } else if (j < s.K) {
+                    float f[VEC];
+                    Num<T>::unpack(v[r], f);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if (j + e < s.K) ((AR_GLOBAL T*)to)[r * row_stride + e] = Num<T>::down(f[e]);
+                }
             }
         }
         __syncthreads();
@@ -101,107 +161,232 @@ struct GradArgs {
     int64_t span;     // elements from the first to the last one, and itself
     int64_t batches;  // of one block
     int64_t splits;
+    int32_t rows;  // of a wavefront
+    int32_t across, down;  // a block's wavefronts side by side, and one below the other; of
+                           // less than four the others take other batches
 };
 
-// The sums of a wavefront's diagonals over rows [i0, i1): EDGE where some of its vectors
-// pass a row's ends.  Such a vector is read whole and what lies outside the row is
-// left out, where it lies between the tensor's first and last element.
-template <class T, bool EDGE>
-__device__ __forceinline__ void add_rows(const T* first, const T* end, const T* from, int64_t step,
-                                         int64_t rows, int64_t j, int64_t K, float* sum) {
-    constexpr int VEC = Num<T>::VEC, DEEP = 8;
-    auto add = [&](const u32x4 w, int64_t at) {
-        float f[VEC];
-        Num<T>::unpack(w, f);
+// A lane's sums of its vector's diagonals, as it goes down the rows of a patch, VEC
+// rows a step.  With b the diagonal of the vector's first element in a step's first
+// row, `main` holds diagonals b .. b + VEC - 1 and `low` the VEC - 1 before them.  In the
+// next step b is VEC less: `low` becomes main, and main the next lane's main, whose
+// vector has now come to those diagonals; the last lane's leaves the wavefront.
+template <int VEC>
+struct Diagonals {
+    float main[VEC], low[VEC];  // (low[0] is not used)
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            sum[e] += !EDGE || (at + e >= 0 && at + e < K) ? f[e] : 0.0f;
-    };
-    auto load = [&](const T* p, int64_t at) {
-        if constexpr (!EDGE) return load_vec(p);
-        if (at <= -VEC || at >= K) return u32x4{0, 0, 0, 0};
-        if (p >= first && p + VEC <= end) return load_vec(p);
-        float f[VEC];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            f[e] = at + e >= 0 && at + e < K ? Num<T>::up(((const AR_GLOBAL T*)p)[e]) : 0.0f;
-        return Num<T>::pack(f);
-    };
-    int64_t i = 0;
-    for (; i + DEEP <= rows; i += DEEP, from += DEEP * step) {
-        u32x4 w[DEEP];
-#pragma unroll
-        for (int d = 0; d < DEEP; ++d) w[d] = load(from + d * step, j + i + d);
-#pragma unroll
-        for (int d = 0; d < DEEP; ++d) add(w[d], j + i + d);
+        for (int e = 0; e < VEC; ++e) main[e] = low[e] = 0.0f;
     }
-    for (; i < rows; ++i, from += step) add(load(from, j + i), j + i);
+    __device__ __forceinline__ void add(int row, const float* f) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            if (e >= row) main[e - row] += f[e];
+            else low[e - row + VEC] += f[e];
+        }
+    }
+    __device__ __forceinline__ void step() {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            // (lane l from lane l - 1, the first from none)
+            const float from = __uint_as_float(uint32_t(__builtin_amdgcn_mov_dpp(
+                int(__float_as_uint(main[e])), 0x138, 0xF, 0xF, true)));
+            main[e] = low[e] + from;
+            low[e] = 0.0f;
+        }
+    }
+    __device__ __forceinline__ void put(AR_LDS float* to, bool first) const {
+        typedef float f4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int e = 0; e < VEC; e += 4) {
+            f4 v = {main[e], main[e + 1], main[e + 2], main[e + 3]};
+            if (!first) v += *(const AR_LDS f4*)(to + e);
+            *(AR_LDS f4*)(to + e) = v;
+        }
+    }
+};
+
+constexpr int kGradRows = 64;  // of a wavefront at most
+
+// A wavefront's sums by diagonal of a patch, `rows` rows (a multiple of 2 VEC) from i0,
+// of which those below i1 are there, and 64 VEC columns from j0 on, to LDS, or added to
+// what is there: diagonal j0 - i0 - rows + x at x.  EDGE: the patch is not whole, or not
+// all of it seen; a vector that passes a row's end is read whole and what lies behind the
+// row left out, where that lies before the tensor's last element.
+template <class T, bool EDGE>
+__device__ __forceinline__ void sum_patch(const T* from, const T* end, int64_t stride, int rows,
+                                          int64_t i0, int64_t i1, int64_t j0, int64_t K, int64_t seen,
+                                          bool first, AR_LDS float* sums) {
+    constexpr int VEC = Num<T>::VEC;
+    const int lane = threadIdx.x & 63, steps = rows / VEC;
+    // a lane's columns that are there, and the rows that see any of them and can be read whole
+    int n = VEC, begin = 0, there = rows, safe = rows;
+    if constexpr (EDGE) {
+        const int64_t left = K - j0 - lane * VEC, late = j0 + lane * VEC - seen - i0;
+        n = int(left < 0 ? 0 : left < VEC ? left : VEC);
+        begin = n == 0 ? rows : int(late < 0 ? 0 : late < rows ? late : rows);
+        if (i1 - i0 < rows) there = int(i1 - i0);
+        safe = there;
+        // (vectors reach that far into a row)
+        const int64_t reach = K - j0 < 64 * VEC ? (K - j0 + VEC - 1) / VEC * VEC : 64 * VEC;
+        while (safe > 0 && from + (safe - 1) * stride + reach > end) --safe;
+    }
+    Diagonals<VEC> d;
+    d.clear();
+    const T* p = from;
+    // The steps' rows one after the other, read once and past the caches: 537 MB 80 us, as
+    // ordinary loads 88.
+    auto load = [&](int step, u32x4* v) {
+        // (one address after the other, not each row's kept in registers of its own)
+        int64_t next = stride;
+        asm("" : "+s"(next));
+#pragma unroll
+        for (int r = 0; r < VEC; ++r, p += next) {
+            const int i = step * VEC + r;
+            if (EDGE) v[r] = u32x4{0, 0, 0, 0};
+            if (!EDGE || (i >= begin && i < safe))
+                v[r] = __builtin_nontemporal_load((const typename Num<T>::V*)(p + lane * VEC));
+        }
+    };
+    auto add = [&](int step, const u32x4* v) {
+#pragma unroll
+        for (int r = 0; r < VEC; ++r) {
+            float f[VEC];
+            Num<T>::unpack(v[r], f);
+            if (EDGE) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f[e] = e < n ? f[e] : 0.0f;
+            }
+            d.add(r, f);
+        }
+        if (lane == 63) d.put(sums + (63 + steps - step) * VEC, first);
+        d.step();
+    };
+    if constexpr (EDGE) {  // (with another step's vectors there are registers too few)
+        u32x4 w[VEC];
+#pragma unroll 1
+        for (int step = 0; step < steps; ++step) {
+            load(step, w);
+            add(step, w);
+        }
+    } else {
+        u32x4 v[VEC], w[VEC];
+        int step = 0;
+        load(0, v);
+#pragma unroll 1
+        for (; step + 2 < steps; step += 2) {
+            load(step + 1, w);
+            add(step, v);
+            load(step + 2, v);
+            add(step + 1, w);
+        }
+        load(step + 1, w);
+        add(step, v);
+        add(step + 1, w);
+    }
+    d.put(sums + lane * VEC, first);
+    if constexpr (EDGE) {  // the tensor's last rows, an element at a time
+#pragma unroll 1
+        for (int i = safe; i < there; ++i) {
+            wave_sync();
+#pragma unroll 1
+            for (int e = 0; e < n && i >= begin; ++e)
+                sums[lane * VEC + e + rows - i] += Num<T>::up(((const AR_GLOBAL T*)(from + i * stride))[lane * VEC + e]);
+        }
+    }
 }
 
 // A block's sums by bucket, to its slot of `part`, or straight to the table where a
-// head has one slot.  Bound by memory: the scores' gradients pass once.
+// head has one slot.  Bound by memory: the gradients pass once.
 template <class T>
-__global__ __launch_bounds__(kBlock) void bias_grad_kernel(BiasShape s, Borders borders, GradArgs a,
+__global__ __launch_bounds__(kBlock, 4) void bias_grad_kernel(BiasShape s, Borders borders, GradArgs a,
                                                            const T* d, int32_t buckets, float* part,
                                                            T* dtable, int64_t table_stride,
                                                            int32_t accumulate) {
-    constexpr int VEC = Num<T>::VEC, WIDTH = 64 * VEC;
-    __shared__ __attribute__((aligned(16))) float sums[kWaves][WIDTH];
+    constexpr int VEC = Num<T>::VEC, WIDTH = 64 * VEC, LENGTH = WIDTH + kGradRows;
+    __shared__ __attribute__((aligned(16))) float sums[kWaves][LENGTH];
+    __shared__ float total[kWaves * (WIDTH + kGradRows)];
     const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6);
     const int64_t per_head = s.row_tiles * s.chunks, patches = s.H * per_head;
+    const int64_t seen = borders.causal ? s.offset : INT64_MAX / 2;
+    const int rows = a.rows, tile = a.down * rows, width = a.across * WIDTH;
+    const int fold = a.across * a.down;     // wavefronts with patches of their own
     for (int64_t n = blockIdx.x; n < patches * a.splits; n += gridDim.x) {
-        const int64_t split = n / patches, in = n % patches;
-        const Patch p = patch_of(s, in, WIDTH);
-        // a tile's rows are shared out to the wavefronts, or, of few rows, the batches
-        const bool by_rows = s.rows >= kWaves;
-        const int64_t per = by_rows ? (s.rows + kWaves - 1) / kWaves : s.rows;
-        const int64_t i0 = p.i0 + (by_rows ? wave * per : 0);
-        const int64_t i1 = i0 + per < p.i1 ? i0 + per : p.i1;
-        const int64_t b0 = split * a.batches, b1 = b0 + a.batches < a.B ? b0 + a.batches : a.B;
-        const int64_t g = p.g0 + lane * VEC, j = g + i0 - (s.Q - 1);
-        float sum[VEC] = {};
-        const bool seen = !borders.causal || p.g0 <= s.c;
-        if (seen && i0 < i1) {
-            const bool whole = p.g0 + i0 - (s.Q - 1) >= 0 && p.g0 + WIDTH - 1 + i1 - 1 - (s.Q - 1) < s.K;
-            for (int64_t b = b0 + (by_rows ? 0 : wave); b < b1; b += by_rows ? 1 : kWaves) {
-                const T* const from = d + b * a.batch_stride + p.h * a.head_stride + i0 * a.row_stride + j;
-                if (whole) add_rows<T, false>(d, d + a.span, from, a.row_stride + 1, i1 - i0, j, s.K, sum);
-                else add_rows<T, true>(d, d + a.span, from, a.row_stride + 1, i1 - i0, j, s.K, sum);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            sums[wave][lane * VEC + e] = borders.causal && g + e > s.c ? 0.0f : sum[e];
-        __syncthreads();
-        for (int b = wave; b < buckets; b += kWaves) {
-            // the bucket's distances [near, far) are diagonals (c - far, c - near], or,
-            // behind the query, [c + near, c + far)
+        const int64_t split = quotient(n, patches), in = n - split * patches;
+        const Patch p = patch_of(s, in, width);
+        const int64_t i0 = p.i0 + wave % fold / a.across * rows, j0 = p.j0 + wave % a.across * WIDTH;
+        const int64_t i1 = i0 + rows < p.i1 ? i0 + rows : p.i1;
+        const int64_t b0 = split * a.batches + wave / fold;
+        const int64_t b1 = (split + 1) * a.batches < a.B ? (split + 1) * a.batches : a.B;
+        AR_LDS float* const mine = (AR_LDS float*)sums[wave];
+        // A lane looks at a bucket, wavefronts in turn.  Its distances [near, far) are
+        // diagonals (offset - far, offset - near], or, behind the query, [offset + near,
+        // offset + far).
+        const int b = lane * kWaves + wave;
+        int from = 0, to = 0;
+        if (b < buckets) {
             const bool behind = b >= borders.side;
             const int m = behind ? b - borders.side : b;
-            const int64_t near = borders.at[m];
-            int64_t lo = behind ? s.c + (near ? near : 1) : 0, hi = behind ? INT64_MAX : s.c - near + 1;
+            const int64_t near = borders.at[m], d0 = p.j0 - p.i0 - tile;
+            int64_t lo = behind ? s.offset + (near ? near : 1) : INT64_MIN / 2;
+            int64_t hi = behind ? INT64_MAX / 2 : s.offset - near + 1;
             if (m + 1 < borders.side) {
-                const int64_t far = borders.at[m + 1];
-                if (behind) hi = s.c + far;
-                else lo = s.c - far + 1;
-            } else if (!behind) {
-                lo = INT64_MIN;
+                if (behind) hi = s.offset + borders.at[m + 1];
+                else lo = s.offset - borders.at[m + 1] + 1;
             }
-            lo = lo > p.g0 ? lo - p.g0 : 0;
-            hi = hi > p.g0 ? (hi - p.g0 < WIDTH ? hi - p.g0 : WIDTH) : 0;
+            lo = lo > d0 ? lo - d0 : 0;
+            hi = hi - d0 < width + tile ? hi - d0 : width + tile;
+            if (lo < hi) {
+                from = int(lo);
+                to = int(hi);
+            }
+        }
+        if (i0 < i1 && j0 < s.K && b0 < b1 && j0 - (i1 - 1) <= seen) {
+            const bool whole = j0 + WIDTH <= s.K && i0 + rows <= i1 && j0 + WIDTH - 1 - i0 <= seen;
+            for (int64_t k = b0; k < b1; k += kWaves / fold) {
+                const T* const at = d + k * a.batch_stride + p.h * a.head_stride + i0 * a.row_stride + j0;
+                if (whole)
+                    sum_patch<T, false>(at, d + a.span, a.row_stride, rows, i0, i1, j0, s.K, seen, k == b0, mine);
+                else
+                    sum_patch<T, true>(at, d + a.span, a.row_stride, rows, i0, i1, j0, s.K, seen, k == b0, mine);
+            }
+        } else {
+            for (int x = lane; x < WIDTH + rows; x += 64) mine[x] = 0.0f;
+        }
+        __syncthreads();
+        // the wavefronts', diagonal j0 - i0 - tile + x at x
+        for (int x = threadIdx.x; x < width + tile; x += kBlock) {
             float t = 0.0f;
-            for (int x = int(lo < WIDTH ? lo : WIDTH) + lane; x < int(hi); x += 64)
-                t += (sums[0][x] + sums[1][x]) + (sums[2][x] + sums[3][x]);
-            t = wave_sum(t);
-            if (lane == 0) {
-                if (part) {
-                    const int64_t slots = per_head * a.splits;
-                    part[(p.h * buckets + b) * slots + split * per_head + in % per_head] = t;
-                } else {
-                    T* const to = dtable + b * table_stride + p.h;
-                    *to = Num<T>::down(accumulate ? t + Num<T>::up(*to) : t);
-                }
+#pragma unroll
+            for (int v = 0; v < kWaves; ++v) {
+                const int y = x - (v % a.across * WIDTH + tile - (v % fold / a.across + 1) * rows);
+                if (y >= 0 && y < WIDTH + rows) t += sums[v][y];
             }
+            total[x] = t;
+        }
+        __syncthreads();
+        auto result = [&](int bucket, float t) {
+            if (part) {
+                const int64_t slots = per_head * a.splits;
+                part[(p.h * buckets + bucket) * slots + split * per_head + in - p.h * per_head] = t;
+            } else {
+                T* const at = dtable + bucket * table_stride + p.h;
+                *at = Num<T>::down(accumulate ? t + Num<T>::up(*at) : t);
+            }
+        };
+        // few diagonals by the lane alone, many by the wavefront
+        constexpr int FEW = 16;
+        float few = 0.0f;
+        for (int x = 0; x < FEW && __builtin_amdgcn_ballot_w64(to - from <= FEW && from + x < to); ++x)
+            few += to - from <= FEW && from + x < to ? total[from + x] : 0.0f;
+        if (b < buckets && to - from <= FEW) result(b, few);
+        for (uint64_t left = __builtin_amdgcn_ballot_w64(to - from > FEW); left; left &= left - 1) {
+            const int l = __builtin_ctzll(left);
+            const int end = __builtin_amdgcn_readlane(to, l);
+            float t = 0.0f;
+            for (int x = __builtin_amdgcn_readlane(from, l) + lane; x < end; x += 64) t += total[x];
+            t = wave_sum(t);
+            if (lane == 0) result(l * kWaves + wave, t);
         }
         __syncthreads();
     }
@@ -282,22 +467,28 @@ Borders borders_of(int32_t buckets, int32_t most, bool causal) {
 template <class T> constexpr int width_of() { return 64 * Num<T>::VEC; }
 
 BiasShape shape_of(int64_t H, int64_t Q, int64_t K, int64_t offset, int64_t rows, int width) {
-    BiasShape s{H, Q, K, offset + Q - 1, std::min(rows, Q), 0, 0};
-    s.row_tiles = ceil_div(Q, s.rows);
-    s.chunks = ceil_div(K + s.rows - 1, width);
+    BiasShape s{H, Q, K, offset, rows, 0, 0};
+    s.row_tiles = ceil_div(Q, rows);
+    s.chunks = ceil_div(K, width);
     return s;
 }
 
-constexpr int64_t kGradRows = 128, kBiasRows = 64;
-
-// How a gradient's batches are shared out: enough blocks for the card, and few of
-// them a block, whose sums run on.
-GradArgs split_of(const BiasShape& s, int64_t B) {
+// How a gradient is shared out: as many rows a wavefront as leave four wavefronts for each
+// of the card's 1024 SIMDs, but two steps; a block's side by side along long rows, below
+// each other in many, or else in other batches; and few batches a block, whose sums run on.
+GradArgs split_of(int64_t B, int64_t H, int64_t Q, int64_t K, int width) {
     GradArgs a{};
     a.B = B;
-    const int64_t patches = s.H * s.row_tiles * s.chunks;
-    const int64_t want = std::max(ceil_div(2048, patches), ceil_div(B, 8));
-    a.batches = ceil_div(B, std::max<int64_t>(1, std::min(B, want)));
+    const int64_t least = width / 32, chunks = ceil_div(K, width);
+    int64_t rows = kGradRows;
+    while (rows > least && (rows >= 2 * Q || B * H * chunks * ceil_div(Q, rows) < 4096)) rows /= 2;
+    a.rows = int32_t(rows);
+    a.across = chunks >= 3 ? 4 : 1;
+    a.down = a.across == 1 && Q > rows ? 4 : 1;
+    const int64_t alone = kWaves / (a.across * a.down);     // batches at a time
+    const int64_t blocks = H * ceil_div(chunks, a.across) * ceil_div(Q, rows * a.down);
+    const int64_t splits = std::max(ceil_div(2048, blocks), ceil_div(B, 8));
+    a.batches = ceil_div(B, std::max<int64_t>(1, std::min(ceil_div(B, alone), splits)));
     a.splits = ceil_div(B, a.batches);
     return a;
 }
@@ -372,12 +563,13 @@ AR_EXPORT ar_status ar_position_bias(int32_t dtype, int32_t buckets, int32_t max
     const Borders borders = borders_of(buckets, max_distance, causal != 0);
     auto go = [&](auto zero) {
         using T = decltype(zero);
-        const BiasShape s = shape_of(H, Q, K, offset, kBiasRows, width_of<T>());
+        const int side = bias_side(Q, K, width_of<T>());
+        const BiasShape s = shape_of(H, Q, K, offset, kWaves / side * kBiasRows, side * width_of<T>());
         const int64_t patches = H * s.row_tiles * s.chunks;
         hipLaunchKernelGGL((bias_kernel<T>), dim3(unsigned(std::min<int64_t>(patches, 1 << 20))),
                            dim3(kBlock), 0, static_cast<hipStream_t>(stream), s, borders,
-                           static_cast<const T*>(table), table_stride, static_cast<T*>(out), head_stride,
-                           row_stride, patches);
+                           static_cast<const T*>(table), table_stride, buckets, static_cast<T*>(out),
+                           head_stride, row_stride, patches, side);
         return launch_status("position bias");
     };
     return dtype == AR_F32 ? go(float(0)) : go(uint16_t(0));
@@ -389,8 +581,9 @@ static ar_status grad_need(int32_t dtype, int32_t buckets, int64_t B, int64_t H,
                            BiasShape* s, GradArgs* a, int64_t* bytes) {
     *bytes = 0;
     if (B == 0 || H == 0 || Q == 0 || K == 0) return AR_OK;
-    *s = shape_of(H, Q, K, 0, kGradRows, dtype == AR_F32 ? width_of<float>() : width_of<uint16_t>());
-    *a = split_of(*s, B);
+    const int width = dtype == AR_F32 ? width_of<float>() : width_of<uint16_t>();
+    *a = split_of(B, H, Q, K, width);
+    *s = shape_of(H, Q, K, 0, a->down * a->rows, a->across * width);
     int64_t parts = 0;
     if (__builtin_mul_overflow(slots_of(*s, *a), H * buckets * 4, &parts))
         return fail(AR_ERR_UNSUPPORTED, "the sizes' product is beyond 2^63");
@@ -450,7 +643,7 @@ AR_EXPORT ar_status ar_position_bias_grad(int32_t dtype, int32_t buckets, int32_
                                    dim3(kBlock), 0, st, H, buckets, to, table_stride);
             return launch_status("position bias gradient");
         }
-        s.c = offset + Q - 1;
+        s.offset = offset;
         a.batch_stride = batch_stride;
         a.head_stride = head_stride;
         a.row_stride = row_stride;
