@@ -20,12 +20,6 @@ namespace {
 
 constexpr int kBlock = 256, kWaves = kBlock / 64;
 
-// Orders a wavefront's accesses to LDS of which one lane's is another's.
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // The distances at which the buckets of a side begin: bucket b of `side` from at[b] on.
 struct Borders {
     int32_t side;
@@ -42,10 +36,6 @@ struct BiasShape {
 struct Patch {
     int64_t h, i0, i1, j0;
 };
-// A quotient, in 32 bits where they hold both.
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-    return ((a | b) >> 32) == 0 ? int64_t(uint32_t(a) / uint32_t(b)) : a / b;
-}
 __device__ __forceinline__ Patch patch_of(const BiasShape& s, int64_t n, int width) {
     const int64_t over = quotient(n, s.chunks), chunk = n - over * s.chunks;
     Patch p;

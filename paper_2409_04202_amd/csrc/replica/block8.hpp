@@ -14,6 +14,8 @@
 // Rows lie at 16 bytes, so a lane writes and reads 16 numbers at once.
 #pragma once
 
+#include <algorithm>
+
 #include "replica.hpp"
 
 namespace arp {
@@ -67,6 +69,36 @@ __device__ __forceinline__ uint32_t four_numbers(const float* x, float inverse) 
 __device__ __forceinline__ void four_values(uint32_t w, float scale, float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = float(int32_t(w << (24 - 8 * i)) >> 24) * scale;
+}
+
+// ------------------------------------------------- passes over rows of runs
+
+// The work in strips of 256 units of 8 or 16 elements, a lane's: `1 << log` units of a
+// row, `chunks` of those to a row, and as many rows as the 256 lanes have left.  No lane
+// divides to find its place.
+struct Cover {
+    int log;
+    int64_t chunks, strips;
+};
+inline Cover cover(int64_t M, int64_t N, int unit) {
+    const int64_t units = kRun / unit * runs_of(N);
+    int log = unit == 8 ? 2 : 1;
+    while (log < 8 && (int64_t(1) << log) < units) ++log;
+    const int64_t chunks = ceil_div(units, int64_t(1) << log);
+    return {log, chunks, chunks * ceil_div(M, int64_t(1) << (8 - log))};
+}
+inline dim3 cover_grid(const Cover& c, int strips) {
+    return dim3(unsigned(std::min<int64_t>(ceil_div(c.strips, strips), 1 << 22)));
+}
+
+struct Place {
+    int64_t row, col;
+};
+template <int UNIT>
+__device__ __forceinline__ Place place(int64_t strip, const Cover& c) {
+    const int64_t rows = quotient(strip, c.chunks), chunk = strip - rows * c.chunks;
+    return {(rows << (8 - c.log)) + (threadIdx.x >> c.log),
+            ((chunk << c.log) + (threadIdx.x & ((1u << c.log) - 1))) * UNIT};
 }
 
 }  // namespace arp

@@ -373,41 +373,58 @@ __global__ __launch_bounds__(256) void factors_kernel(int64_t M, int64_t F, cons
     }
 }
 
-// The same from factors in 8 bits, 16 elements a lane, half of a run.
+// The same from factors in 8 bits.
 template <class T>
-__global__ __launch_bounds__(256) void factors_8_kernel(int64_t M, int64_t F, const T* dh,
+__global__ __launch_bounds__(256) void factors_8_kernel(int64_t M, int64_t F, Cover c, const T* dh,
                                                         int64_t dh_stride, const uint8_t* sg,
                                                         const uint8_t* su, int64_t saved_stride, T* dg,
                                                         T* du, int64_t stride) {
-    constexpr int VEC = Num<T>::VEC, N = 16;
-    const int64_t per = (F + N - 1) / N, step = int64_t(gridDim.x) * 256;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < M * per; i += step) {
-        const int64_t r = i / per, c = i % per * N;
-        const T* const pd = dh + r * dh_stride + c;
-        const uint8_t *pg = sg + r * saved_stride, *pu = su + r * saved_stride;
-        const int64_t scale = runs_of(F) * kRun + c / kRun;
-        const u32x4 cg = *(const AR_GLOBAL u32x4*)(pg + c), cu = *(const AR_GLOBAL u32x4*)(pu + c);
-        const float s = run_scale(pg[scale]), t = run_scale(pu[scale]);
-        float g[N], u[N];
+    constexpr int VEC = Num<T>::VEC, N = 8;
+    const int64_t scales = runs_of(F) * kRun;
+    for (int64_t s = int64_t(blockIdx.x) * 2; s < c.strips; s += int64_t(gridDim.x) * 2) {
+        Place at[2];
+        u32x4 w[2][N / VEC];
+        uint64_t codes[2][2];
+        uint32_t byte[2][2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            four_values(cg[e], s, g + 4 * e);
-            four_values(cu[e], t, u + 4 * e);
+        for (int h = 0; h < 2; ++h) {
+            at[h] = place<N>(s + h, c);
+            if (s + h >= c.strips || at[h].col >= F) at[h].row = M;
+            if (at[h].row >= M) continue;
+            const T* const pd = dh + at[h].row * dh_stride + at[h].col;
+            const int64_t left = F - at[h].col, from = at[h].row * saved_stride;
+#pragma unroll
+            for (int i = 0; i < N / VEC; ++i) {
+                w[h][i] = u32x4{0, 0, 0, 0};
+                if (left >= (i + 1) * VEC) w[h][i] = load_vec(pd + i * VEC);
+                else if (left > i * VEC) w[h][i] = load_part(pd + i * VEC, int(left - i * VEC));
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint8_t* const row = (k ? su : sg) + from;
+                codes[h][k] = *(const AR_GLOBAL uint64_t*)(row + at[h].col);
+                byte[h][k] = row[scales + at[h].col / kRun];
+            }
         }
 #pragma unroll
-        for (int v = 0; v < N; v += VEC) {
-            const int64_t left = F - c - v;
-            if (left <= 0) break;
-            float d[VEC];
-            Num<T>::unpack(left >= VEC ? load_vec(pd + v) : load_part(pd + v, int(left)), d);
+        for (int h = 0; h < 2; ++h) {
+            if (at[h].row >= M) continue;
+            const int64_t left = F - at[h].col;
+            float d[N];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                // (a run of NaN ends with the row)
-                g[v + e] = e < left ? g[v + e] * d[e] : 0.0f;
-                u[v + e] = e < left ? u[v + e] * d[e] : 0.0f;
+            for (int i = 0; i < N / VEC; ++i) Num<T>::unpack(w[h][i], d + i * VEC);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float v[N];
+                four_values(uint32_t(codes[h][k]), run_scale(byte[h][k]), v);
+                four_values(uint32_t(codes[h][k] >> 32), run_scale(byte[h][k]), v + 4);
+                T* const to = (k ? du : dg) + at[h].row * stride + at[h].col;
+                // (rows are whole vectors of 8: the last one's rest is zero, also of a run of NaN)
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = e < left ? v[e] * d[e] : 0.0f;
+#pragma unroll
+                for (int i = 0; i < N; i += VEC) store_vec(to + i, Num<T>::pack(v + i));
             }
-            store_vec(dg + r * stride + c + v, Num<T>::pack(g + v));
-            store_vec(du + r * stride + c + v, Num<T>::pack(u + v));
         }
     }
 }
@@ -858,13 +875,13 @@ AR_EXPORT ar_status ar_glu_backward(int32_t dtype, int64_t M, int64_t D, int64_t
                                saved_stride, dg, du, fs);
         };
         if (M > 0 && F > 0) {
-            if (saved_dtype == AR_BLOCK8)
-                hipLaunchKernelGGL((factors_8_kernel<T>),
-                                   dim3(unsigned(std::min<int64_t>(ceil_div(M * ceil_div(F, 16), 256), 1 << 16))),
-                                   dim3(256), 0, st, M, F, static_cast<const T*>(dh), dh_stride,
+            if (saved_dtype == AR_BLOCK8) {
+                const Cover c = cover(M, F, 8);
+                hipLaunchKernelGGL((factors_8_kernel<T>), cover_grid(c, 2), dim3(256), 0, st, M, F, c,
+                                   static_cast<const T*>(dh), dh_stride,
                                    static_cast<const uint8_t*>(saved_gate),
                                    static_cast<const uint8_t*>(saved_up), saved_stride, dg, du, fs);
-            else if (saved_dtype == AR_F32) factors(float(0));
+            } else if (saved_dtype == AR_F32) factors(float(0));
             else factors(T(0));
         }
         const BackSpace space = back_space(M, D, F, es);

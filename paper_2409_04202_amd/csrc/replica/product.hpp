@@ -496,10 +496,4 @@ struct Store {
     }
 };
 
-// The wavefront's LDS traffic of one lane is another's: order it.
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 }  // namespace arp

@@ -59,6 +59,10 @@ __device__ __forceinline__ uint32_t scalar(uint32_t v) {
     return uint32_t(__builtin_amdgcn_readfirstlane(int(v)));
 }
 
+// A quotient, in 32 bits where they hold both.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? int64_t(uint32_t(a) / uint32_t(b)) : a / b;
+}
 template <class T> struct Num;
 template <> struct Num<float> {
     static constexpr int VEC = 4;  // elements of a 16-byte vector
@@ -117,6 +121,12 @@ __device__ __forceinline__ void store_part(T* p, const u32x4 v, int n) {
     Num<T>::unpack(v, f);
     for (int i = 0; i < Num<T>::VEC; ++i)
         if (i < n) ((AR_GLOBAL T*)p)[i] = Num<T>::down(f[i]);
+}
+
+// The wavefront's LDS traffic of one lane is another's: order it.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 // Reductions over a wavefront, in the register file: after four shifts within

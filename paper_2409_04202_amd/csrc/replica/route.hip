@@ -110,37 +110,47 @@ template <> struct Rank<float> {
     }
 };
 
-// A lane's P logits from `first` on; behind the row's end -inf.
+// A lane's P logits from `first` on, as they lie; the rest of a row's last vector, and
+// what is behind the row, is not read.
 template <class T, int P>
-__device__ __forceinline__ void load_logits(const T* row, int first, int E, float* z) {
-    constexpr int VEC = Num<T>::VEC;
+struct Logits {
+    static constexpr int VEC = Num<T>::VEC, VECS = P / VEC;
+    u32x4 raw[VECS];
+    __device__ __forceinline__ void load(const T* row, int first, int E) {
 #pragma unroll
-    for (int i = 0; i < P; i += VEC) {
-        if (first + i + VEC <= E) {
-            Num<T>::unpack(load_vec(row + first + i), z + i);
-        } else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                z[i + e] = first + i + e < E ? Num<T>::up(((const AR_GLOBAL T*)row)[first + i + e])
-                                             : -INFINITY;
+        for (int i = 0; i < VECS; ++i) {
+            const int left = E - first - i * VEC;
+            raw[i] = u32x4{0, 0, 0, 0};
+            if (left >= VEC) raw[i] = load_vec(row + first + i * VEC);
+            else if (left > 0) raw[i] = load_part(row + first + i * VEC, left);
         }
     }
-}
+    // behind the row's end -inf
+    __device__ __forceinline__ void get(float* z, int first, int E) const {
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) Num<T>::unpack(raw[i], z + i * VEC);
+        if (E % P) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) z[i] = first + i < E ? z[i] : -INFINITY;
+        } else if (first >= E) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) z[i] = -INFINITY;
+        }
+    }
+};
 
-// The row's probabilities and the inverse of their sum, from its largest logit: all NaN
-// where that is a NaN or an infinity.
+// exp of the logits less the largest, and the inverse of their sum: NaN and an infinity, so
+// that their product is NaN, where the largest is a NaN or an infinity; zero for no row.
 template <int LOG, int P>
-__device__ __forceinline__ float softmax(const float* z, float top, float* p) {
+__device__ __forceinline__ float softmax(const float* z, float top, bool any, float* e) {
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        p[i] = exp_below(z[i] - top);
-        s += p[i];
+        e[i] = exp_below(z[i] - top);
+        s += e[i];
     }
-    const float inverse = 1.0f / group_sum<LOG>(s);
-#pragma unroll
-    for (int i = 0; i < P; ++i) p[i] *= inverse;
-    return inverse;
+    s = group_sum<LOG>(s);
+    return any ? 1.0f / s : 0.0f;
 }
 
 // Compares and exchanges until the larger are in front: merges of sorted halves, odd and
@@ -180,11 +190,6 @@ struct RouteArgs {
     float* mass;      // E, or a part a block
 };
 
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // A lane's logits are sorted once; each choice is then a reduction over the lanes'
 // first ones, and the lane that it came from moves on to its next.  Lane j keeps choice
 // j, so gates, counts and stores are made for all of them at once.  Bound by the
@@ -202,16 +207,25 @@ __global__ __launch_bounds__(kRouteBlock) void route_kernel(const T* logits, Rou
     __shared__ float sums[WAVES][WIDE];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> LOG;
     const int sub = lane & (LANES - 1), first = sub * P;
+    const int64_t step = int64_t(gridDim.x) * WAVES * GROUPS;
+    int64_t r0 = (int64_t(blockIdx.x) * WAVES + wave) * GROUPS;
+    Logits<T, P> next;
+    uint8_t next_live = 0;
+    auto fetch = [&](int64_t r) {
+        const bool in = r < a.T;
+        next.load(logits + r * a.stride, in ? first : a.E, a.E);
+        next_live = in ? (a.live ? a.live[r] : 1) : 0;
+    };
+    fetch(r0 + group);
     for (int i = threadIdx.x; i <= WIDE; i += kRouteBlock) hist[i] = 0;
     __syncthreads();
     float mass[P] = {};
-    const int64_t step = int64_t(gridDim.x) * WAVES * GROUPS;
-    for (int64_t r0 = (int64_t(blockIdx.x) * WAVES + wave) * GROUPS; r0 < a.T; r0 += step) {
+    for (; r0 < a.T; r0 += step) {
         const int64_t r = r0 + group;
-        const bool in = r < a.T;
-        float z[P], p[P];
-        load_logits<T, P>(logits + r * a.stride, in ? first : a.E, a.E, z);
-        const bool live = in && (!a.live || a.live[r]);
+        const bool in = r < a.T, live = next_live;
+        float z[P], e[P];
+        next.get(z, first, a.E);
+        fetch(r + step);
         // (a vector, not an array: a choice between its elements is one of registers)
         V key;
         K mine[SLOTS];
@@ -220,9 +234,9 @@ __global__ __launch_bounds__(kRouteBlock) void route_kernel(const T* logits, Rou
         sort_falling<P>(key);
         K best = group_best<LOG>(key[0]);
         const bool any = best != 0;
-        const float top = R::logit(best), inverse = softmax<LOG, P>(z, top, p);
+        const float top = R::logit(best), inverse = softmax<LOG, P>(z, top, any, e);
 #pragma unroll
-        for (int i = 0; i < P; ++i) mass[i] += any ? p[i] : 0.0f;
+        for (int i = 0; i < P; ++i) mass[i] = fmaf(e[i], inverse, mass[i]);
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
             mine[s] = 0;
@@ -247,10 +261,10 @@ __global__ __launch_bounds__(kRouteBlock) void route_kernel(const T* logits, Rou
         for (int s = 0; s < SLOTS; ++s) {
             const int j = s * LANES + sub;
             if (j < a.k && in) {
-                const int e = mine[s] ? int(R::place(mine[s])) : -1;
-                a.ids[r * a.k + j] = e;
+                const int id = mine[s] ? int(R::place(mine[s])) : -1;
+                a.ids[r * a.k + j] = id;
                 a.gates[r * a.k + j] = gate[s] * scale;
-                if (mine[s]) atomicAdd(&hist[e], 1);
+                if (mine[s]) atomicAdd(&hist[id], 1);
             }
         }
         if (sub == 0 && any) atomicAdd(&hist[a.E], 1);
@@ -350,34 +364,50 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> LOG;
     const int sub = lane & (LANES - 1), first = sub * P;
+    const int64_t step = int64_t(gridDim.x - 1) * WAVES * GROUPS;
+    int64_t r0 = (int64_t(blockIdx.x) * WAVES + wave) * GROUPS;
+    Logits<T, P> next;
+    int64_t next_id[SLOTS], next_first = -1;
+    float next_g[SLOTS];
+    auto fetch = [&](int64_t r) {
+        const bool in = r < a.T;
+        next.load(logits + r * a.stride, in ? first : a.E, a.E);
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            const int j = s * LANES + sub;
+            next_id[s] = in && j < a.k ? a.ids[r * a.k + j] : -1;
+            next_g[s] = in && j < a.k && a.dgates ? a.dgates[r * a.k + j] : 0.0f;
+        }
+        next_first = in ? a.ids[r * a.k] : -1;
+    };
+    fetch(r0 + group);
     // the slopes of the loss: coefficient E counts_e / (k N^2)
     const float n = float(a.counts[a.E]);
     const float unit = n > 0.0f ? a.coefficient * float(a.E) / float(a.k) / n / n : 0.0f;
     float slope[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) slope[i] = first + i < a.E ? float(a.counts[first + i]) * unit : 0.0f;
-    const int64_t step = int64_t(gridDim.x - 1) * WAVES * GROUPS;
-    for (int64_t r0 = (int64_t(blockIdx.x) * WAVES + wave) * GROUPS; r0 < a.T; r0 += step) {
+    for (; r0 < a.T; r0 += step) {
         const int64_t r = r0 + group;
-        const bool in = r < a.T;
+        const bool in = r < a.T, live = next_first >= 0;
         float z[P], p[P];
-        load_logits<T, P>(logits + r * a.stride, in ? first : a.E, a.E, z);
+        next.get(z, first, a.E);
         int64_t id[SLOTS];
         float g[SLOTS];
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
-            const int j = s * LANES + sub;
-            const bool here = in && j < a.k;
-            id[s] = here ? a.ids[r * a.k + j] : -1;
-            g[s] = here && a.dgates ? a.dgates[r * a.k + j] : 0.0f;
+            id[s] = next_id[s];
+            g[s] = next_g[s];
         }
-        const bool live = in && a.ids[r * a.k] >= 0;
+        fetch(r + step);
         float top = z[0];
 #pragma unroll
         for (int i = 1; i < P; ++i) top = larger(top, z[i]);
         top = group_max<LOG>(top);
         const bool any = live && top != -INFINITY;
-        softmax<LOG, P>(z, top, p);
+        const float inverse = softmax<LOG, P>(z, top, any, p);
+#pragma unroll
+        for (int i = 0; i < P; ++i) p[i] *= inverse;
         // wants: the sum of the gates' gradients, of those chosen `times` times
         float times[P], wants[P];
 #pragma unroll
