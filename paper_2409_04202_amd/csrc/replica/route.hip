@@ -12,7 +12,10 @@
 namespace arp {
 namespace {
 
-constexpr int kRouteBlock = 1024, kBalanceBlock = 256;
+constexpr int kBalanceBlock = 256;
+constexpr int kWideRow = 512;   // experts above which a lane holds 16 logits, for whose ranks
+                                // 1024 lanes have registers too few
+constexpr int route_block(int logits) { return logits == 16 ? 512 : 1024; }
 constexpr int kMaxParts = 512;  // blocks whose sums are joined: two a CU, all its wavefronts
 
 // exp(x) for x <= 0, to a few units in the last place: 2^(x log2 e) with what the
@@ -23,6 +26,13 @@ __device__ __forceinline__ float exp_below(float x) {
     const float t = x * 1.44269504f, lost = fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269504f, -t));
     const float e = __builtin_amdgcn_exp2f(t);
     return fmaf(e, lost * 0.69314718f, e);
+}
+// The same for sums of bf16 logits' exponentials: as the hardware has it, |x| units off,
+// which is below what a logit's own rounding makes of it.
+template <class T>
+__device__ __forceinline__ float exp_of_logit(float x) {
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(fmaxf(x, -200.0f) * 1.44269504f);
+    else return exp_below(x);
 }
 // The larger number, or a NaN where there is one.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
@@ -71,43 +81,67 @@ template <int LOG> __device__ __forceinline__ float group_max(float v) {
 template <int LOG> __device__ __forceinline__ uint32_t group_most(uint32_t v) {
     return group_reduce<LOG>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
+// The largest of a whole wavefront's lanes, to a scalar register.
+__device__ __forceinline__ uint32_t wave_most(uint32_t v) {
+    auto step = [&](auto ctrl, auto rows) {
+        const uint32_t o = uint32_t(__builtin_amdgcn_update_dpp(0, int(v), decltype(ctrl)::value,
+                                                                decltype(rows)::value, 0xF, false));
+        v = o > v ? o : v;
+    };
+    using std::integral_constant;
+    const integral_constant<int, 0xF> all{};
+    step(integral_constant<int, 0x111>{}, all);     // as wave_reduce's
+    step(integral_constant<int, 0x112>{}, all);
+    step(integral_constant<int, 0x114>{}, all);
+    step(integral_constant<int, 0x118>{}, all);
+    step(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});
+    step(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
+    return uint32_t(__builtin_amdgcn_readlane(int(v), 63));
+}
 // The largest of ranks; one of 64 bits by its upper and then its lower half.
-template <int LOG> __device__ __forceinline__ uint32_t group_best(uint32_t v) { return group_most<LOG>(v); }
+template <int LOG> __device__ __forceinline__ uint32_t group_best(uint32_t v) {
+    if constexpr (LOG == 6) return wave_most(v);
+    else return group_most<LOG>(v);
+}
 template <int LOG> __device__ __forceinline__ uint64_t group_best(uint64_t v) {
-    const uint32_t hi = group_most<LOG>(uint32_t(v >> 32));
-    const uint32_t lo = group_most<LOG>(uint32_t(v >> 32) == hi ? uint32_t(v) : 0u);
+    const uint32_t hi = group_best<LOG>(uint32_t(v >> 32));
+    const uint32_t lo = group_best<LOG>(uint32_t(v >> 32) == hi ? uint32_t(v) : 0u);
     return uint64_t(hi) << 32 | lo;
 }
 
-// A logit and its place as one number: larger for a larger logit, and of equal
-// ones for the lower place.  A NaN is above everything; 0 is an absent expert's.
-// bf16's 16 bits and the place fit 32 bits.
+// A logit and its place as one number: larger for a larger logit, and of equal ones for
+// the lower place.  ODD: where a NaN, which is above everything, or a -0, which is 0, may be
+// among them.  Up to NONE it is -inf's, an absent expert.  bf16's 16 bits and the place fit 32
+// bits.
+__device__ __forceinline__ uint32_t ordered(float z) {
+    const uint32_t u = __float_as_uint(z);
+    return u ^ uint32_t(int32_t(u) >> 31 | int32_t(0x80000000));
+}
+__device__ __forceinline__ float unordered(uint32_t o) {
+    return __uint_as_float(int32_t(o) < 0 ? o ^ 0x80000000u : ~o);
+}
 template <class T> struct Rank;
 template <> struct Rank<uint16_t> {
     using K = uint32_t;
-    static __device__ __forceinline__ K of(float z, uint32_t place) {
-        const uint32_t u = __float_as_uint(z + 0.0f);   // (-0 is 0)
-        const uint32_t o = z != z ? 0xFFFF0000u : (u ^ uint32_t(int32_t(u) >> 31 | int32_t(0x80000000)));
-        return z == -INFINITY ? 0u : (o & 0xFFFF0000u) | (0xFFFFu - place);
+    static constexpr K NONE = 0x007FFFFFu;
+    template <bool ODD> static __device__ __forceinline__ K of(float z, uint32_t place) {
+        const uint32_t o = ODD && z != z ? 0xFFFF0000u : ordered(ODD ? z + 0.0f : z);
+        return (o & 0xFFFF0000u) | (0xFFFFu - place);
     }
     static __device__ __forceinline__ uint32_t place(K k) { return 0xFFFFu - (k & 0xFFFFu); }
     static __device__ __forceinline__ float logit(K k) {
-        const uint32_t o = k & 0xFFFF0000u;
-        return __uint_as_float((int32_t(o) < 0 ? o ^ 0x80000000u : ~o) & 0xFFFF0000u);
+        return __uint_as_float(__float_as_uint(unordered(k)) & 0xFFFF0000u);
     }
 };
 template <> struct Rank<float> {
     using K = uint64_t;
-    static __device__ __forceinline__ K of(float z, uint32_t place) {
-        const uint32_t u = __float_as_uint(z + 0.0f);
-        const uint32_t o = z != z ? 0xFFFFFFFFu : u ^ uint32_t(int32_t(u) >> 31 | int32_t(0x80000000));
-        return z == -INFINITY ? 0u : K(o) << 32 | (0xFFFFFFFFu - place);
+    static constexpr K NONE = 0x007FFFFFFFFFFFFFull;
+    template <bool ODD> static __device__ __forceinline__ K of(float z, uint32_t place) {
+        const uint32_t o = ODD && z != z ? 0xFFFFFFFFu : ordered(ODD ? z + 0.0f : z);
+        return K(o) << 32 | (0xFFFFFFFFu - place);
     }
     static __device__ __forceinline__ uint32_t place(K k) { return 0xFFFFFFFFu - uint32_t(k); }
-    static __device__ __forceinline__ float logit(K k) {
-        const uint32_t o = uint32_t(k >> 32);
-        return __uint_as_float(int32_t(o) < 0 ? o ^ 0x80000000u : ~o);
-    }
+    static __device__ __forceinline__ float logit(K k) { return unordered(uint32_t(k >> 32)); }
 };
 
 // A lane's P logits from `first` on, as they lie; the rest of a row's last vector, and
@@ -141,12 +175,12 @@ struct Logits {
 
 // exp of the logits less the largest, and the inverse of their sum: NaN and an infinity, so
 // that their product is NaN, where the largest is a NaN or an infinity; zero for no row.
-template <int LOG, int P>
+template <class T, int LOG, int P>
 __device__ __forceinline__ float softmax(const float* z, float top, bool any, float* e) {
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        e[i] = exp_below(z[i] - top);
+        e[i] = exp_of_logit<T>(z[i] - top);
         s += e[i];
     }
     s = group_sum<LOG>(s);
@@ -195,11 +229,12 @@ struct RouteArgs {
 // j, so gates, counts and stores are made for all of them at once.  Bound by the
 // reductions' instructions.
 template <class T, int LOG, int P>
-__global__ __launch_bounds__(kRouteBlock) void route_kernel(const T* logits, RouteArgs a) {
+__global__ __launch_bounds__(route_block(P)) void route_kernel(const T* logits, RouteArgs a) {
+    constexpr int BLOCK = route_block(P);
     using R = Rank<T>;
     using K = typename R::K;
     typedef K V __attribute__((ext_vector_type(P)));
-    constexpr int LANES = 1 << LOG, GROUPS = 64 / LANES, WAVES = kRouteBlock / 64;
+    constexpr int LANES = 1 << LOG, GROUPS = 64 / LANES, WAVES = BLOCK / 64;
     constexpr int WIDE = LANES * P;                     // experts at most
     constexpr int PICKS = WIDE < AR_ROUTE_MAX_K ? WIDE : AR_ROUTE_MAX_K;
     constexpr int SLOTS = (PICKS + LANES - 1) / LANES;  // choices a lane keeps
@@ -217,7 +252,7 @@ __global__ __launch_bounds__(kRouteBlock) void route_kernel(const T* logits, Rou
         next_live = in ? (a.live ? a.live[r] : 1) : 0;
     };
     fetch(r0 + group);
-    for (int i = threadIdx.x; i <= WIDE; i += kRouteBlock) hist[i] = 0;
+    for (int i = threadIdx.x; i <= WIDE; i += BLOCK) hist[i] = 0;
     __syncthreads();
     float mass[P] = {};
     for (; r0 < a.T; r0 += step) {
@@ -229,12 +264,20 @@ __global__ __launch_bounds__(kRouteBlock) void route_kernel(const T* logits, Rou
         // (a vector, not an array: a choice between its elements is one of registers)
         V key;
         K mine[SLOTS];
+        bool odd = false;
 #pragma unroll
-        for (int i = 0; i < P; ++i) key[i] = live ? R::of(z[i], uint32_t(first + i)) : K(0);
+        for (int i = 0; i < P; ++i) odd |= __builtin_amdgcn_classf(z[i], 0x23);  // NaN, -0
+        if (__builtin_amdgcn_ballot_w64(odd)) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) key[i] = R::template of<true>(z[i], uint32_t(first + i));
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) key[i] = R::template of<false>(z[i], uint32_t(first + i));
+        }
         sort_falling<P>(key);
         K best = group_best<LOG>(key[0]);
-        const bool any = best != 0;
-        const float top = R::logit(best), inverse = softmax<LOG, P>(z, top, any, e);
+        const bool any = live && best > R::NONE;
+        const float top = R::logit(best), inverse = softmax<T, LOG, P>(z, top, any, e);
 #pragma unroll
         for (int i = 0; i < P; ++i) mass[i] = fmaf(e[i], inverse, mass[i]);
 #pragma unroll
@@ -249,6 +292,7 @@ __global__ __launch_bounds__(kRouteBlock) void route_kernel(const T* logits, Rou
         float gate[SLOTS], total = 0.0f;
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
+            if (!live || mine[s] <= R::NONE) mine[s] = 0;
             gate[s] = mine[s] ? exp_below(R::logit(mine[s]) - top) * inverse : 0.0f;
             total += gate[s];
         }
@@ -277,7 +321,7 @@ __global__ __launch_bounds__(kRouteBlock) void route_kernel(const T* logits, Rou
     __syncthreads();
     int32_t* const counts = a.counts + int64_t(blockIdx.x) * (a.E + 1);
     float* const masses = a.mass + int64_t(blockIdx.x) * a.E;
-    for (int e = threadIdx.x; e <= a.E; e += kRouteBlock) {
+    for (int e = threadIdx.x; e <= a.E; e += BLOCK) {
         counts[e] = hist[e];
         if (e == a.E) break;
         float s = 0.0f;
@@ -367,7 +411,8 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
     const int64_t step = int64_t(gridDim.x - 1) * WAVES * GROUPS;
     int64_t r0 = (int64_t(blockIdx.x) * WAVES + wave) * GROUPS;
     Logits<T, P> next;
-    int64_t next_id[SLOTS], next_first = -1;
+    int next_id[SLOTS];
+    int64_t next_first = -1;
     float next_g[SLOTS];
     auto fetch = [&](int64_t r) {
         const bool in = r < a.T;
@@ -375,7 +420,8 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
             const int j = s * LANES + sub;
-            next_id[s] = in && j < a.k ? a.ids[r * a.k + j] : -1;
+            const int64_t id = in && j < a.k ? a.ids[r * a.k + j] : -1;
+            next_id[s] = id >= 0 && id < a.E ? int(id) : -1;
             next_g[s] = in && j < a.k && a.dgates ? a.dgates[r * a.k + j] : 0.0f;
         }
         next_first = in ? a.ids[r * a.k] : -1;
@@ -387,12 +433,13 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
     float slope[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) slope[i] = first + i < a.E ? float(a.counts[first + i]) * unit : 0.0f;
+    const float plain = a.normalize ? 0.0f : 1.0f;
     for (; r0 < a.T; r0 += step) {
         const int64_t r = r0 + group;
         const bool in = r < a.T, live = next_first >= 0;
         float z[P], p[P];
         next.get(z, first, a.E);
-        int64_t id[SLOTS];
+        int id[SLOTS];
         float g[SLOTS];
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
@@ -405,7 +452,7 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
         for (int i = 1; i < P; ++i) top = larger(top, z[i]);
         top = group_max<LOG>(top);
         const bool any = live && top != -INFINITY;
-        const float inverse = softmax<LOG, P>(z, top, any, p);
+        const float inverse = softmax<T, LOG, P>(z, top, any, p);
 #pragma unroll
         for (int i = 0; i < P; ++i) p[i] *= inverse;
         // wants: the sum of the gates' gradients, of those chosen `times` times
@@ -413,32 +460,36 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
 #pragma unroll
         for (int i = 0; i < P; ++i) times[i] = wants[i] = 0.0f;
         if (a.dgates) {
-            int* const number = chosen[wave] + group * WIDE;
-            float* const want = wanted[wave] + group * WIDE;
+            AR_LDS int* const number = (AR_LDS int*)chosen[wave] + group * WIDE;
+            AR_LDS float* const want = (AR_LDS float*)wanted[wave] + group * WIDE;
             wave_sync();
 #pragma unroll
-            for (int i = 0; i < P; i += 4) *(AR_LDS i32x4*)((AR_LDS int*)number + first + i) = i32x4{0, 0, 0, 0};
+            for (int i = 0; i < P; i += 4) {
+                *(AR_LDS f32x4*)(want + first + i) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (a.normalize) *(AR_LDS i32x4*)(number + first + i) = i32x4{0, 0, 0, 0};
+            }
             wave_sync();
             bool twice = false;
 #pragma unroll
             for (int s = 0; s < SLOTS; ++s)
-                if (id[s] >= 0 && id[s] < a.E) {
+                if (id[s] >= 0) {
                     number[id[s]] = s * LANES + sub + 1;
                     want[id[s]] = g[s];
                 }
             wave_sync();
 #pragma unroll
             for (int s = 0; s < SLOTS; ++s)
-                if (id[s] >= 0 && id[s] < a.E) twice |= number[id[s]] != s * LANES + sub + 1;
+                if (id[s] >= 0) twice |= number[id[s]] != s * LANES + sub + 1;
             if (!__builtin_amdgcn_ballot_w64(twice)) {
 #pragma unroll
                 for (int i = 0; i < P; i += 4) {
-                    const i32x4 m = *(AR_LDS i32x4*)((AR_LDS int*)number + first + i);
-                    const f32x4 w = *(AR_LDS f32x4*)((AR_LDS float*)want + first + i);
+                    const f32x4 w = *(AR_LDS f32x4*)(want + first + i);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        times[i + e] = m[e] ? 1.0f : 0.0f;
-                        wants[i + e] = m[e] ? w[e] : 0.0f;
+                    for (int e = 0; e < 4; ++e) wants[i + e] = w[e];
+                    if (a.normalize) {
+                        const i32x4 m = *(AR_LDS i32x4*)(number + first + i);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) times[i + e] = m[e] ? 1.0f : 0.0f;
                     }
                 }
             } else if (in) {  // an expert more than once in a row: every choice at every lane
@@ -456,8 +507,8 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
         float d[P], sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            d[i] = slope[i] + (a.normalize ? 0.0f : wants[i]);
-            sum += p[i] * d[i];
+            d[i] = fmaf(wants[i], plain, slope[i]);
+            sum = fmaf(p[i], d[i], sum);
         }
         sum = group_sum<LOG>(sum);
 #pragma unroll
@@ -487,7 +538,7 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
     }
 }
 
-// Lanes that hold a row: 8 logits each, 16 above 512 experts.
+// Lanes that hold a row: 8 logits each, 16 of the widest.
 template <class F>
 void by_width(int E, F&& f) {
     const auto go = [&](auto log, auto p) { f(log, p); };
@@ -498,7 +549,7 @@ void by_width(int E, F&& f) {
     else if (E <= 64) go(std::integral_constant<int, 3>{}, eight);
     else if (E <= 128) go(std::integral_constant<int, 4>{}, eight);
     else if (E <= 256) go(std::integral_constant<int, 5>{}, eight);
-    else if (E <= 512) go(std::integral_constant<int, 6>{}, eight);
+    else if (E <= kWideRow) go(std::integral_constant<int, 6>{}, eight);
     else go(std::integral_constant<int, 6>{}, std::integral_constant<int, 16>{});
 }
 int group_log(int64_t E) {
@@ -509,7 +560,7 @@ int group_log(int64_t E) {
 
 // Blocks of a routing, as many as the rows fill.
 int64_t parts_of(int64_t T, int64_t E) {
-    const int64_t rows = (kRouteBlock / 64) * (64 >> group_log(E));
+    const int64_t rows = (route_block(E > kWideRow ? 16 : 8) / 64) * (64 >> group_log(E));
     return std::max<int64_t>(1, std::min<int64_t>(kMaxParts, ceil_div(T, rows)));
 }
 int64_t part_bytes(int64_t T, int64_t E) {
@@ -574,7 +625,7 @@ AR_EXPORT ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, con
         using U = decltype(zero);
         by_width(int(E), [&](auto log, auto p) {
             hipLaunchKernelGGL((route_kernel<U, decltype(log)::value, decltype(p)::value>),
-                               dim3(unsigned(parts)), dim3(kRouteBlock), 0, st,
+                               dim3(unsigned(parts)), dim3(route_block(decltype(p)::value)), 0, st,
                                static_cast<const U*>(logits), a);
         });
         if (parts > 1)

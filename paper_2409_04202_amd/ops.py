@@ -117,9 +117,9 @@ class _on:
     def __exit__(self, *exc):
         for e in reversed(self.entered):
             e.__exit__(*exc)
-        for t in self.written:
-            if t is not None:
-                increment_version(t)
+        written = [t for t in self.written if t is not None]
+        if written:
+            increment_version(written)
         if self.stream is not None:
             for t in self.tensors:
                 if t is not None:

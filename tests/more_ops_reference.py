@@ -68,15 +68,16 @@ def route(logits, k, live=None, normalize=False):
     z = logits.double().numpy()
     ids, gates = np.full((T, k), -1, np.int64), np.zeros((T, k))
     counts, mass = np.zeros(E + 1, np.int64), np.zeros(E)
+    order = np.argsort(-z, axis=1, kind="stable")[:, :k]    # (of equal ones the lower first)
     for t in range(T):
         if (live is not None and not live[t]) or np.all(np.isneginf(z[t])):
             continue
         p = np.exp(z[t] - z[t].max())
         p /= p.sum()
-        order = [e for e in sorted(range(E), key=lambda e: (-z[t, e], e)) if z[t, e] > -np.inf][:k]
-        ids[t, :len(order)] = order
-        gates[t, :len(order)] = p[order] / (p[order].sum() if normalize else 1)
-        counts[order] += 1
+        at = order[t][z[t, order[t]] > -np.inf]
+        ids[t, :len(at)] = at
+        gates[t, :len(at)] = p[at] / (p[at].sum() if normalize else 1)
+        counts[at] += 1
         counts[E] += 1
         mass += p
     return tuple(torch.from_numpy(x) for x in (ids, gates, counts, mass))

@@ -182,7 +182,8 @@ ROUTES = [  # T, E, k, kind
     (1, 4, 1, ""), (8, 64, 2, ""), (9, 1, 1, ""), (70, 8, 8, "ties"), (33, 9, 3, "holes"),
     (300, 16, 5, "ties"), (200, 31, 31, "holes"), (129, 61, 4, ""), (500, 64, 8, "ties"),
     (250, 100, 32, "holes"), (1500, 128, 8, ""), (100, 130, 6, "ties"), (60, 256, 8, "holes"),
-    (70, 511, 7, ""), (40, 513, 9, "ties"), (30, 1024, 32, "holes"), (0, 8, 2, "")]
+    (70, 511, 7, ""), (40, 513, 9, "ties"), (30, 1024, 32, "holes"), (0, 8, 2, ""),
+    (9000, 300, 3, "ties"), (4500, 600, 8, "")]     # (more rows than a launch's wavefronts)
 
 
 def gate_bound(E, k):
