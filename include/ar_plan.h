@@ -652,7 +652,8 @@ ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, const void* l
  * logits, ids, k and normalize are ar_route's; counts and N may be all replicas'
  * (summed by a plan): then the replicas' losses, each with its own mass, add up to
  * the whole batch's, and so do their gradients.  Rows with ids[t, 0] < 0 have a
- * gradient of zero, other ids outside [0, E) none of their gate's.  grad may be logits
+ * gradient of zero, other ids outside [0, E) none of their gate's; an id that a row
+ * has twice counts twice.  A NaN or +inf in a routed row makes its gradient NaN.  grad may be logits
  * itself with the same stride (in place).  coefficient is finite
  * (AR_ERR_INVALID_ARG). */
 ar_status ar_balance(int32_t dtype, int64_t T, int64_t E, int64_t k, const void* logits,

@@ -373,7 +373,9 @@ __global__ __launch_bounds__(256) void factors_kernel(int64_t M, int64_t F, cons
     }
 }
 
-// The same from factors in 8 bits.
+// The same from factors in 8 bits, two strips of rows at a time, 8 elements a lane so that
+// every store is to adjacent bytes.  Bound by memory: 8192 x 16384 bf16 192 us, 5.6 TB/s (16
+// elements a lane 284; from fp32 factors 367).
 template <class T>
 __global__ __launch_bounds__(256) void factors_8_kernel(int64_t M, int64_t F, Cover c, const T* dh,
                                                         int64_t dh_stride, const uint8_t* sg,

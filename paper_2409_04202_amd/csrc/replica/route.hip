@@ -226,8 +226,10 @@ struct RouteArgs {
 
 // A lane's logits are sorted once; each choice is then a reduction over the lanes'
 // first ones, and the lane that it came from moves on to its next.  Lane j keeps choice
-// j, so gates, counts and stores are made for all of them at once.  Bound by the
-// reductions' instructions.
+// j, so gates, counts and stores are made for all of them at once.  The block's sums over its
+// rows go to a part of their own, added in order by another launch: no atomics on floats.
+// Bound by the vector units, by the ranks' sort (a sixth) and the choices (a half): 65536 x 512
+// bf16, k = 8, 48 us (a maximum over all logits for each choice 129), 16384 x 128 7.6.
 template <class T, int LOG, int P>
 __global__ __launch_bounds__(route_block(P)) void route_kernel(const T* logits, RouteArgs a) {
     constexpr int BLOCK = route_block(P);
@@ -332,7 +334,8 @@ __global__ __launch_bounds__(route_block(P)) void route_kernel(const T* logits, 
 }
 
 // The blocks' counts and sums, added in order: 16 experts a block of 64 x 16 lanes,
-// each lane every 64th part.
+// each lane every 64th part, all of its loads in flight together.  512 parts of 512 experts
+// 4.8 us.
 __global__ __launch_bounds__(1024) void route_join_kernel(int parts, int E, const int32_t* counts,
                                                           const float* mass, int32_t* counts_out,
                                                           float* mass_out) {
@@ -391,7 +394,9 @@ __global__ __launch_bounds__(64) void loss_kernel(BalanceArgs a) { loss_of(a); }
 
 // The gradient, and in the last block the loss.  What is chosen reaches the lanes that
 // hold its logits through LDS: a place a logit, with the choice's number (0: none) and
-// its gate's gradient.
+// its gate's gradient.  65536 x 512 bf16, k = 8: 40 us, 3.4 TB/s, bound by the vector units
+// (with every choice compared at every logit 87).  16384 x 128: 10, a row's loads, sums and
+// stores one after the other.
 template <class T, int LOG, int P>
 __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits, T* grad, BalanceArgs a) {
     constexpr int VEC = Num<T>::VEC;

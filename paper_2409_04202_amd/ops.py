@@ -103,10 +103,11 @@ class _on:
 
     def __enter__(self):
         if self.stream is None:
-            if self.like.device.index != torch.cuda.current_device():
-                self.entered = (torch.cuda.device(self.like.device),)
+            device = self.like.device
+            if device.index != torch.cuda.current_device():
+                self.entered = (torch.cuda.device(device),)
                 self.entered[0].__enter__()
-            return _current_stream(self.like.device.index)
+            return _current_stream(device.index)
         if self.stream.device != self.like.device:
             raise ValueError("stream: one of the operands' device expected")
         self.entered = (torch.cuda.device(self.like.device), torch.cuda.stream(self.stream))
@@ -115,11 +116,12 @@ class _on:
         return self.stream.cuda_stream
 
     def __exit__(self, *exc):
-        for e in reversed(self.entered):
-            e.__exit__(*exc)
-        written = [t for t in self.written if t is not None]
-        if written:
-            increment_version(written)
+        if self.entered:
+            for e in reversed(self.entered):
+                e.__exit__(*exc)
+        for t in self.written:
+            if t is not None:
+                increment_version(t)
         if self.stream is not None:
             for t in self.tensors:
                 if t is not None:

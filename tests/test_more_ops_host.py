@@ -2,6 +2,9 @@
 workspaces they ask for (no GPU call is made: every check comes before the first launch)."""
 
 import ctypes
+import os
+import shutil
+import subprocess
 
 import pytest
 
@@ -183,3 +186,16 @@ def test_tensors_are_checked():
                  lambda: ops.glu_forward(x, x, x, save=torch.uint8)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.skipif(not shutil.which("g++"), reason="no C++ compiler")
+def test_no_exception_leaves_an_entry(tmp_path):
+    here = os.path.dirname(os.path.abspath(__file__))
+    exe = str(tmp_path / "more_ops_no_memory")
+    lib = os.path.dirname(arplan._lib._name)
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror",
+                    "-I", os.path.join(os.path.dirname(here), "include"),
+                    os.path.join(here, "c_abi", "more_ops_no_memory.cpp"), "-o", exe,
+                    "-L", lib, "-larplan", "-Wl,-rpath," + lib], check=True)
+    r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=60)
+    assert r.returncode == 0 and r.stdout.count(": %d\n" % arplan.AR_ERR_OOM) == 10, r.stdout
