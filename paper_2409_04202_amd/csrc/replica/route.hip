@@ -213,6 +213,12 @@ __device__ __forceinline__ V moved_up(V v) {
     if constexpr (P == 8) return __builtin_shufflevector(v, zero, 1, 2, 3, 4, 5, 6, 7, 8);
     else return __builtin_shufflevector(v, zero, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 16);
 }
+// The first of a lane's sorted ranks, as many as can be chosen.
+template <int LIST, class V>
+__device__ __forceinline__ auto front(V v) {
+    if constexpr (LIST == sizeof(V) / sizeof(v[0])) return v;
+    else return __builtin_shufflevector(v, v, 0, 1, 2, 3, 4, 5, 6, 7);
+}
 
 struct RouteArgs {
     int64_t T, stride;
@@ -228,17 +234,18 @@ struct RouteArgs {
 // first ones, and the lane that it came from moves on to its next.  Lane j keeps choice
 // j, so gates, counts and stores are made for all of them at once.  The block's sums over its
 // rows go to a part of their own, added in order by another launch: no atomics on floats.
-// Bound by the vector units, by the ranks' sort (a sixth) and the choices (a half): 65536 x 512
-// bf16, k = 8, 48 us (a maximum over all logits for each choice 129), 16384 x 128 7.6.
-template <class T, int LOG, int P>
-__global__ __launch_bounds__(route_block(P)) void route_kernel(const T* logits, RouteArgs a) {
-    constexpr int BLOCK = route_block(P);
+// Bound by the vector units, by the ranks' sort and the choices: 65536 x 512 bf16, k = 8,
+// 44 us (a maximum over all logits for each choice 129), 16384 x 128 7.6.
+template <class T, int LOG, int P, int LIST>
+__global__ __launch_bounds__(route_block(LIST)) void route_kernel(const T* logits, RouteArgs a) {
+    constexpr int BLOCK = route_block(LIST);
     using R = Rank<T>;
     using K = typename R::K;
     typedef K V __attribute__((ext_vector_type(P)));
     constexpr int LANES = 1 << LOG, GROUPS = 64 / LANES, WAVES = BLOCK / 64;
     constexpr int WIDE = LANES * P;                     // experts at most
-    constexpr int PICKS = WIDE < AR_ROUTE_MAX_K ? WIDE : AR_ROUTE_MAX_K;
+    constexpr int MOST = LIST < P ? LIST : AR_ROUTE_MAX_K;
+    constexpr int PICKS = WIDE < MOST ? WIDE : MOST;
     constexpr int SLOTS = (PICKS + LANES - 1) / LANES;  // choices a lane keeps
     __shared__ int32_t hist[WIDE + 1];
     __shared__ float sums[WAVES][WIDE];
@@ -264,19 +271,20 @@ __global__ __launch_bounds__(route_block(P)) void route_kernel(const T* logits, 
         next.get(z, first, a.E);
         fetch(r + step);
         // (a vector, not an array: a choice between its elements is one of registers)
-        V key;
+        V all;
         K mine[SLOTS];
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < P; ++i) odd |= __builtin_amdgcn_classf(z[i], 0x23);  // NaN, -0
         if (__builtin_amdgcn_ballot_w64(odd)) {
 #pragma unroll
-            for (int i = 0; i < P; ++i) key[i] = R::template of<true>(z[i], uint32_t(first + i));
+            for (int i = 0; i < P; ++i) all[i] = R::template of<true>(z[i], uint32_t(first + i));
         } else {
 #pragma unroll
-            for (int i = 0; i < P; ++i) key[i] = R::template of<false>(z[i], uint32_t(first + i));
+            for (int i = 0; i < P; ++i) all[i] = R::template of<false>(z[i], uint32_t(first + i));
         }
-        sort_falling<P>(key);
+        sort_falling<P>(all);
+        auto key = front<LIST>(all);
         K best = group_best<LOG>(key[0]);
         const bool any = live && best > R::NONE;
         const float top = R::logit(best), inverse = softmax<T, LOG, P>(z, top, any, e);
@@ -287,7 +295,7 @@ __global__ __launch_bounds__(route_block(P)) void route_kernel(const T* logits, 
             mine[s] = 0;
             for (int j = 0; j < LANES && s * LANES + j < a.k; ++j) {
                 mine[s] = sub == j ? best : mine[s];
-                key = key[0] == best ? moved_up<P>(key) : key;
+                key = key[0] == best ? moved_up<LIST>(key) : key;
                 best = group_best<LOG>(key[0]);
             }
         }
@@ -564,12 +572,20 @@ int group_log(int64_t E) {
 }
 
 // Blocks of a routing, as many as the rows fill.
-int64_t parts_of(int64_t T, int64_t E) {
-    const int64_t rows = (route_block(E > kWideRow ? 16 : 8) / 64) * (64 >> group_log(E));
+int64_t parts_of(int64_t T, int64_t E, int log) {
+    const int64_t rows = (route_block(E > kWideRow ? 16 : 8) / 64) * (64 >> log);
     return std::max<int64_t>(1, std::min<int64_t>(kMaxParts, ceil_div(T, rows)));
 }
+// Many bf16 rows of which up to 8 are chosen: 16 logits a lane of half as many lanes, of whose
+// ranks the first 8 can be chosen.  A wavefront then has twice the rows for each of its
+// reductions, but half as many fit a SIMD's registers.  us with 8 and with 16 logits a lane,
+// join included: 65536 x 512 47 and 44, 65536 x 128 22 and 19, 262144 x 100 58 and 44; but
+// 16384 x 512 18.6 and 19.9, 32768 x 256 18.7 and 19.4.
+bool doubled(int32_t dtype, int64_t T, int64_t E, int64_t k) {
+    return dtype == AR_BF16 && k <= 8 && E > 64 && E <= kWideRow && T >= 65536;
+}
 int64_t part_bytes(int64_t T, int64_t E) {
-    const int64_t parts = parts_of(T, E);
+    const int64_t parts = parts_of(T, E, group_log(E));     // (or fewer)
     return parts > 1 ? round_up(parts * (2 * E + 1) * 4, 16) : 0;
 }
 
@@ -620,7 +636,8 @@ AR_EXPORT ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, con
         AR_TRY(check_apart(outs[o], mv));
         for (int p = 0; p < o; ++p) AR_TRY(check_apart(outs[o], outs[p]));
     }
-    const int64_t parts = parts_of(T, E);
+    const bool twice = doubled(dtype, T, E, k);
+    const int64_t parts = parts_of(T, E, group_log(E) - (twice ? 1 : 0));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     int32_t* const part_counts = static_cast<int32_t*>(workspace);
     float* const part_mass = reinterpret_cast<float*>(part_counts + parts * (E + 1));
@@ -629,9 +646,15 @@ AR_EXPORT ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, con
     auto go = [&](auto zero) {
         using U = decltype(zero);
         by_width(int(E), [&](auto log, auto p) {
-            hipLaunchKernelGGL((route_kernel<U, decltype(log)::value, decltype(p)::value>),
-                               dim3(unsigned(parts)), dim3(route_block(decltype(p)::value)), 0, st,
-                               static_cast<const U*>(logits), a);
+            constexpr int LOG = decltype(log)::value, P = decltype(p)::value;
+            auto run = [&](auto kernel, int list) {
+                hipLaunchKernelGGL(kernel, dim3(unsigned(parts)), dim3(route_block(list)), 0, st,
+                                   static_cast<const U*>(logits), a);
+            };
+            if constexpr (sizeof(U) == 2 && P == 8 && LOG > 3) {
+                if (twice) return run(route_kernel<U, LOG - 1, 16, 8>, 8);
+            }
+            run(route_kernel<U, LOG, P, P>, P);
         });
         if (parts > 1)
             hipLaunchKernelGGL(route_join_kernel, dim3(unsigned(ceil_div(E + 1, 16))), dim3(1024), 0,

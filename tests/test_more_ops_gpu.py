@@ -186,6 +186,25 @@ ROUTES = [  # T, E, k, kind
     (9000, 300, 3, "ties"), (4500, 600, 8, "")]     # (more rows than a launch's wavefronts)
 
 
+@pytest.mark.parametrize("E,k", [(66, 8), (100, 3), (129, 8), (250, 1), (300, 5), (512, 8)])
+def test_route_of_many_rows(E, k):
+    """The form for many rows chooses as that for few does, ties and holes among them, bit for
+    bit; its sums over rows are the few rows' sums up to the additions."""
+    T, step = 70000, 5000
+    z = torch.cat([logits_of(90 + i, T // 7, E, "bf16", ("", "ties", "holes")[i % 3]) for i in range(7)])
+    z = z[:, torch.randperm(E, generator=torch.Generator().manual_seed(91))].cuda()
+    live = (torch.rand(T, generator=torch.Generator().manual_seed(92)) < 0.8).cuda()
+    ids, gates, counts, mass = ops.route(z, k, live=live, normalize=True)
+    parts = [ops.route(z[i:i + step], k, live=live[i:i + step], normalize=True)
+             for i in range(0, T, step)]
+    assert torch.equal(ids, torch.cat([p[0] for p in parts]))
+    assert torch.equal(counts, sum(p[2] for p in parts))
+    few = torch.cat([p[1] for p in parts])
+    near(gates, few.double().cpu(), few.double().cpu() * 2 * gate_bound(E, k) + 2e-36)
+    want = sum(p[3].double() for p in parts).cpu()
+    near(mass, want, want * 2 * (E + 16 + T / 512) * U + T * 1e-36)
+
+
 def gate_bound(E, k):
     """exp to 4 units, the sum's E additions, its inverse and a product, twice where gates
     are normalized (by a sum of k); what underflows is below 1e-36."""
