@@ -382,7 +382,7 @@ __global__ __launch_bounds__(1024) void route_join_kernel(int parts, int E, cons
 struct BalanceArgs {
     int64_t T, stride, grad_stride;
     int E, k, normalize;
-    float coefficient;
+    float coefficient, scale;   // coefficient E / k
     const int64_t* ids;
     const int32_t* counts;
     const float *mass, *dgates;
@@ -402,9 +402,9 @@ __global__ __launch_bounds__(64) void loss_kernel(BalanceArgs a) { loss_of(a); }
 
 // The gradient, and in the last block the loss.  What is chosen reaches the lanes that
 // hold its logits through LDS: a place a logit, with the choice's number (0: none) and
-// its gate's gradient.  65536 x 512 bf16, k = 8: 40 us, 3.4 TB/s, bound by the vector units
-// (with every choice compared at every logit 87).  16384 x 128: 10, a row's loads, sums and
-// stores one after the other.
+// its gate's gradient.  65536 x 512 bf16, k = 8: 33 us, 4 TB/s, bound by the vector units
+// (with every choice compared at every logit 87).  At most five blocks a CU, all that fit its
+// registers: 16384 blocks, each of which gets the slopes first, took 87.
 template <class T, int LOG, int P>
 __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits, T* grad, BalanceArgs a) {
     constexpr int VEC = Num<T>::VEC;
@@ -440,12 +440,14 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
         next_first = in ? a.ids[r * a.k] : -1;
     };
     fetch(r0 + group);
-    // the slopes of the loss: coefficient E counts_e / (k N^2)
-    const float n = float(a.counts[a.E]);
-    const float unit = n > 0.0f ? a.coefficient * float(a.E) / float(a.k) / n / n : 0.0f;
+    // the slopes of the loss: coefficient E counts_e / (k N^2), all counts in flight together
+    Logits<float, P> counts;
+    counts.load(reinterpret_cast<const float*>(a.counts), first, a.E);
+    const float n = float(a.counts[a.E]), share = n > 0.0f ? 1.0f / n : 0.0f;
+    const float unit = a.scale * share * share;
     float slope[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i) slope[i] = first + i < a.E ? float(a.counts[first + i]) * unit : 0.0f;
+    for (int i = 0; i < P; ++i) slope[i] = float(int32_t(counts.raw[i / 4][i % 4])) * unit;
     const float plain = a.normalize ? 0.0f : 1.0f;
     for (; r0 < a.T; r0 += step) {
         const int64_t r = r0 + group;
@@ -530,14 +532,14 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
             float total = 0.0f, dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                total += times[i] != 0.0f ? p[i] * times[i] : 0.0f;
-                dot += times[i] != 0.0f ? p[i] * wants[i] : 0.0f;
+                total = fmaf(p[i], times[i], total);
+                dot = fmaf(p[i], wants[i], dot);
             }
-            const float share = 1.0f / group_sum<LOG>(total);
+            total = group_sum<LOG>(total);
+            const float share = total > 0.0f ? 1.0f / total : 0.0f;
             dot = group_sum<LOG>(dot) * share;
 #pragma unroll
-            for (int i = 0; i < P; ++i)
-                d[i] += times[i] != 0.0f ? p[i] * share * (wants[i] - times[i] * dot) : 0.0f;
+            for (int i = 0; i < P; ++i) d[i] = fmaf(p[i] * share, fmaf(-times[i], dot, wants[i]), d[i]);
         }
         if (!in) continue;
         T* const to = grad + r * a.grad_stride;
@@ -688,7 +690,7 @@ AR_EXPORT ar_status ar_balance(int32_t dtype, int64_t T, int64_t E, int64_t k, c
     for (const MatArg& i : {ml, mi, mc, mm, md, mg}) AR_TRY(check_apart(mo, i));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const BalanceArgs a{T, logits_stride, grad_stride, int(E), int(k), normalize, coefficient,
-                        ids, counts, mass, dgates, loss};
+                        coefficient * float(E) / float(k), ids, counts, mass, dgates, loss};
     if (rows == 0) {
         hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(64), 0, st, a);
         return launch_status("balance loss");
@@ -698,7 +700,7 @@ AR_EXPORT ar_status ar_balance(int32_t dtype, int64_t T, int64_t E, int64_t k, c
         by_width(int(E), [&](auto log, auto p) {
             const int64_t blocks = ceil_div(T, (kBalanceBlock / 64) * (64 >> decltype(log)::value));
             hipLaunchKernelGGL((balance_kernel<U, decltype(log)::value, decltype(p)::value>),
-                               dim3(unsigned(std::min<int64_t>(blocks, 2048)) + 1), dim3(kBalanceBlock),
+                               dim3(unsigned(std::min<int64_t>(blocks, 1280)) + 1), dim3(kBalanceBlock),
                                0, st,
                                static_cast<const U*>(logits), static_cast<U*>(grad), a);
         });
