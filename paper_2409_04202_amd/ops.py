@@ -49,9 +49,9 @@ def _matrix(name, x, shape=None, like=None):
     if like is None:
         if x.dtype not in _DT:
             raise ValueError("%s: float32 or bfloat16 expected, got %s" % (name, x.dtype))
-    elif x.dtype != like.dtype or x.device != like.device:
+    elif x.dtype != like.dtype or x.get_device() != like.get_device():
         raise ValueError("%s: type and device differ from the first operand's" % name)
-    if shape is not None and tuple(x.shape) != tuple(shape):
+    if shape is not None and x.shape != shape:
         raise ValueError("%s: shape %s expected, got %s" % (name, tuple(shape), tuple(x.shape)))
     rows, cols = x.shape
     if cols > 1 and x.stride(1) != 1:
@@ -61,9 +61,9 @@ def _matrix(name, x, shape=None, like=None):
 
 def _strides(name, x, shape, like):
     """The strides of all but the last dimension, after the checks."""
-    if not isinstance(x, torch.Tensor) or tuple(x.shape) != tuple(shape):
+    if not isinstance(x, torch.Tensor) or x.shape != shape:
         raise ValueError("%s: shape %s expected" % (name, tuple(shape)))
-    if x.dtype != like.dtype or x.device != like.device:
+    if x.dtype != like.dtype or x.get_device() != like.get_device():
         raise ValueError("%s: type and device differ from the first operand's" % name)
     if x.shape[-1] > 1 and x.stride(-1) != 1:
         raise ValueError("%s: the elements of a row have to be adjacent" % name)
@@ -364,16 +364,9 @@ def checkpoint_load(kept, width, dtype=None, out=None, stream=None):
 
 # --------------------------------------------------------------- routing
 
-def _vector(name, x, n, dtype, like):
-    if (not isinstance(x, torch.Tensor) or x.shape != (n,) or x.dtype != dtype
-            or x.device != like.device or not x.is_contiguous()):
-        raise ValueError("%s: a contiguous %s vector of %d on the operands' device expected"
-                         % (name, str(dtype)[6:], n))
-
-
-def _choices(name, x, shape, dtype, like):
-    if (not isinstance(x, torch.Tensor) or tuple(x.shape) != tuple(shape) or x.dtype != dtype
-            or x.device != like.device or not x.is_contiguous()):
+def _whole_rows(name, x, shape, dtype, like):
+    if (not isinstance(x, torch.Tensor) or x.shape != shape or x.dtype != dtype
+            or x.get_device() != like.get_device() or not x.is_contiguous()):
         raise ValueError("%s: a contiguous %s tensor of shape %s on the operands' device expected"
                          % (name, str(dtype)[6:], tuple(shape)))
 
@@ -390,18 +383,18 @@ def route(logits, k, live=None, normalize=False, counts=None, mass=None, workspa
     sl = _matrix("logits", logits)
     T, E = logits.shape
     if live is not None:
-        _vector("live", live, T, torch.bool, logits)
+        _whole_rows("live", live, (T,), torch.bool, logits)
     with _on(logits, stream, (logits, live, counts, mass, workspace), (counts, mass)) as s:
         dev = logits.device
         w, n, keep = _space(workspace, arplan.ar_route_workspace(T, E, k), logits)
         if counts is None:
             counts = torch.empty(E + 1, dtype=torch.int32, device=dev)
         else:
-            _vector("counts", counts, E + 1, torch.int32, logits)
+            _whole_rows("counts", counts, (E + 1,), torch.int32, logits)
         if mass is None:
             mass = torch.empty(E, dtype=torch.float32, device=dev)
         else:
-            _vector("mass", mass, E, torch.float32, logits)
+            _whole_rows("mass", mass, (E,), torch.float32, logits)
         ids = torch.empty(T, k, dtype=torch.int64, device=dev)
         gates = torch.empty(T, k, dtype=torch.float32, device=dev)
         arplan.ar_route(_DT[logits.dtype], T, E, k, logits, sl, live, normalize, ids, gates, counts,
@@ -419,15 +412,14 @@ def balance(logits, ids, counts, mass, coefficient=0.01, normalize=False, dgates
     losses and gradients then add up to the whole batch's."""
     sl = _matrix("logits", logits)
     T, E = logits.shape
-    _ids("ids", ids, logits)
-    if ids.dim() != 2 or ids.shape[0] != T:
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
         raise ValueError("ids: a row for each of logits' expected")
     k = ids.shape[1]
-    _choices("ids", ids, (T, k), torch.int64, logits)
-    _vector("counts", counts, E + 1, torch.int32, logits)
-    _vector("mass", mass, E, torch.float32, logits)
+    _whole_rows("ids", ids, (T, k), torch.int64, logits)
+    _whole_rows("counts", counts, (E + 1,), torch.int32, logits)
+    _whole_rows("mass", mass, (E,), torch.float32, logits)
     if dgates is not None:
-        _choices("dgates", dgates, (T, k), torch.float32, logits)
+        _whole_rows("dgates", dgates, (T, k), torch.float32, logits)
         if grad is None:
             raise ValueError("dgates: grad has to be given")
     sg = _matrix("grad", grad, (T, E), logits) if grad is not None else 0
