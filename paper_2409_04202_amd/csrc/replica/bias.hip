@@ -92,6 +92,12 @@ __device__ __forceinline__ void vectors_of(const u32x4 a, const u32x4 b, uint16_
         }
 }
 
+template <class T>
+__device__ __forceinline__ T element(const u32x4 v, int e) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(v[e]);
+    else return T(v[e / 2] >> (16 * (e % 2)));
+}
+
 // The values of a patch's diagonals lie in LDS; a lane reads those of VEC rows at once,
 // and their vectors are parts of them.  Bound by memory, the matrix is written once: 16 x
 // 2048 x 2048 bf16, 134 MB, 26.4 us, 5.1 TB/s (a fill of that size 24).  Lanes that keep a
@@ -139,11 +145,10 @@ __global__ __launch_bounds__(kBlock) void bias_kernel(BiasShape s, Borders borde
                 if (j + VEC <= s.K) {
                     store_vec(to + r * row_stride, v[r]);
                 } else if (j < s.K) {
-                    float f[VEC];
-                    Num<T>::unpack(v[r], f);
+                    // (bits: a conversion would change those of a NaN)
 #pragma unroll
                     for (int e = 0; e < VEC; ++e)
-                        if (j + e < s.K) ((AR_GLOBAL T*)to)[r * row_stride + e] = Num<T>::down(f[e]);
+                        if (j + e < s.K) ((AR_GLOBAL T*)to)[r * row_stride + e] = element<T>(v[r], e);
                 }
             }
         }

@@ -54,30 +54,26 @@ struct ForwardArgs {
 // it, and columns behind the matrix' last are zeros.
 __device__ __forceinline__ void store_runs(const AR_LDS float* part, uint8_t* out, int64_t stride,
                                            int64_t r0, int64_t rows, int64_t c0, int64_t cols) {
-    const int lane = int(threadIdx.x) & 63, c = (lane & 1) * 16;
+    const int lane = int(threadIdx.x) & 63, r = lane >> 1, c = (lane & 1) * 16;
     if (c0 >= cols) return;
+    const AR_LDS float* const row = part + r * Store<1>::PITCH + c;
+    float v[16];
+    uint32_t top = 0;
 #pragma unroll
-    for (int b = 0; b < 32; b += 32) {
-        const int r = b + (lane >> 1);
-        const AR_LDS float* const row = part + r * Store<1>::PITCH + c;
-        float v[16];
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            v[e] = c0 + c + e < cols ? row[e] : 0.0f;
-            top = max(top, magnitude(v[e]));
-        }
-        top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0xB1, 0xF, 0xF, true)));
-        const uint32_t byte = run_byte(top);
-        const float inverse = run_inverse(byte);
-        if (r0 + r >= rows) continue;
-        uint8_t* const to = out + (r0 + r) * stride;
-        u32x4 codes;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) codes[i] = four_numbers(v + 4 * i, inverse);
-        *(AR_GLOBAL u32x4*)(to + c0 + c) = codes;
-        if (c == 0) to[runs_of(cols) * kRun + c0 / kRun] = uint8_t(byte);
+    for (int e = 0; e < 16; ++e) {
+        v[e] = c0 + c + e < cols ? row[e] : 0.0f;
+        top = max(top, magnitude(v[e]));
     }
+    top = max(top, uint32_t(__builtin_amdgcn_mov_dpp(int(top), 0xB1, 0xF, 0xF, true)));
+    const uint32_t byte = run_byte(top);
+    const float inverse = run_inverse(byte);
+    if (r0 + r >= rows) return;
+    uint8_t* const to = out + (r0 + r) * stride;
+    u32x4 codes;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) codes[i] = four_numbers(v + 4 * i, inverse);
+    *(AR_GLOBAL u32x4*)(to + c0 + c) = codes;
+    if (c == 0) to[runs_of(cols) * kRun + c0 / kRun] = uint8_t(byte);
 }
 
 // Where the sums of a part of a tile (rows x cols) are.

@@ -72,6 +72,20 @@ def test_position_bias(H, Q, K, offset, buckets, most, causal, dtype, layout):
         assert bool((around == 7.0).all()), "elements around the output were written"
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", (8, 13, 519))
+def test_position_bias_copies_bits(K, dtype):
+    """Every bit of the table's values, those of NaN among them, at whole vectors and parts."""
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    top = 1 << 15 if dtype == "bf16" else 1 << 31
+    g = torch.Generator().manual_seed(9)
+    table = torch.randint(-top, top, (32, 3), generator=g).to(bits)
+    table[::2] = (table[::2] | (0x7F80 if dtype == "bf16" else 0x7F800000))     # NaN of all kinds
+    want = ref.position_bias(table.view(ref.TORCH[dtype]), 21, K, 3, 128, False)
+    got = ops.position_bias(table.view(ref.TORCH[dtype]).cuda(), 21, K, offset=3)
+    assert torch.equal(got.cpu().view(bits), want.view(bits))
+
+
 @pytest.mark.parametrize("accumulate", (False, True))
 @pytest.mark.parametrize("layout", ("rows", "wide"))
 @pytest.mark.parametrize("dtype", DTYPES)
