@@ -124,6 +124,24 @@ def test_position_bias_grad_of_real_numbers(dtype):
     near(out, want, size * (8 * 32 + 3 + 8 + 6 + 16 + 6) * U + stored(want, dtype))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,H,Q,K,offset,causal", [
+    (70, 2, 1, 40, 39, True), (33, 1, 5, 1600, 0, False), (9, 3, 17, 30, 0, False),
+    (2, 1, 1, 100003, 99000, False), (1, 2, 700, 1, 0, False), (1, 1, 300, 300, 1 << 62, True),
+    (1, 1, 30, 300, -(1 << 62), True), (1, 1, 30, 300, -(1 << 62), False), (2, 40, 90, 2100, 0, False)])
+def test_position_bias_grad_at_its_ends(B, H, Q, K, offset, causal, dtype):
+    """Many sequences, single rows and columns, distances beyond 32 bits: whole numbers."""
+    g = torch.Generator().manual_seed(10)
+    d = torch.randint(-1, 2, (B, H, Q, K), generator=g).to(ref.TORCH[dtype])
+    want, _ = ref.position_bias_grad(d, 32, offset, 128, causal)
+    out = torch.empty(32, H, dtype=d.dtype, device="cuda")
+    ops.position_bias_grad(d.cuda(), out, offset=offset, causal=causal)
+    assert torch.equal(out.cpu(), want.float().to(d.dtype))
+    table = rnd(11, 32, H, dtype=dtype)
+    assert torch.equal(ops.position_bias(table.cuda(), Q, K, offset=offset, causal=causal).cpu(),
+                       ref.position_bias(table, Q, K, offset, 128, causal))
+
+
 def test_position_bias_grad_of_shared_heads_and_batches():
     """A gradient that is the same for several heads and sequences has strides of zero."""
     g = torch.Generator().manual_seed(4)
@@ -580,6 +598,37 @@ def test_calls_on_another_stream():
     for a, b in zip((bias, ids, gates, counts, mass, dlogits, dtable), want[:5] + [want[6], want[11]]):
         assert torch.equal(a, b)
     assert torch.equal(x, ops.checkpoint_load(ops.checkpoint_store(s["x"]), 72, torch.bfloat16))
+
+
+def test_two_streams_at_once():
+    """Calls that overlap, each with what it allocates itself."""
+    a, b = state("bf16"), state("f32")
+    want = [[t.clone() for t in step(s)] for s in (a, b)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [None, None]
+    for _ in range(5):
+        for i, s in enumerate((a, b)):
+            with torch.cuda.stream(streams[i]):
+                got[i] = step(s)
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        for p, q in zip(x, y):
+            assert torch.equal(p, q)
+
+
+def test_counts_in_a_slice_of_a_vector():
+    """Counts and mass at any element of a vector that a plan sums, and nothing beside them."""
+    z = rnd(81, 3000, 61, dtype="bf16").cuda()
+    ids, _, counts, mass = ops.route(z, 3)
+    loss, grad = ops.balance(z, ids, counts, mass, grad=torch.empty_like(z))
+    whole, sums = torch.full((100,), -5, dtype=torch.int32, device="cuda"), torch.full((99,), 7.0, device="cuda")
+    ops.route(z, 3, counts=whole[7:69], mass=sums[5:66])
+    assert torch.equal(whole[7:69], counts) and torch.equal(sums[5:66], mass)
+    assert bool((whole[:7] == -5).all()) and bool((whole[69:] == -5).all())
+    assert bool((sums[:5] == 7).all()) and bool((sums[66:] == 7).all())
+    again, other = ops.balance(z, ids, whole[7:69], sums[5:66], grad=torch.empty_like(z))
+    assert torch.equal(again, loss) and torch.equal(other, grad)
 
 
 def test_given_workspaces_and_what_counts_as_changed():
