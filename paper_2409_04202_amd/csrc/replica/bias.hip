@@ -298,9 +298,9 @@ __device__ __forceinline__ void sum_patch(const T* from, const T* end, int64_t s
 
 // A block's sums by bucket, to its slot of `part`, or straight to the table where a
 // head has one slot.  Bound by memory, the gradients pass once: 4 x 16 x 2048 x 2048 bf16, 537
-// MB, 83 us, 6.4 TB/s, its join 4.6.  (Lanes that walk down their diagonals, each row's
+// MB, 85 us, 6.3 TB/s, its join 4.6.  (Lanes that walk down their diagonals, each row's
 // vector off 16 bytes by one element more: 113.)  3 x 5 x 509 x 1021 f32, of which 23 MB are
-// seen: 13.8 and 3.8, the steps of a block one after the other.
+// seen: 13.6 and 3.8, the steps of a block one after the other.
 template <class T>
 __global__ __launch_bounds__(kBlock, 4) void bias_grad_kernel(BiasShape s, Borders borders, GradArgs a,
                                                            const T* d, int32_t buckets, float* part,

@@ -20,7 +20,7 @@ ar_status check_block8(const char* name, const void* p, int64_t rows, int64_t wi
 namespace {
 
 // 16 elements a lane, half of a run, whose numbers are one vector.  Bound by memory: 8192 x
-// 16384 bf16 82 us, 5.0 TB/s.  (8 elements a lane, or stores past the caches: 89.)
+// 16384 bf16 84 us, 4.9 TB/s.  (8 elements a lane, or stores past the caches: 89.)
 template <class T>
 __global__ __launch_bounds__(256) void keep_kernel(int64_t M, int64_t N, Cover c, const T* x,
                                                    int64_t x_stride, uint8_t* kept, int64_t stride) {

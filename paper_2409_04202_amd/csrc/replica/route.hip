@@ -13,8 +13,9 @@ namespace arp {
 namespace {
 
 constexpr int kBalanceBlock = 256;
-constexpr int kWideRow = 512;   // experts above which a lane holds 16 logits, for whose ranks
-                                // 1024 lanes have registers too few
+constexpr int kWideRow = 512;   // experts above which a lane holds 16 logits
+// (Of blocks with 16 logits a lane a CU's registers hold one of 1024 lanes, and all 512 parts
+// at once as blocks of 512: 65536 x 512 44 and 42 us.)
 constexpr int route_block(int logits) { return logits == 16 ? 512 : 1024; }
 constexpr int kMaxParts = 512;  // blocks whose sums are joined: two a CU, all its wavefronts
 
@@ -235,10 +236,10 @@ struct RouteArgs {
 // j, so gates, counts and stores are made for all of them at once.  The block's sums over its
 // rows go to a part of their own, added in order by another launch: no atomics on floats.
 // Bound by the vector units, by the ranks' sort and the choices: 65536 x 512 bf16, k = 8,
-// 44 us (a maximum over all logits for each choice 129), 16384 x 128 7.6.
+// 42 us (a maximum over all logits for each choice 129), 16384 x 128 7.6.
 template <class T, int LOG, int P, int LIST>
-__global__ __launch_bounds__(route_block(LIST)) void route_kernel(const T* logits, RouteArgs a) {
-    constexpr int BLOCK = route_block(LIST);
+__global__ __launch_bounds__(route_block(P)) void route_kernel(const T* logits, RouteArgs a) {
+    constexpr int BLOCK = route_block(P);
     using R = Rank<T>;
     using K = typename R::K;
     typedef K V __attribute__((ext_vector_type(P)));
@@ -402,7 +403,7 @@ __global__ __launch_bounds__(64) void loss_kernel(BalanceArgs a) { loss_of(a); }
 
 // The gradient, and in the last block the loss.  What is chosen reaches the lanes that
 // hold its logits through LDS: a place a logit, with the choice's number (0: none) and
-// its gate's gradient.  65536 x 512 bf16, k = 8: 33 us, 4 TB/s, bound by the vector units
+// its gate's gradient.  65536 x 512 bf16, k = 8: 35 us, 3.9 TB/s, bound by the vector units
 // (with every choice compared at every logit 87).  At most five blocks a CU, all that fit its
 // registers: 16384 blocks, each of which gets the slopes first, took 87.
 template <class T, int LOG, int P>
@@ -578,10 +579,11 @@ int64_t parts_of(int64_t T, int64_t E, int log) {
     const int64_t rows = (route_block(E > kWideRow ? 16 : 8) / 64) * (64 >> log);
     return std::max<int64_t>(1, std::min<int64_t>(kMaxParts, ceil_div(T, rows)));
 }
+
 // Many bf16 rows of which up to 8 are chosen: 16 logits a lane of half as many lanes, of whose
 // ranks the first 8 can be chosen.  A wavefront then has twice the rows for each of its
 // reductions, but half as many fit a SIMD's registers.  us with 8 and with 16 logits a lane,
-// join included: 65536 x 512 47 and 44, 65536 x 128 22 and 19, 262144 x 100 58 and 44; but
+// join included: 65536 x 512 47 and 42, 65536 x 128 22 and 19, 262144 x 100 58 and 43; but
 // 16384 x 512 18.6 and 19.9, 32768 x 256 18.7 and 19.4.
 bool doubled(int32_t dtype, int64_t T, int64_t E, int64_t k) {
     return dtype == AR_BF16 && k <= 8 && E > 64 && E <= kWideRow && T >= 65536;
@@ -654,7 +656,7 @@ AR_EXPORT ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, con
                                    static_cast<const U*>(logits), a);
             };
             if constexpr (sizeof(U) == 2 && P == 8 && LOG > 3) {
-                if (twice) return run(route_kernel<U, LOG - 1, 16, 8>, 8);
+                if (twice) return run(route_kernel<U, LOG - 1, 16, 8>, 16);
             }
             run(route_kernel<U, LOG, P, P>, P);
         });
