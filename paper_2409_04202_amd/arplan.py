@@ -165,9 +165,8 @@ def _check(status):
 def _ptr(x):
     if x is None:
         return None
-    if hasattr(x, "data_ptr"):
-        return int(x.data_ptr())
-    return int(x)
+    at = getattr(x, "data_ptr", None)
+    return int(x) if at is None else at()
 
 
 def pointers(bufs):

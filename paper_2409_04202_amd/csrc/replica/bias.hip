@@ -11,7 +11,6 @@
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
-#include <vector>
 
 #include "replica.hpp"
 
@@ -423,44 +422,48 @@ __global__ __launch_bounds__(kBlock) void table_zero_kernel(int64_t H, int32_t b
 
 // ---------------------------------------------------------------- host
 
-// Whether a >= b, for products of whole numbers: little ends first.
-using Whole = std::vector<uint32_t>;
-void times(Whole* w, uint32_t by) {
-    uint64_t carry = 0;
-    for (uint32_t& x : *w) {
-        carry += uint64_t(x) * by;
-        x = uint32_t(carry);
-        carry >>= 32;
+// Products of up to AR_POSITION_MAX_BUCKETS / 2 numbers below 2^32, little ends first.
+struct Whole {
+    uint32_t word[AR_POSITION_MAX_BUCKETS / 2];
+    int words = 1;
+    Whole() { word[0] = 1; }
+    void times(uint32_t by) {
+        uint64_t carry = 0;
+        for (int i = 0; i < words; ++i) {
+            carry += uint64_t(word[i]) * by;
+            word[i] = uint32_t(carry);
+            carry >>= 32;
+        }
+        if (carry) word[words++] = uint32_t(carry);
     }
-    if (carry) w->push_back(uint32_t(carry));
-}
-bool at_least(const Whole& a, const Whole& b) {
-    if (a.size() != b.size()) return a.size() > b.size();
-    for (size_t i = a.size(); i-- > 0;)
-        if (a[i] != b[i]) return a[i] > b[i];
-    return true;
-}
+    bool at_least(const Whole& o) const {
+        if (words != o.words) return words > o.words;
+        for (int i = words; i-- > 0;)
+            if (word[i] != o.word[i]) return word[i] > o.word[i];
+        return true;
+    }
+};
 
 // Where far bucket ones + m begins: the least n with (n / ones)^q >= (most / ones)^m,
-// q = side - ones.  The root is taken in 64 bits of significand; where it lies so near a
-// whole number that this may have decided wrongly, whole numbers decide.
+// q = side - ones.  The powers of the root are within 3e-14 of their value; where one lies so
+// near a whole number that this may decide wrongly, whole numbers decide.
 Borders borders_of(int32_t buckets, int32_t most, bool causal) {
     Borders s{};
     s.causal = causal;
     s.side = causal ? buckets : buckets / 2;
     const int32_t ones = s.side / 2, q = s.side - ones;
     for (int32_t b = 0; b <= ones; ++b) s.at[b] = b;
-    const long double ratio = powl((long double)most / ones, 1.0L / q);
-    long double v = ones;
+    const double ratio = std::pow(double(most) / ones, 1.0 / q);
+    double v = ones;
     for (int32_t m = 1; m < q; ++m) {
         v *= ratio;
-        int64_t n = int64_t(ceill(v));
-        const int64_t near = int64_t(llroundl(v));
-        if (fabsl(v - near) <= 1e-14L * v) {
-            Whole left{1}, right{1};
-            for (int32_t i = 0; i < q; ++i) times(&left, uint32_t(near));
-            for (int32_t i = 0; i < q; ++i) times(&right, uint32_t(i < m ? most : ones));
-            n = at_least(left, right) ? near : near + 1;
+        int64_t n = int64_t(std::ceil(v));
+        const int64_t near = int64_t(v + 0.5);
+        if (std::fabs(v - double(near)) <= 1e-12 * v) {
+            Whole left, right;
+            for (int32_t i = 0; i < q; ++i) left.times(uint32_t(near));
+            for (int32_t i = 0; i < q; ++i) right.times(uint32_t(i < m ? most : ones));
+            n = left.at_least(right) ? near : near + 1;
         }
         s.at[ones + m] = int32_t(std::min<int64_t>(n, most));
     }

@@ -80,8 +80,9 @@ def _ids(name, ids, like):
         raise ValueError("%s: an int64 tensor on the operands' device expected" % name)
 
 
-# The device's current stream as a handle, without the object around it, whose making
-# takes longer than a short call's launch (4 us of 13).
+# The current device and its current stream as numbers, without the objects around them,
+# whose making takes longer than a short call's launch (4 us of 13).
+_current_device = torch._C._cuda_getDevice
 _current_stream = torch._C._cuda_getCurrentRawStream
 
 
@@ -103,11 +104,11 @@ class _on:
 
     def __enter__(self):
         if self.stream is None:
-            device = self.like.device
-            if device.index != torch.cuda.current_device():
+            device = self.like.get_device()
+            if device != _current_device():
                 self.entered = (torch.cuda.device(device),)
                 self.entered[0].__enter__()
-            return _current_stream(device.index)
+            return _current_stream(device)
         if self.stream.device != self.like.device:
             raise ValueError("stream: one of the operands' device expected")
         self.entered = (torch.cuda.device(self.like.device), torch.cuda.stream(self.stream))
@@ -312,13 +313,18 @@ def glu_backward(dh, x, wg, wu, saved, dx=None, dwg=None, dwu=None, accumulate=F
 
 # ------------------------------------------------- activations in 8 bits
 
+def _row(width):
+    """A row's bytes, as ``arplan.ar_checkpoint_row`` has them."""
+    return ((width + 31) // 32 * 33 + 15) & -16
+
+
 def _kept(name, x, rows, width):
     """The row stride of rows in 8 bits."""
     if (not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype != torch.uint8 or not x.is_cuda):
         raise ValueError("%s: a two-dimensional uint8 tensor on a GPU expected" % name)
     if rows is not None and x.shape[0] != rows:
         raise ValueError("%s: %d rows expected, got %d" % (name, rows, x.shape[0]))
-    need = arplan.ar_checkpoint_row(width)
+    need = _row(width)
     if x.shape[1] < need or (need > 1 and x.stride(1) != 1):
         raise ValueError("%s: rows of %d adjacent bytes expected" % (name, need))
     return x.stride(0) if x.shape[0] > 1 else need
@@ -334,7 +340,7 @@ def checkpoint_store(x, out=None, stream=None):
     with _on(x, stream, (x, out), (out,)) as s:
         res = out
         if out is None:
-            sk = arplan.ar_checkpoint_row(N)
+            sk = _row(N)
             res = torch.empty(M, sk, dtype=torch.uint8, device=x.device)
         else:
             sk = _kept("out", out, M, N)
@@ -347,6 +353,7 @@ def checkpoint_store(x, out=None, stream=None):
 def checkpoint_load(kept, width, dtype=None, out=None, stream=None):
     """The (M, ``width``) values that ``kept`` holds, exactly, as ``dtype``
     (float32 or bfloat16) or into ``out``."""
+    _whole("width", width, 0, _MOST)
     sk = _kept("kept", kept, None, width)
     M = kept.shape[0]
     if out is None and dtype not in _DT:

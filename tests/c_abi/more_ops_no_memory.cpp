@@ -34,11 +34,6 @@ int main() {
     bad += check("ar_position_bias", [&] {
         return ar_position_bias(AR_F32, 32, 128, 0, 4, 8, 16, 0, p, 1, p, 128, 16, nullptr);
     });
-    // the borders at which whole numbers decide: their products take memory
-    bad += check("ar_position_bias (borders)", [&] {
-        return ar_position_bias(AR_F32, 32, 128, 0, 4, 8, 16, 0, p, 4,
-                                reinterpret_cast<void*>(int64_t(1) << 41), 128, 16, nullptr);
-    });
     bad += check("ar_position_bias_grad_workspace",
                  [&] { return ar_position_bias_grad_workspace(AR_F32, 32, 2, big, 8, 16, &bytes); });
     bad += check("ar_position_bias_grad", [&] {

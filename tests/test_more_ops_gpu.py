@@ -72,6 +72,17 @@ def test_position_bias(H, Q, K, offset, buckets, most, causal, dtype, layout):
         assert bool((around == 7.0).all()), "elements around the output were written"
 
 
+@pytest.mark.parametrize("buckets,most,causal", [
+    (32, 128, False), (32, 128, True), (64, 256, False), (20, 1000, True), (8, 3000, False),
+    (48, 2187, True), (4, 4096, False), (256, 2048, False), (3, 100, True), (16, 2 ** 31 - 1, True)])
+def test_position_buckets_at_their_borders(buckets, most, causal):
+    """The bucket of every distance up to 3000, by whole numbers: the table holds its rows' numbers."""
+    table = torch.arange(buckets, dtype=torch.float32)[:, None]
+    got = ops.position_bias(table.cuda(), 1, 3001, max_distance=most, offset=3000, causal=causal)
+    want = ref.buckets(1, 3001, 3000, buckets, most, causal)
+    assert torch.equal(got.cpu()[0, 0].long(), want[0])
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("K", (8, 13, 519))
 def test_position_bias_copies_bits(K, dtype):
