@@ -479,17 +479,18 @@ BiasShape shape_of(int64_t H, int64_t Q, int64_t K, int64_t offset, int64_t rows
     return s;
 }
 
-// How a gradient is shared out: as many rows a wavefront as leave four wavefronts for each
-// of the card's 1024 SIMDs, but two steps; a block's side by side along long rows, below
-// each other in many, or else in other batches; and few batches a block, whose sums run on.
-// (4 x 16 x 2048 x 2048 bf16: side by side 86 us, below each other 100; 3 x 5 x 509 x 1021
-// f32 with 64 rows a wavefront 23, with 8 14.)
+// How a gradient is shared out: as many rows a wavefront as leave two wavefronts for each
+// of the card's 1024 SIMDs, but two steps; a block's side by side along long rows, below each
+// other in many, or else in other batches; and few batches a block, whose sums run on.  (Four
+// wavefronts a SIMD: 32 x 1024 x 1024 bf16 20.1 us a call, two 18.8.  4 x 16 x 2048 x 2048
+// bf16: side by side 86 us, below each other 100.  3 x 5 x 509 x 1021 f32 with 64 rows a
+// wavefront 23, with 8 14.)
 GradArgs split_of(int64_t B, int64_t H, int64_t Q, int64_t K, int width) {
     GradArgs a{};
     a.B = B;
     const int64_t least = width / 32, chunks = ceil_div(K, width);
     int64_t rows = kGradRows;
-    while (rows > least && (rows >= 2 * Q || B * H * chunks * ceil_div(Q, rows) < 4096)) rows /= 2;
+    while (rows > least && (rows >= 2 * Q || B * H * chunks * ceil_div(Q, rows) < 2048)) rows /= 2;
     a.rows = int32_t(rows);
     a.across = chunks >= 3 ? 4 : 1;
     a.down = a.across == 1 && Q > rows ? 4 : 1;
