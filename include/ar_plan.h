@@ -655,7 +655,8 @@ ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, const void* l
  * gradient of zero, other ids outside [0, E) none of their gate's; an id that a row
  * has twice counts twice.  A NaN or +inf in a routed row makes its gradient NaN.  grad may be logits
  * itself with the same stride (in place).  coefficient is finite
- * (AR_ERR_INVALID_ARG). */
+ * (AR_ERR_INVALID_ARG).  The loss and each c_e are made in 64 bits and rounded once; where a
+ * c_e is beyond fp32's range the gradient of routed rows is not finite. */
 ar_status ar_balance(int32_t dtype, int64_t T, int64_t E, int64_t k, const void* logits,
                      int64_t logits_stride, const int64_t* ids, const int32_t* counts,
                      const float* mass, float coefficient, int32_t normalize, const float* dgates,

@@ -383,7 +383,7 @@ __global__ __launch_bounds__(1024) void route_join_kernel(int parts, int E, cons
 struct BalanceArgs {
     int64_t T, stride, grad_stride;
     int E, k, normalize;
-    float coefficient, scale;   // coefficient E / k
+    float coefficient;
     const int64_t* ids;
     const int32_t* counts;
     const float *mass, *dgates;
@@ -441,14 +441,16 @@ __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits,
         next_first = in ? a.ids[r * a.k] : -1;
     };
     fetch(r0 + group);
-    // the slopes of the loss: coefficient E counts_e / (k N^2), all counts in flight together
+    // the slopes of the loss: coefficient E counts_e / (k N^2), all counts in flight together.
+    // (Made in 64 bits and rounded once: in 32 the factor before counts_e is infinite or
+    // denormal for coefficients whose slopes are neither.)
     Logits<float, P> counts;
     counts.load(reinterpret_cast<const float*>(a.counts), first, a.E);
-    const float n = float(a.counts[a.E]), share = n > 0.0f ? 1.0f / n : 0.0f;
-    const float unit = a.scale * share * share;
+    const double n = double(a.counts[a.E]);
+    const double unit = n > 0.0 ? double(a.coefficient) * a.E / a.k / n / n : 0.0;
     float slope[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i) slope[i] = float(int32_t(counts.raw[i / 4][i % 4])) * unit;
+    for (int i = 0; i < P; ++i) slope[i] = float(double(int32_t(counts.raw[i / 4][i % 4])) * unit);
     const float plain = a.normalize ? 0.0f : 1.0f;
     for (; r0 < a.T; r0 += step) {
         const int64_t r = r0 + group;
@@ -681,7 +683,7 @@ AR_EXPORT ar_status ar_balance(int32_t dtype, int64_t T, int64_t E, int64_t k, c
     int32_t es = 0;
     AR_TRY(check_dtype("dtype", dtype, &es));
     AR_TRY(check_route_sizes(T, E, k));
-    if (!(std::abs(coefficient) <= 3.4e38f))
+    if (!std::isfinite(coefficient))
         return fail(AR_ERR_INVALID_ARG, "the coefficient is not finite");
     const int64_t rows = grad ? T : 0;
     const MatArg ml{"logits", logits, rows, E, logits_stride, es}, mi{"ids", ids, rows, k, k, 8},
@@ -694,7 +696,7 @@ AR_EXPORT ar_status ar_balance(int32_t dtype, int64_t T, int64_t E, int64_t k, c
     for (const MatArg& i : {ml, mi, mc, mm, md, mg}) AR_TRY(check_apart(mo, i));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const BalanceArgs a{T, logits_stride, grad_stride, int(E), int(k), normalize, coefficient,
-                        coefficient * float(E) / float(k), ids, counts, mass, dgates, loss};
+                        ids, counts, mass, dgates, loss};
     if (rows == 0) {
         hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(64), 0, st, a);
         return launch_status("balance loss");

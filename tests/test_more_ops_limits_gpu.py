@@ -1,0 +1,62 @@
+"""Position bias, routing with its balance loss and activations in 8 bits at the ends of
+what they accept, on the GPU, against plain definitions in 64 bits."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import more_ops_reference as ref
+
+arplan = pytest.importorskip(
+    "paper_2409_04202_amd.arplan",
+    reason="HIP library not built (run python -m paper_2409_04202_amd.build)")
+from paper_2409_04202_amd import ops  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DTYPES = ("f32", "bf16")
+U, UB = ref.U, ref.UB
+LARGEST = float(np.finfo(np.float32).max)
+
+
+def rnd(seed, *shape, dtype="f32", scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(ref.TORCH[dtype])
+
+
+def near(got, want, bound):
+    off = (got.double().cpu() - want).abs()
+    assert bool((off <= bound).all()), (float(off.max()), float((off / bound).max()))
+
+
+# --------------------------------------------------------------- balance
+
+@pytest.mark.parametrize("normalize", (False, True))
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,E,k,coefficient,many", [
+    (600, 1024, 2, 1e36, 0), (600, 1024, 2, -LARGEST, 0), (300, 512, 8, LARGEST, 0),
+    (40, 4, 1, 1e-24, 1 << 31), (40, 16, 2, 1e-22, 1 << 30)])
+def test_balance_of_extreme_coefficients(T, E, k, coefficient, many, dtype, normalize):
+    """Coefficients whose product with E leaves fp32, and counts of so many replicas that
+    E / N^2 does; an expert without choices among them.  The slopes are rounded once, the
+    gradient as in any other call."""
+    z = rnd(1, T, E, dtype=dtype)
+    ids, _, counts, mass = ref.route(z, k, None, normalize)
+    counts[3] = 0
+    if many:
+        counts[:3], counts[E] = many - 1 - torch.arange(3) * 1000003, many - 1
+    mass = mass.float()
+    loss, grad, size = ref.balance(z, ids, counts, mass, float(np.float32(coefficient)), normalize)
+    got, out = ops.balance(z.cuda(), ids.cuda(), counts.int().cuda(), mass.cuda(), coefficient,
+                           normalize, grad=torch.empty(T, E, dtype=z.dtype, device="cuda"))
+    # (a loss of 3.485e38 lies beyond the largest fp32 number, 3.403e38, by more than half of
+    # that one's last place, 2^103: rounded, it is infinite)
+    if abs(loss) >= LARGEST + 2.0 ** 103:
+        assert float(got) == math.copysign(math.inf, loss)
+    else:
+        assert abs(float(got) - loss) <= 8 * U * abs(loss)
+    # a slope of one rounding, probabilities of E + 16, a sum of E and three operations; half
+    # of the least bf16 number, and a few of fp32's
+    near(out, grad, size * (3 * (E + 16) + 16) * U
+         + (grad.abs() * UB + 2.0 ** -134 if dtype == "bf16" else grad.abs() * U) + 1e-44)
