@@ -30,6 +30,23 @@ def near(got, want, bound):
     assert bool((off <= bound).all()), (float(off.max()), float((off / bound).max()))
 
 
+# --------------------------------------------------------------- routing
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("E", (2, 8, 60, 128, 512, 1000))
+def test_mass_of_far_experts(E, dtype):
+    """Each probability of one row whose logits go down to 85 below the largest, which is 0, so
+    that no difference is rounded: an exponential to 4 units, one in the sum, whose 16 + 6
+    additions (of a lane's and over the lanes) and inverse follow, and the product."""
+    g = torch.Generator().manual_seed(2)
+    z = (torch.rand(1, E, generator=g) * -85).to(ref.TORCH[dtype])
+    z[0, E // 2], z[0, 0] = 0, -84
+    p = torch.softmax(z.double(), 1)[0]
+    ids, gates, counts, mass = ops.route(z.cuda(), min(E, 32))
+    near(mass, p, p * (4 + 4 + 22 + 2) * U)
+    near(gates[0], p[ids[0].cpu()], p[ids[0].cpu()] * (4 + 4 + 22 + 2) * U)
+
+
 # --------------------------------------------------------------- balance
 
 @pytest.mark.parametrize("normalize", (False, True))
