@@ -577,12 +577,19 @@ int group_log(int64_t E) {
     return log;
 }
 
-// Blocks of a routing: as many as the rows fill, but one for up to three times its wavefronts'
-// rows, which takes less than the join's launch (a call for 128 x 128 bf16, k = 8, 11.3 us
-// against 16.0, four times 14.2 and 16.1; fp32, twice as slow, 11.8, 20.6 and 16.0).
-int64_t parts_of(int64_t T, int64_t E, int log) {
+// Blocks of a routing: as many as the rows fill, but one where its passes over its
+// wavefronts' rows take less than a call with the join does, which are fewer for fp32's ranks
+// of 64 bits, and for many choices or all of few experts.  us of a call, and of its launches in a
+// graph, in one block and with the join:
+//   192 x 128, k = 8   bf16, 3 passes: 12.4 and 16.3, 11.2 and 8.3; fp32: 16.1 and 16.2, 16.1 and 9.6
+//   128 x 128, k = 8   2 passes: bf16 12.6 and 16.4, 8.5 and 8.2; fp32 12.3 and 16.2, 11.6 and 9.5
+//   128 x 128, k = 32  bf16, 2 passes: 14.0 and 16.5, 13.9 and 10.8; fp32: 23.0 and 16.4, 23.0 and 15.7
+//   16 x 1024, k = 32  bf16, 2 passes: 14.4 and 16.3, 14.0 and 11.7; fp32: 23.2 and 16.8, 23.1 and 15.9
+//   2048 x 8, k = 8    bf16, 2 passes: 15.7 and 16.5, 15.7 and 10.7; a third: 20.9 and 16.3
+int64_t parts_of(int32_t dtype, int64_t T, int64_t E, int64_t k, int log) {
     const int64_t rows = (route_block(E > kWideRow ? 16 : 8) / 64) * (64 >> log);
-    return T <= 3 * rows ? 1 : std::min<int64_t>(kMaxParts, ceil_div(T, rows));
+    const int64_t passes = (dtype == AR_F32 ? 1 : 2) + (k <= 8 && k < E ? 1 : 0);
+    return T <= passes * rows ? 1 : std::min<int64_t>(kMaxParts, ceil_div(T, rows));
 }
 
 // Many bf16 rows of which up to 8 are chosen: 16 logits a lane of half as many lanes, of whose
@@ -593,8 +600,8 @@ int64_t parts_of(int64_t T, int64_t E, int log) {
 bool doubled(int32_t dtype, int64_t T, int64_t E, int64_t k) {
     return dtype == AR_BF16 && k <= 8 && E > 64 && E <= kWideRow && T >= 65536;
 }
-int64_t part_bytes(int64_t T, int64_t E) {
-    const int64_t parts = parts_of(T, E, group_log(E));     // (or fewer)
+int64_t part_bytes(int64_t T, int64_t E, int64_t k) {
+    const int64_t parts = parts_of(AR_F32, T, E, k, group_log(E));  // (bf16 has as many or fewer)
     return parts > 1 ? round_up(parts * (2 * E + 1) * 4, 16) : 0;
 }
 
@@ -618,7 +625,7 @@ AR_EXPORT ar_status ar_route_workspace(int64_t T, int64_t E, int64_t k, int64_t*
     clear_error();
     if (!bytes) return fail(AR_ERR_INVALID_ARG, "bytes is NULL");
     AR_TRY(check_route_sizes(T, E, k));
-    *bytes = part_bytes(T, E);
+    *bytes = part_bytes(T, E, k);
     return AR_OK;
 } catch (...) {
     return thrown();
@@ -632,7 +639,7 @@ AR_EXPORT ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, con
     int32_t es = 0;
     AR_TRY(check_dtype("dtype", dtype, &es));
     AR_TRY(check_route_sizes(T, E, k));
-    const int64_t need = part_bytes(T, E);
+    const int64_t need = part_bytes(T, E, k);
     const MatArg ml{"logits", logits, T, E, logits_stride, es}, mv{"live", live, live ? 1 : 0, T, T, 1},
         mi{"ids", ids, T, k, k, 8}, mg{"gates", gates, T, k, k, 4},
         mc{"counts", counts, 1, E + 1, E + 1, 4}, mm{"mass", mass, 1, E, E, 4},
@@ -646,7 +653,7 @@ AR_EXPORT ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, con
         for (int p = 0; p < o; ++p) AR_TRY(check_apart(outs[o], outs[p]));
     }
     const bool twice = doubled(dtype, T, E, k);
-    const int64_t parts = parts_of(T, E, group_log(E) - (twice ? 1 : 0));
+    const int64_t parts = parts_of(dtype, T, E, k, group_log(E) - (twice ? 1 : 0));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     int32_t* const part_counts = static_cast<int32_t*>(workspace);
     float* const part_mass = reinterpret_cast<float*>(part_counts + parts * (E + 1));

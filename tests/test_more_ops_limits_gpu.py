@@ -47,6 +47,24 @@ def test_mass_of_far_experts(E, dtype):
     near(gates[0], p[ids[0].cpu()], p[ids[0].cpu()] * (4 + 4 + 22 + 2) * U)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,E,k", [
+    (1024, 8, 8), (1025, 8, 8), (2048, 8, 8), (2049, 8, 8), (3072, 8, 7), (3073, 8, 7), (128, 61, 9),
+    (129, 61, 32), (257, 61, 9), (64, 128, 32), (65, 128, 32), (129, 128, 32), (128, 128, 8), (129, 128, 8),
+    (192, 128, 8), (193, 128, 8), (49, 512, 8), (33, 512, 9), (8, 1024, 32), (9, 1024, 32), (17, 1024, 32),
+    (25, 1024, 8)])
+def test_route_on_both_sides_of_the_join(T, E, k, dtype):
+    """The largest calls of one block and the smallest of several, with ties among the logits."""
+    g = torch.Generator().manual_seed(3)
+    z = (torch.randint(-6, 7, (T, E), generator=g).float() * 0.5).to(ref.TORCH[dtype])
+    ids, gates, counts, mass = ref.route(z, k, None, True)
+    got = ops.route(z.cuda(), k, normalize=True)
+    assert torch.equal(got[0].cpu(), ids) and torch.equal(got[2].cpu().long(), counts)
+    # exponentials, sums over experts and rows, inverses and products, twice where normalized
+    near(got[1], gates, gates * (2 * (E + 12) + k + 4) * U)
+    near(got[3], mass, mass * (E + 16 + T) * U)
+
+
 # --------------------------------------------------------------- balance
 
 @pytest.mark.parametrize("normalize", (False, True))

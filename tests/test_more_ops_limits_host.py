@@ -22,3 +22,15 @@ def test_every_finite_coefficient_is_accepted(coefficient):
     with pytest.raises(arplan.ArError, match="overlaps"):
         arplan.ar_balance("bf16", 4, 16, 2, at(0), 16, at(1), at(2), at(3), coefficient, 1, at(4),
                           at(3), at(6), 16)
+
+
+@pytest.mark.parametrize("E,rows", [(8, 1024), (61, 128), (128, 64), (512, 16), (1024, 8)])
+def test_routings_that_one_block_takes(E, rows):
+    """A routing without a workspace is one block's for both types: two passes over its
+    wavefronts' rows at most, and of many choices or all experts one, for another would take
+    longer in fp32 than the blocks' join."""
+    for k in (1, 8, 9, 32):
+        if k <= E:
+            passes = 2 if k <= 8 and k < E else 1
+            assert arplan.ar_route_workspace(passes * rows, E, k) == 0
+            assert arplan.ar_route_workspace(passes * rows + 1, E, k) > 0
