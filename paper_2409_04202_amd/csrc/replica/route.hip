@@ -594,11 +594,19 @@ int64_t parts_of(int32_t dtype, int64_t T, int64_t E, int64_t k, int log) {
 
 // Many bf16 rows of which up to 8 are chosen: 16 logits a lane of half as many lanes, of whose
 // ranks the first 8 can be chosen.  A wavefront then has twice the rows for each of its
-// reductions, but half as many fit a SIMD's registers.  us with 8 and with 16 logits a lane,
-// join included: 65536 x 512 47 and 42, 65536 x 128 22 and 19, 262144 x 100 58 and 43; but
-// 16384 x 512 18.6 and 19.9, 32768 x 256 18.7 and 19.4.
-bool doubled(int32_t dtype, int64_t T, int64_t E, int64_t k) {
-    return dtype == AR_BF16 && k <= 8 && E > 64 && E <= kWideRow && T >= 65536;
+// reductions, but there are half as many wavefronts: it takes longer until blocks of 8 logits a
+// lane are more than the card's 256 CUs, of long rows more than four a CU.  us of the launches,
+// with 8 and with 16 logits a lane, k = 8:
+//   16384 x 128 (256 blocks) 9.9 and 11.2, 16547 x 128 (259) 14.1 and 11.4, 24576 x 128 14.5 and
+//   11.6, 40960 x 128 19.0 and 15.6, 65536 x 128 22.5 and 17.8, 66 experts alike
+//   8192 x 256 (256 blocks) 9.2 and 11.1, 16384 x 256 13.4 and 12.1, but 24576 x 256 15.7 and
+//   16.3, 32768 x 256 (1024) 18.5 and 17.4, 65536 x 256 28.3 and 25.1
+//   4096 x 512 (256 blocks) 9.4 and 11.3, 8192 x 512 14.0 and 12.5, but 12288 x 512 16.3 and
+//   17.1, 16384 x 512 (1024) 19.1 and 18.4, 32768 x 512 28.1 and 26.0, 65536 x 512 48.3 and 42.0
+// (k = 2: 128 experts alike; 32768 x 512 21.7 and 22.2, 65536 x 512 35.5 and 35.0.)
+bool doubled(int32_t dtype, int64_t T, int64_t E, int64_t k, int log) {
+    const int64_t rows = (route_block(8) / 64) * (64 >> log);
+    return dtype == AR_BF16 && k <= 8 && E > 64 && E <= kWideRow && T > (E <= 128 ? 256 : 1024) * rows;
 }
 int64_t part_bytes(int64_t T, int64_t E, int64_t k) {
     const int64_t parts = parts_of(AR_F32, T, E, k, group_log(E));  // (bf16 has as many or fewer)
@@ -652,7 +660,7 @@ AR_EXPORT ar_status ar_route(int32_t dtype, int64_t T, int64_t E, int64_t k, con
         AR_TRY(check_apart(outs[o], mv));
         for (int p = 0; p < o; ++p) AR_TRY(check_apart(outs[o], outs[p]));
     }
-    const bool twice = doubled(dtype, T, E, k);
+    const bool twice = doubled(dtype, T, E, k, group_log(E));
     const int64_t parts = parts_of(dtype, T, E, k, group_log(E) - (twice ? 1 : 0));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     int32_t* const part_counts = static_cast<int32_t*>(workspace);

@@ -65,6 +65,28 @@ def test_route_on_both_sides_of_the_join(T, E, k, dtype):
     near(got[3], mass, mass * (E + 16 + T) * U)
 
 
+@pytest.mark.parametrize("E,k,T,step", [
+    (66, 8, 16385, 8192), (100, 3, 17000, 8500), (128, 8, 30001, 15001), (129, 8, 33000, 16500),
+    (256, 1, 32769, 16385), (300, 5, 16385, 8193), (512, 8, 20011, 10006)])
+def test_route_of_many_rows_and_of_their_halves(E, k, T, step):
+    """bf16 rows past the limits of 16 logits a lane, with ties, absent experts and padding: what
+    is chosen is bit for bit what the halves of the rows choose, with 8."""
+    g = torch.Generator().manual_seed(4)
+    z = torch.randint(-9, 10, (T, E), generator=g).float() * 0.5 + torch.randn(1, E, generator=g).bfloat16()
+    z[torch.rand(T, E, generator=g) < 0.05] = -math.inf
+    z = z.bfloat16().cuda()
+    live = (torch.rand(T, generator=g) < 0.8).cuda()
+    ids, gates, counts, mass = ops.route(z, k, live=live, normalize=True)
+    parts = [ops.route(z[i:i + step], k, live=live[i:i + step], normalize=True)
+             for i in range(0, T, step)]
+    assert torch.equal(ids, torch.cat([p[0] for p in parts]))
+    assert torch.equal(counts, sum(p[2] for p in parts))
+    few = torch.cat([p[1] for p in parts]).double().cpu()
+    near(gates, few, few * 2 * (2 * (E + 12) + k + 4) * U + 2e-36)
+    want = sum(p[3].double() for p in parts).cpu()
+    near(mass, want, want * 2 * (E + 16 + T / 512) * U + T * 1e-36)
+
+
 # --------------------------------------------------------------- balance
 
 @pytest.mark.parametrize("normalize", (False, True))
