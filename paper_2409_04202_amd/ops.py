@@ -81,9 +81,11 @@ def _ids(name, ids, like):
 
 
 # The current device and its current stream as numbers, without the objects around them,
-# whose making takes longer than a short call's launch (4 us of 13).
-_current_device = torch._C._cuda_getDevice
-_current_stream = torch._C._cuda_getCurrentRawStream
+# whose making takes longer than a short call's launch (4 us of 13); with them where torch
+# has no such functions, as one without GPU support has not.
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_current_stream = (getattr(torch._C, "_cuda_getCurrentRawStream", None)
+                   or (lambda device: torch.cuda.current_stream(device).cuda_stream))
 
 
 class _on:

@@ -30,6 +30,22 @@ def near(got, want, bound):
     assert bool((off <= bound).all()), (float(off.max()), float((off / bound).max()))
 
 
+# --------------------------------------------------------- position bias
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,H,Q,K", [(4, 3, 32, 32), (5, 3, 32, 32), (8, 3, 32, 32), (1, 3, 250, 250),
+                                     (1, 3, 256, 256), (32, 3, 8, 8), (8, 3, 32, 256), (3, 3, 64, 1000)])
+def test_position_bias_grad_on_both_sides_of_the_join(B, H, Q, K, dtype):
+    """A head in one block or in several: whole numbers, bit for bit."""
+    g = torch.Generator().manual_seed(5)
+    d = torch.randint(-4, 5, (B, H, Q, K), generator=g).to(ref.TORCH[dtype])
+    for causal in (False, True):
+        want, _ = ref.position_bias_grad(d, 32, 0, 128, causal)
+        got = ops.position_bias_grad(d.cuda(), torch.empty(32, H, dtype=d.dtype, device="cuda"),
+                                     causal=causal)
+        assert torch.equal(got.cpu(), want.float().to(d.dtype))
+
+
 # --------------------------------------------------------------- routing
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -117,3 +133,19 @@ def test_balance_of_extreme_coefficients(T, E, k, coefficient, many, dtype, norm
     # of the least bf16 number, and a few of fp32's
     near(out, grad, size * (3 * (E + 16) + 16) * U
          + (grad.abs() * UB + 2.0 ** -134 if dtype == "bf16" else grad.abs() * U) + 1e-44)
+
+
+# ------------------------------------------------- calls, streams, graphs
+
+def test_calls_through_torchs_public_stream_functions(monkeypatch):
+    """What the functions fall back to where torch has no others: the same stream."""
+    monkeypatch.setattr(ops, "_current_device", torch.cuda.current_device)
+    monkeypatch.setattr(ops, "_current_stream", lambda d: torch.cuda.current_stream(d).cuda_stream)
+    x = rnd(6, 40, 100).cuda()
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        kept = ops.checkpoint_store(x)
+    other.synchronize()
+    monkeypatch.undo()
+    assert torch.equal(kept[:, :33 * 4], ops.checkpoint_store(x)[:, :33 * 4])

@@ -1,6 +1,10 @@
 """What position bias, routing, balance loss and activations in 8 bits accept at the ends of
 their arguments, and what the functions on tensors need of torch (no GPU call is made)."""
 
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
@@ -34,3 +38,21 @@ def test_routings_that_one_block_takes(E, rows):
             passes = 2 if k <= 8 and k < E else 1
             assert arplan.ar_route_workspace(passes * rows, E, k) == 0
             assert arplan.ar_route_workspace(passes * rows + 1, E, k) > 0
+
+
+def test_tensors_are_refused_by_a_torch_without_gpu_functions():
+    """The module imports, and refuses what is not on a GPU, where torch has no functions for
+    the current device and stream."""
+    pytest.importorskip("torch")
+    code = ("import torch\n"
+            "for n in ('_cuda_getDevice', '_cuda_getCurrentRawStream'):\n"
+            "    if hasattr(torch._C, n):\n"
+            "        delattr(torch._C, n)\n"
+            "from paper_2409_04202_amd import ops\n"
+            "try:\n"
+            "    ops.checkpoint_store(torch.zeros(2, 2))\n"
+            "except ValueError as e:\n"
+            "    print('refused:', e)\n")
+    r = subprocess.run([sys.executable, "-c", code], stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
+                       text=True, timeout=300, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and "refused: x: a GPU tensor expected" in r.stdout, r.stdout
