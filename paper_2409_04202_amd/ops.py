@@ -389,6 +389,7 @@ def route(logits, k, live=None, normalize=False, counts=None, mass=None, workspa
     (E,) (the probabilities' sums).  Rows whose ``live`` (bool (T,)) is false are
     padding.  ``counts`` and ``mass`` may be given, such as a slice of the vector
     that an int32 plan sums."""
+    _whole("k", k, 0, _MOST)
     sl = _matrix("logits", logits)
     T, E = logits.shape
     if live is not None:

@@ -103,6 +103,16 @@ def test_route_of_many_rows_and_of_their_halves(E, k, T, step):
     near(mass, want, want * 2 * (E + 16 + T / 512) * U + T * 1e-36)
 
 
+def test_route_refuses_a_number_of_choices():
+    z = rnd(7, 4, 8).cuda()
+    for k in (2.0, None, -1, (1 << 64) + 2, torch.tensor(2)):
+        with pytest.raises(ValueError):
+            ops.route(z, k)
+    for k in (0, 9):
+        with pytest.raises(arplan.ArError):
+            ops.route(z, k)
+
+
 # --------------------------------------------------------------- balance
 
 @pytest.mark.parametrize("normalize", (False, True))

@@ -56,3 +56,11 @@ def test_tensors_are_refused_by_a_torch_without_gpu_functions():
     r = subprocess.run([sys.executable, "-c", code], stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
                        text=True, timeout=300, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert r.returncode == 0 and "refused: x: a GPU tensor expected" in r.stdout, r.stdout
+
+
+@pytest.mark.parametrize("k", (2.0, "2", None, -1, (1 << 64) + 2))
+def test_a_number_of_choices_that_is_none(k):
+    torch = pytest.importorskip("torch")
+    from paper_2409_04202_amd import ops
+    with pytest.raises(ValueError, match="k: a whole number"):
+        ops.route(torch.zeros(4, 8), k)
