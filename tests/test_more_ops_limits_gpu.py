@@ -159,3 +159,164 @@ def test_calls_through_torchs_public_stream_functions(monkeypatch):
     other.synchronize()
     monkeypatch.undo()
     assert torch.equal(kept[:, :33 * 4], ops.checkpoint_store(x)[:, :33 * 4])
+
+
+def state(dtype):
+    """A replica's tensors of sizes whose routing and whose bias gradient leave parts in a
+    workspace, which another launch joins."""
+    n = lambda i, *shape: rnd(10 + i, *shape, dtype=dtype).cuda()   # noqa: E731
+    e = lambda *shape: torch.empty(*shape, dtype=ref.TORCH[dtype], device="cuda")   # noqa: E731
+    s = {"table": n(0, 32, 3), "bias": e(3, 130, 1100), "logits": n(1, 600, 40),
+         "counts": torch.empty(41, dtype=torch.int32, device="cuda"), "x": n(2, 600, 72),
+         "dlogits": e(600, 40), "dbias": n(3, 2, 3, 130, 1100), "dtable": e(32, 3)}
+    s["needs"] = (arplan.ar_route_workspace(600, 40, 2),
+                  arplan.ar_position_bias_grad_workspace(dtype, 32, 2, 3, 130, 1100))
+    assert min(s["needs"]) > 0
+    s["spaces"] = (None, None)
+    return s
+
+
+def step(s, stream=None):
+    on = {"stream": stream}
+    bias = ops.position_bias(s["table"], 130, 1100, offset=970, causal=True, out=s["bias"], **on)
+    ids, gates, counts, mass = ops.route(s["logits"], 2, normalize=True, counts=s["counts"],
+                                         workspace=s["spaces"][0], **on)
+    loss, dlogits = ops.balance(s["logits"], ids, counts, mass, normalize=True, dgates=gates,
+                                grad=s["dlogits"], **on)
+    x = ops.checkpoint_load(ops.checkpoint_store(s["x"], **on), 72, s["x"].dtype, **on)
+    dtable = ops.position_bias_grad(s["dbias"], s["dtable"], offset=970, causal=True,
+                                    workspace=s["spaces"][1], **on)
+    return bias, ids, gates, counts, mass, loss, dlogits, x, dtable
+
+
+def copies(got):
+    return [t.clone() for t in got]
+
+
+def checked(got, want):
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert torch.equal(a, b), i
+
+
+def test_a_step_of_several_blocks_against_definitions():
+    """The step that the tests below repeat, against 64 bits."""
+    s = state("f32")
+    bias, ids, gates, counts, mass, loss, dlogits, x, dtable = step(s)
+    assert torch.equal(bias.cpu(), ref.position_bias(s["table"].cpu(), 130, 1100, 970, 128, True))
+    want = ref.route(s["logits"].cpu(), 2, None, True)
+    assert torch.equal(ids.cpu(), want[0]) and torch.equal(counts.cpu().long(), want[2])
+    near(gates, want[1], want[1] * (2 * (40 + 12) + 6) * U)
+    near(mass, want[3], want[3] * (40 + 16 + 600) * U)
+    total, grad, size = ref.balance(s["logits"].cpu(), want[0], want[2], mass.cpu(), 0.01, True, gates.cpu())
+    assert abs(float(loss) - total) <= 8 * U * total
+    near(dlogits, grad, size * (3 * (40 + 16) + 4 + 16) * U + grad.abs() * U + 1e-36)
+    want, size = ref.position_bias_grad(s["dbias"].cpu(), 32, 970, 128, True)
+    # a lane's additions: rows of both batches; those over the wavefronts, the diagonals, the lanes
+    # and the slots' join, at most 64 of each
+    near(dtable, want, size * (2 * 64 + 4 * 64) * U + want.abs() * U)
+    values = ref.fetched(*ref.kept(s["x"].cpu()), 72)
+    assert torch.equal(x.cpu().double(), values)
+
+
+@pytest.mark.parametrize("given", (False, True))
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_step_of_several_blocks_captured_and_replayed(dtype, given):
+    """Two graphs of it, with workspaces of their own or sharing given ones, replayed in turn with
+    the program's own work between the replays; inputs change."""
+    s = state(dtype)
+    if given:
+        s["spaces"] = tuple(torch.full((n + 64,), 255, dtype=torch.uint8, device="cuda") for n in s["needs"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(s)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs, got = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            got.append(step(s))
+    fresh = state(dtype)
+    for i in range(5):
+        for k in ("x", "logits", "dbias", "table"):
+            s[k].copy_(fresh[k] * (1.0 if i % 2 else 0.5))
+        eager = copies(step(s))
+        for g, out in zip(graphs, got):
+            for t in out:
+                t.zero_()
+            if given:
+                for w in s["spaces"]:
+                    w.fill_(255)
+            g.replay()
+            torch.cuda.synchronize()
+            checked(out, eager)
+            for w, n in zip(s["spaces"], s["needs"]) if given else ():
+                assert bool((w[n:] == 255).all()) and not bool((w[:n] == 255).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_step_of_several_blocks_on_another_stream(dtype):
+    s = state(dtype)
+    want = copies(step(s))
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    for t in want:
+        t.record_stream(other)
+    got = step(s, other)
+    other.synchronize()
+    checked(got, want)
+
+
+def test_steps_of_several_blocks_on_two_streams_at_once():
+    a, b = state("bf16"), state("f32")
+    want = [copies(step(s)) for s in (a, b)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [None, None]
+    for _ in range(5):
+        for i, s in enumerate((a, b)):
+            with torch.cuda.stream(streams[i]):
+                got[i] = copies(step(s))
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        checked(x, y)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_given_workspaces_of_several_blocks(dtype):
+    """The bytes that were asked for and no others are written, and what they held has no effect;
+    one byte less is refused."""
+    s = state(dtype)
+    want = copies(step(s))
+    rooms = [torch.full((n + 64,), 255, dtype=torch.uint8, device="cuda") for n in s["needs"]]
+    s["spaces"] = tuple(r[:n] for r, n in zip(rooms, s["needs"]))
+    checked(step(s), want)
+    for r, n in zip(rooms, s["needs"]):
+        assert bool((r[n:] == 255).all()) and not bool((r[:n] == 255).all())
+    with pytest.raises(arplan.ArError):
+        ops.route(s["logits"], 2, workspace=rooms[0][:s["needs"][0] - 1])
+    with pytest.raises(arplan.ArError):
+        ops.position_bias_grad(s["dbias"], s["dtable"], workspace=rooms[1][:s["needs"][1] - 1])
+
+
+# ------------------------------------------------- activations in 8 bits
+
+@pytest.mark.parametrize("as_dtype", DTYPES)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,N", [(1, 1), (2, 33), (5, 31), (3, 4100), (200, 40), (33, 1001)])
+def test_runs_of_nan_into_strided_rows(M, N, dtype, as_dtype):
+    """Runs with NaN and infinities, loaded to an odd element of wider rows, and nothing beside
+    them."""
+    x = rnd(8, M, N)
+    g = torch.Generator().manual_seed(9)
+    x[torch.rand(M, N, generator=g) < 0.02] = math.nan
+    x[torch.rand(M, N, generator=g) < 0.02] = -math.inf
+    x[-1, -1] = math.inf
+    x = x.to(ref.TORCH[dtype])
+    want = ref.fetched(*ref.kept(x), N)
+    assert bool(want.isnan().any())
+    around = torch.full((M + 1, N + 5), 7.0, dtype=ref.TORCH[as_dtype], device="cuda")
+    ops.checkpoint_load(ops.checkpoint_store(x.cuda()), N, out=around[:M, 3:3 + N])
+    got = around[:M, 3:3 + N].cpu().double()
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got.nan_to_num(0.0), want.nan_to_num(0.0))
+    around[:M, 3:3 + N] = 7.0
+    assert bool((around == 7.0).all()), "elements around the output were written"

@@ -64,3 +64,25 @@ def test_a_number_of_choices_that_is_none(k):
     from paper_2409_04202_amd import ops
     with pytest.raises(ValueError, match="k: a whole number"):
         ops.route(torch.zeros(4, 8), k)
+
+
+def test_workspaces_of_several_blocks_are_asked_for():
+    """A byte less than asked for, none, one off 16 bytes, and those that are an operand's, at the
+    smallest sizes that need any."""
+    def refused(f, *args):
+        with pytest.raises(arplan.ArError) as e:
+            f(*args)
+        assert e.value.status == arplan.AR_ERR_INVALID_ARG
+
+    for dtype, B, Q, K in (("bf16", 5, 32, 32), ("f32", 9, 32, 32), ("f32", 2, 130, 1100)):
+        need = arplan.ar_position_bias_grad_workspace(dtype, 32, B, 4, Q, K)
+        assert need > 0
+        for space, n in ((at(2), need - 1), (None, need), (at(2) + 8, need), (at(0), need), (at(1), need)):
+            refused(arplan.ar_position_bias_grad, dtype, 32, 128, 0, B, 4, Q, K, 0, at(0), 4 * Q * K,
+                    Q * K, K, 0, at(1), 4, space, n)
+    need = arplan.ar_route_workspace(385, 40, 2)
+    assert need > 0
+    for dtype in ("bf16", "f32"):
+        for space, n in ((at(6), need - 1), (None, need), (at(6) + 8, need), (at(0), need), (at(2), need)):
+            refused(arplan.ar_route, dtype, 385, 40, 2, at(0), 40, None, 1, at(2), at(3), at(4), at(5),
+                    space, n)
