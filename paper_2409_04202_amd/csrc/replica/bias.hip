@@ -99,7 +99,7 @@ __device__ __forceinline__ T element(const u32x4 v, int e) {
 
 // The values of a patch's diagonals lie in LDS; a lane reads those of VEC rows at once,
 // and their vectors are parts of them.  Bound by memory, the matrix is written once: 16 x
-// 2048 x 2048 bf16, 134 MB, 26.4 us, 5.1 TB/s (a fill of that size 24).  Lanes that keep a
+// 2048 x 2048 bf16, 134 MB, 26.4 us, 5.1 TB/s (a fill of that size 24), f32 51, 5.3.  Lanes that keep a
 // vector of diagonals and store it one element further on in each row, off 16 bytes, took 28.3;
 // rows of 1 KB a block in place of whole ones of 4 KB 31.8.  One query over 4001 keys for 32
 // heads: 5.0, the borders' and the table's way to LDS and the lookups.
@@ -261,7 +261,9 @@ __device__ __forceinline__ void sum_patch(const T* from, const T* end, int64_t s
         if (lane == 63) d.put(sums + (63 + steps - step) * VEC, first);
         d.step();
     };
-    if constexpr (EDGE) {  // (with another step's vectors there are registers too few)
+    // (Of bf16, with another step's vectors there are registers too few; fp32's are half as
+    // many, and its steps wait here all the same: a second one in flight has not been built.)
+    if constexpr (EDGE) {
         u32x4 w[VEC];
 #pragma unroll 1
         for (int step = 0; step < steps; ++step) {
@@ -298,8 +300,10 @@ __device__ __forceinline__ void sum_patch(const T* from, const T* end, int64_t s
 // A block's sums by bucket, to its slot of `part`, or straight to the table where a
 // head has one slot.  Bound by memory, the gradients pass once: 4 x 16 x 2048 x 2048 bf16, 537
 // MB, 85 us, 6.3 TB/s, its join 4.6.  (Lanes that walk down their diagonals, each row's
-// vector off 16 bytes by one element more: 113.)  3 x 5 x 509 x 1021 f32, of which 23 MB are
-// seen: 13.6 and 3.8, the steps of a block one after the other.
+// vector off 16 bytes by one element more: 113.)  In f32, 1074 MB, 195, 5.5 TB/s, and 4.8.  3 x 5
+// x 509 x 1021 f32, of which 23 MB are seen: 13.8 and 4.0, the steps of a block one after the other.
+// Keys fewer than 64 vectors leave lanes idle: 32 x 16 x 1024 x 48, 50 MB in bf16 and 101 in f32,
+// 47 and 43.
 template <class T>
 __global__ __launch_bounds__(kBlock, 4) void bias_grad_kernel(BiasShape s, Borders borders, GradArgs a,
                                                            const T* d, int32_t buckets, float* part,
@@ -491,7 +495,9 @@ GradArgs split_of(int64_t B, int64_t H, int64_t Q, int64_t K, int width) {
     const int64_t least = width / 32, chunks = ceil_div(K, width);
     // A head in one block, without a join, where a lane gets at most 256 elements: 8 x 128 x
     // 128 bf16 10.3 us a call against 15.4, f32 9.8 and 15.1, 8 x 256 x 256 f32 9.9 and 14.5;
-    // with twice as many in bf16 14.3 and 15.1, with four times 22 and 15.
+    // with twice as many in bf16 14.3 and 15.1, with four times 22 and 15.  256 of f32 rows that
+    // end inside a wavefront's columns are the longest: a call as long as with the join, 8 x 250 x
+    // 250 12.6 and 14.6, 8 x 8 x 32 x 32 14.9 and 14.4, but in a graph 12.2 and 8.7, 14.5 and 8.5.
     for (int64_t rows = least; rows <= kGradRows; rows *= 2) {
         a.across = chunks > 1 ? 4 : 1;
         a.down = a.across == 1 && Q > rows ? 4 : 1;

@@ -20,7 +20,8 @@ ar_status check_block8(const char* name, const void* p, int64_t rows, int64_t wi
 namespace {
 
 // 16 elements a lane, half of a run, whose numbers are one vector.  Bound by memory: 8192 x
-// 16384 bf16 84 us, 4.9 TB/s.  (8 elements a lane, or stores past the caches: 89.)
+// 16384 bf16 84 us, 4.9 TB/s.  (8 elements a lane, or stores past the caches: 89.)  Of fp32 a
+// load takes 16 of every 64 bytes: 8192 x 8192 78 us, 4.3 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void keep_kernel(int64_t M, int64_t N, Cover c, const T* x,
                                                    int64_t x_stride, uint8_t* kept, int64_t stride) {
@@ -61,9 +62,10 @@ __global__ __launch_bounds__(256) void keep_kernel(int64_t M, int64_t N, Cover c
     }
 }
 
-// 8 elements a lane, so that a wavefront's every store is to adjacent bytes, and two strips
-// at a time, whose loads are in flight together.  Bound by memory: 8192 x 16384 bf16 63 us,
-// 6.5 TB/s (16 elements a lane 71).
+// 8 elements a lane, so that a wavefront's every store of bf16 is to adjacent bytes, and two
+// strips at a time, whose loads are in flight together.  Bound by memory: 8192 x 16384 bf16 63
+// us, 6.5 TB/s (16 elements a lane 71).  Of fp32 a store takes 16 of every 32 bytes: 8192 x 8192
+// 79 us, 4.3 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void fetch_kernel(int64_t M, int64_t N, Cover c,
                                                     const uint8_t* kept, int64_t stride, T* x,

@@ -30,7 +30,7 @@ __device__ __forceinline__ float exp_below(float x) {
 }
 // The same where what is made of it is rounded to bf16: as the hardware has it, |x| units
 // off, 2^-17 of the value at most, of which a rounding of 2^-9 leaves nothing.  (A routing's
-// masses and gates are fp32: they take exp_below, 65536 x 512 bf16 44.6 us for 42.0.)
+// masses and gates are fp32: they take exp_below, 65536 x 512 bf16 44.8 us for 42.2.)
 template <bool ROUGH>
 __device__ __forceinline__ float exp_of_logit(float x) {
     if constexpr (ROUGH) return __builtin_amdgcn_exp2f(fmaxf(x, -200.0f) * 1.44269504f);
@@ -236,8 +236,10 @@ struct RouteArgs {
 // first ones, and the lane that it came from moves on to its next.  Lane j keeps choice
 // j, so gates, counts and stores are made for all of them at once.  The block's sums over its
 // rows go to a part of their own, added in order by another launch: no atomics on floats.
-// Bound by the vector units, by the ranks' sort and the choices: 65536 x 512 bf16, k = 8,
-// 44.6 us (a maximum over all logits for each choice 129), 16384 x 128 7.6.
+// Bound by the vector units, by the ranks' sort and the choices, 43 operations a bf16 logit:
+// they are busy for nearly all of the time that 65536 x 512 bf16, k = 8, takes, 44.8 us (a maximum
+// over all logits for each choice 129); 16384 x 128 7.6.  fp32's ranks of 64 bits take twice that,
+// 92 us, and 10.2.
 template <class T, int LOG, int P, int LIST>
 __global__ __launch_bounds__(route_block(P)) void route_kernel(const T* logits, RouteArgs a) {
     constexpr int BLOCK = route_block(P);
@@ -405,8 +407,8 @@ __global__ __launch_bounds__(64) void loss_kernel(BalanceArgs a) { loss_of(a); }
 // The gradient, and in the last block the loss.  What is chosen reaches the lanes that
 // hold its logits through LDS: a place a logit, with the choice's number (0: none) and
 // its gate's gradient.  65536 x 512 bf16, k = 8: 35 us, 3.9 TB/s, bound by the vector units
-// (with every choice compared at every logit 87).  At most five blocks a CU, all that fit its
-// registers: 16384 blocks, each of which gets the slopes first, took 87.
+// (with every choice compared at every logit 87); fp32 52, 5.2 TB/s.  At most five blocks a CU, all
+// that fit its registers: 16384 blocks, each of which gets the slopes first, took 87.
 template <class T, int LOG, int P>
 __global__ __launch_bounds__(kBalanceBlock) void balance_kernel(const T* logits, T* grad, BalanceArgs a) {
     constexpr int VEC = Num<T>::VEC;

@@ -270,8 +270,9 @@ def glu_backward(dh, x, wg, wu, saved, dx=None, dwg=None, dwu=None, accumulate=F
                  workspace=None, stream=None):
     """(dx, dwg, dwu) for ``dh`` (M, F), the gradient at ``glu_forward``'s
     result, and what that saved.  With bfloat16 the gradients at the two
-    projections are rounded to it before the products, and the results again.  Outputs that are given are written in place;
-    with ``accumulate`` dwg and dwu are added to (and have to be given)."""
+    projections are rounded to it before the products, and the results again.
+    Outputs that are given are written in place; with ``accumulate`` dwg and dwu
+    are added to (and have to be given)."""
     sh = _matrix("dh", dh)
     M, F = dh.shape
     sx = _matrix("x", x, None, dh)

@@ -320,3 +320,20 @@ def test_runs_of_nan_into_strided_rows(M, N, dtype, as_dtype):
     assert torch.equal(got.nan_to_num(0.0), want.nan_to_num(0.0))
     around[:M, 3:3 + N] = 7.0
     assert bool((around == 7.0).all()), "elements around the output were written"
+
+
+@pytest.mark.parametrize("M,D,F", [(70, 90, 110), (300, 200, 515), (1, 64, 40), (777, 130, 64)])
+def test_glu_gradients_from_8_bits_lose_the_rounding_of_dg_and_du_alone(M, D, F):
+    """bf16: 64-bit products of dg and du, each rounded to bf16 once as the matrices are (before
+    that they are exact: 8 bits times 7), up to fp32 sums and the result's own rounding."""
+    x, wg, wu, dh = (rnd(20 + i, *s, dtype="bf16") for i, s in
+                     enumerate(((M, D), (F, D), (F, D), (M, F))))
+    factors = [rnd(24 + i, M, F) for i in range(2)]
+    saved = torch.stack([ops.checkpoint_store(f.cuda()) for f in factors])
+    dg, du = ((dh.double() * ref.fetched(*ref.kept(f), F)).float().bfloat16().double() for f in factors)
+    X, G, W = x.double(), wg.double(), wu.double()
+    got = ops.glu_backward(dh.cuda(), x.cuda(), wg.cuda(), wu.cuda(), saved)
+    for out, want, size, n in ((got[0], dg @ G + du @ W, dg.abs() @ G.abs() + du.abs() @ W.abs(), 2 * F),
+                               (got[1], dg.T @ X, dg.T.abs() @ X.abs(), M),
+                               (got[2], du.T @ X, du.T.abs() @ X.abs(), M)):
+        near(out, want, size * (n + 2) * U + want.abs() * UB + 1e-38)
