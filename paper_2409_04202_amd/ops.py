@@ -29,6 +29,8 @@ gradients enabled a tensor that requires one raises ValueError (call under
 given tensor counts as a change of it, as of any torch call in place.
 """
 
+from operator import index
+
 import torch
 from torch.autograd.graph import increment_version
 
@@ -71,8 +73,14 @@ def _strides(name, x, shape, like):
 
 
 def _whole(name, v, low, high):
-    if not isinstance(v, int) or not low <= v <= high:
+    """The whole number, of any type that is one."""
+    try:
+        n = index(v)
+    except TypeError:
+        n = low - 1
+    if not low <= n <= high:
         raise ValueError("%s: a whole number from %d to %d expected" % (name, low, high))
+    return n
 
 
 def _ids(name, ids, like):
@@ -192,10 +200,9 @@ def position_bias(table, queries, keys, max_distance=128, offset=0, causal=False
     them."""
     st = _matrix("table", table)
     buckets, H = table.shape
-    for name, v in (("queries", queries), ("keys", keys)):
-        _whole(name, v, 0, _MOST)
-    _whole("max_distance", max_distance, 1, _MOST)
-    _whole("offset", offset, -1 << 62, 1 << 62)
+    queries, keys = _whole("queries", queries, 0, _MOST), _whole("keys", keys, 0, _MOST)
+    max_distance = _whole("max_distance", max_distance, 1, _MOST)
+    offset = _whole("offset", offset, -1 << 62, 1 << 62)
     with _on(table, stream, (table, out), (out,)) as s:
         if out is None:
             res = torch.empty(H, queries, keys, dtype=table.dtype, device=table.device)
@@ -218,8 +225,8 @@ def position_bias_grad(dbias, dtable, max_distance=128, offset=0, causal=False, 
         dbias = dbias[None]
     if not isinstance(dbias, torch.Tensor) or dbias.dim() != 4:
         raise ValueError("dbias: a (batch, heads, queries, keys) tensor expected")
-    _whole("max_distance", max_distance, 1, _MOST)
-    _whole("offset", offset, -1 << 62, 1 << 62)
+    max_distance = _whole("max_distance", max_distance, 1, _MOST)
+    offset = _whole("offset", offset, -1 << 62, 1 << 62)
     B, H, Q, K = dbias.shape
     buckets = dtable.shape[0]
     if dtable.shape[1] != H:
@@ -356,7 +363,7 @@ def checkpoint_store(x, out=None, stream=None):
 def checkpoint_load(kept, width, dtype=None, out=None, stream=None):
     """The (M, ``width``) values that ``kept`` holds, exactly, as ``dtype``
     (float32 or bfloat16) or into ``out``."""
-    _whole("width", width, 0, _MOST)
+    width = _whole("width", width, 0, _MOST)
     sk = _kept("kept", kept, None, width)
     M = kept.shape[0]
     if out is None and dtype not in _DT:
@@ -390,7 +397,7 @@ def route(logits, k, live=None, normalize=False, counts=None, mass=None, workspa
     (E,) (the probabilities' sums).  Rows whose ``live`` (bool (T,)) is false are
     padding.  ``counts`` and ``mass`` may be given, such as a slice of the vector
     that an int32 plan sums."""
-    _whole("k", k, 0, _MOST)
+    k = _whole("k", k, 0, _MOST)
     sl = _matrix("logits", logits)
     T, E = logits.shape
     if live is not None:
