@@ -15,7 +15,7 @@ namespace {
 constexpr int kBalanceBlock = 256;
 constexpr int kWideRow = 512;   // experts above which a lane holds 16 logits
 // (Of blocks with 16 logits a lane a CU's registers hold one of 1024 lanes, and all 512 parts
-// at once as blocks of 512: 65536 x 512 44 and 42 us.)
+// at once as blocks of 512: 65536 x 512 46.4 and 44.2 us with the join.)
 constexpr int route_block(int logits) { return logits == 16 ? 512 : 1024; }
 constexpr int kMaxParts = 512;  // blocks whose sums are joined: two a CU, all its wavefronts
 
@@ -583,11 +583,13 @@ int group_log(int64_t E) {
 // wavefronts' rows take less than a call with the join does, which are fewer for fp32's ranks
 // of 64 bits, and for many choices or all of few experts.  us of a call, and of its launches in a
 // graph, in one block and with the join:
-//   192 x 128, k = 8   bf16, 3 passes: 12.4 and 16.3, 11.2 and 8.3; fp32: 16.1 and 16.2, 16.1 and 9.6
-//   128 x 128, k = 8   2 passes: bf16 12.6 and 16.4, 8.5 and 8.2; fp32 12.3 and 16.2, 11.6 and 9.5
-//   128 x 128, k = 32  bf16, 2 passes: 14.0 and 16.5, 13.9 and 10.8; fp32: 23.0 and 16.4, 23.0 and 15.7
-//   16 x 1024, k = 32  bf16, 2 passes: 14.4 and 16.3, 14.0 and 11.7; fp32: 23.2 and 16.8, 23.1 and 15.9
-//   2048 x 8, k = 8    bf16, 2 passes: 15.7 and 16.5, 15.7 and 10.7; a third: 20.9 and 16.3
+//   192 x 128, k = 8   bf16, 3 passes: 13.1 and 18.0, 11.7 and 8.2; fp32: 16.3 and 17.7, 16.1 and 9.6
+//   128 x 128, k = 8   2 passes: bf16 13.3 and 17.9, 8.7 and 8.2; fp32 13.2 and 17.8, 11.5 and 9.6
+//   128 x 128, k = 32  bf16, 2 passes: 14.5 and 17.7, 14.1 and 10.8; fp32: 23.0 and 17.6, 23.0 and 15.6
+//   16 x 1024, k = 32  bf16, 2 passes: 14.3 and 17.8, 13.7 and 12.6; fp32: 23.2 and 17.6, 23.0 and 15.9
+//   2048 x 8, k = 8    bf16, 2 passes: 15.8 and 17.7, 15.7 and 10.7; fp32: 15.6 and 17.5, 15.3 and 11.5
+// (In calls alone fp32's third pass of k = 8, and its second of 8 of 8, gain little beside what
+// they cost a graph; bf16's third of 8 of 8 takes 20.9 and 16.3.)
 int64_t parts_of(int32_t dtype, int64_t T, int64_t E, int64_t k, int log) {
     const int64_t rows = (route_block(E > kWideRow ? 16 : 8) / 64) * (64 >> log);
     const int64_t passes = (dtype == AR_F32 ? 1 : 2) + (k <= 8 && k < E ? 1 : 0);
@@ -599,13 +601,13 @@ int64_t parts_of(int32_t dtype, int64_t T, int64_t E, int64_t k, int log) {
 // reductions, but there are half as many wavefronts: it takes longer until blocks of 8 logits a
 // lane are more than the card's 256 CUs, of long rows more than four a CU.  us of the launches,
 // with 8 and with 16 logits a lane, k = 8:
-//   16384 x 128 (256 blocks) 9.9 and 11.2, 16547 x 128 (259) 14.1 and 11.4, 24576 x 128 14.5 and
-//   11.6, 40960 x 128 19.0 and 15.6, 65536 x 128 22.5 and 17.8, 66 experts alike
-//   8192 x 256 (256 blocks) 9.2 and 11.1, 16384 x 256 13.4 and 12.1, but 24576 x 256 15.7 and
-//   16.3, 32768 x 256 (1024) 18.5 and 17.4, 65536 x 256 28.3 and 25.1
-//   4096 x 512 (256 blocks) 9.4 and 11.3, 8192 x 512 14.0 and 12.5, but 12288 x 512 16.3 and
-//   17.1, 16384 x 512 (1024) 19.1 and 18.4, 32768 x 512 28.1 and 26.0, 65536 x 512 48.3 and 42.0
-// (k = 2: 128 experts alike; 32768 x 512 21.7 and 22.2, 65536 x 512 35.5 and 35.0.)
+//   16384 x 128 (256 blocks) 10.1 and 11.6, 16547 x 128 (259) 14.0 and 11.7, 24576 x 128 14.7 and
+//   12.0, 40960 x 128 18.9 and 16.0, 65536 x 128 22.3 and 17.5, 66 experts alike
+//   8192 x 256 (256 blocks) 9.3 and 11.4, 16384 x 256 13.6 and 12.3, but 24576 x 256 15.9 and
+//   16.7, 32768 x 256 (1024) 19.1 and 17.7, 65536 x 256 29.6 and 26.2
+//   4096 x 512 (256 blocks) 9.5 and 11.4, 8192 x 512 13.9 and 12.4, but 12288 x 512 16.1 and
+//   17.3, 16384 x 512 (1024) 19.2 and 18.6, 32768 x 512 29.2 and 26.7, 65536 x 512 50.0 and 44.1
+// (k = 2: 128 experts alike; 32768 x 512 22.6 and 23.0, 65536 x 512 37.4 and 36.8.)
 bool doubled(int32_t dtype, int64_t T, int64_t E, int64_t k, int log) {
     const int64_t rows = (route_block(8) / 64) * (64 >> log);
     return dtype == AR_BF16 && k <= 8 && E > 64 && E <= kWideRow && T > (E <= 128 ? 256 : 1024) * rows;
